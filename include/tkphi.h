@@ -359,6 +359,115 @@ int32_t tkphi_budget_paper(int64_t L, int32_t r_bp, int32_t n_sink, int32_t n_ta
 /* K = floor(r |M|): budget as a fraction of the mid-region size; r in basis points. */
 int32_t tkphi_budget_mid(int64_t L, int32_t r_bp, int32_t n_sink, int32_t n_tail);
 
+/* ---- paged key/value cache ------------------------------------------------------------------------
+ * What a serving program runs next to the calls above, on a cache whose pages lie anywhere in a pool:
+ *   tkphi_kv_append        rotates new queries and keys to their positions, writes keys and values to
+ *                          their pages, and the mean key of every block of tokens that fills up
+ *   tkphi_paged_attention  new tokens (one, a few, a chunk, a whole prompt) over everything cached,
+ *                          causal, optionally through a window
+ *   tkphi_block_attention  new tokens over the first and last blocks of their sequence and those whose
+ *                          mean keys score highest against them
+ * Token t of a sequence is row t % page_tokens of page pages[seq][t / page_tokens].  A step brings
+ * new_tokens more tokens per sequence behind the `cached` that are there; the tokens of all sequences
+ * stand one behind another in the rows of q, k, v and out.  tkphi_kv_append comes first: the attention
+ * calls read the new tokens' keys and values from their pages, like all others.
+ *
+ * All structs below are HOST structs, read at call time; the pointers inside are DEVICE pointers.
+ * The calls allocate nothing, only enqueue, and may be captured into a HIP graph (the lengths are read
+ * by the kernels: a captured step serves others within the same bounds).  Deterministic.
+ * Rows, strides and pointers are multiples of 16 bytes unless said otherwise.
+ *
+ * What the host cannot see is checked by the kernels and recorded in the workspace's status word
+ * (tkphi_read_device_status): a sequence with cached or new_tokens negative, new_tokens > max_new,
+ * cached + new_tokens > max_len, rows outside [0, rows) is skipped (TKPHI_DEV_BAD_LENGTH; its outputs
+ * are left alone); a page id outside [-1, n_pages), or -1 (absent) where tkphi_kv_append has to write,
+ * counts as absent (TKPHI_DEV_BAD_PAGE).  Tokens of absent pages are seen by nobody; a query that sees
+ * nothing gets the output 0 and lse -inf.  What a query does not see does not touch its output,
+ * whatever the memory holds there.
+ *
+ * The workspace must be 256-byte aligned and ZERO before its first use (tkphi_paged_workspace_bytes of them
+ * suffice for one step description and all smaller ones).  The calls leave what has to be zero at zero;
+ * status bits stay until the caller clears the first 4 bytes.  Two calls that overlap in time must not share one. */
+typedef struct tkphi_paged_config {
+  int32_t n_q_heads;     /* a multiple of n_kv_heads, ratio <= 8                                    */
+  int32_t n_kv_heads;
+  int32_t d_head;        /* 64 or 128                                                               */
+  int32_t kv_dtype;      /* tkphi_dtype of q, k, v, out and the cache                               */
+  float score_scale;     /* > 0 and finite                                                          */
+  int32_t page_tokens;   /* tokens per page, >= 1                                                   */
+  int64_t stride_page;   /* elements between pages, heads and tokens of K and of V (channels adjoin): */
+  int64_t stride_head;   /*   [page][head][token][channel] or [page][token][head][channel]          */
+  int64_t stride_tok;
+  int32_t window;        /* tkphi_paged_attention: tokens a query sees, its own among them; 0 = all  */
+  int32_t rot_dim;       /* tkphi_kv_append: rotated channels (the first ones), a multiple of 16; 0 = none */
+  int32_t rot_adjacent;  /* pairs (2j, 2j + 1) instead of (j, j + rot_dim / 2)                       */
+  int32_t block;         /* tokens per block: 16, 32 or 64, page_tokens a multiple of it; 0 = no blocks */
+  int32_t first_blocks;  /* tkphi_block_attention: the first and last blocks, which every query sees (last_blocks >= 1: its own */
+  int32_t last_blocks;   /*   among them), and how many of the others it retrieves; the three add up to at most 1024 */
+  int32_t top_blocks;
+  int32_t workgroups;    /* attention calls: workgroups that the cached tokens are spread over (tests, tuning); 0 = by the step */
+  int32_t reserved[4];   /* 0 */
+} tkphi_paged_config;
+
+typedef struct tkphi_step {
+  const int32_t* seqs;   /* [n_seqs][4]: cached, new_tokens, first row, 0                           */
+  const int32_t* pages;  /* [n_seqs][max_pages] page ids; -1 = absent                               */
+  int32_t n_seqs;        /* at most 65535                                                           */
+  int32_t max_pages;
+  int32_t rows;          /* rows of q, k, v, out                                                    */
+  int32_t max_new;       /* bounds over the sequences: new_tokens,                                  */
+  int32_t max_len;       /*   cached + new_tokens (tokens past max_pages pages count as absent)      */
+  int32_t reserved;      /* 0 */
+} tkphi_step;
+
+typedef struct tkphi_kv_pool {
+  void* K;               /* keys and values, strides of the config                                  */
+  void* V;
+  void* M;               /* mean keys [n_pages][n_kv_heads][page_tokens / block][d_head]; may be NULL where config.block is 0 */
+  int32_t n_pages;
+  int32_t reserved;      /* 0 */
+} tkphi_kv_pool;
+
+/* New tokens for tkphi_kv_append; strides in elements between rows (tokens) and heads. */
+typedef struct tkphi_new_rows {
+  const void* q;         /* [rows][n_q_heads][d_head]; NULL: only keys and values                   */
+  const void* k;         /* [rows][n_kv_heads][d_head]                                              */
+  const void* v;
+  void* q_rot;           /* rotated queries; may be q itself                                        */
+  const double* inv_freq;/* [rot_dim / 2] radians per position; the angle of position p is p * inv_freq[j] in 64 bits */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, q_rot_row, q_rot_head;
+} tkphi_new_rows;
+
+typedef struct tkphi_attention_rows {
+  const void* q;         /* [rows][n_q_heads][d_head] (rotated)                                     */
+  void* out;             /* [rows][n_q_heads][d_head]                                               */
+  float* lse;            /* tkphi_paged_attention: natural log of the sum of exponentials [rows][n_q_heads]; may be NULL.  4-byte aligned */
+  int64_t q_row, q_head, out_row, out_head;
+} tkphi_attention_rows;
+
+/* bits of the device status word */
+#define TKPHI_DEV_BAD_PAGE 4u
+
+/* Bytes of zeroed DEVICE workspace that the three calls need for a step (only its bounds are read: n_seqs, rows,
+ * max_new, max_len); the same for all smaller bounds.  0 if the config or the step is invalid. */
+size_t tkphi_paged_workspace_bytes(const tkphi_paged_config* cfg, const tkphi_step* step);
+
+/* q_rot, K, V and M of the step's new tokens.  Token i of a sequence has position cached + i.  Pairs of
+ * channels (a, b) turn to (a cos - b sin, a sin + b cos); channels from rot_dim on, and values, are copied.  A block's
+ * mean is taken over its keys as stored, summed in 32 bits, when its last token arrives. */
+tkphi_status tkphi_kv_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
+                             const tkphi_new_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* out = softmax(score_scale q K^T) V and lse over the tokens t <= cached + i of the sequence (and t > cached + i - window). */
+tkphi_status tkphi_paged_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
+                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* The same over blocks: of the sequence's blocks up to the query's own, the first first_blocks, the last last_blocks, and of the
+ * others the top_blocks with the highest max over the KV head's queries of q . M_b (compared in 64 bits, ties to the lower
+ * block; blocks whose score is NaN or -inf are not retrieved).  lse is not written; window must be 0. */
+tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
+                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, never-null strings. */
 const char* tkphi_status_string(int32_t status);
 const char* tkphi_last_error(void);

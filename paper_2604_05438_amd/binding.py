@@ -21,13 +21,14 @@ TKPHI_MODE_SUB, TKPHI_MODE_NOSUB, TKPHI_MODE_TOPK_ONLY = 0, 1, 2
 TKPHI_FLAG_DIAG = 0x100
 TKPHI_PHI_EXP_AFFINE, TKPHI_PHI_MLP = 0, 1
 TKPHI_DIAG_STRIDE = 8
-TKPHI_DEV_BAD_LENGTH, TKPHI_DEV_CLAMPED = 1, 2
+TKPHI_DEV_BAD_LENGTH, TKPHI_DEV_CLAMPED, TKPHI_DEV_BAD_PAGE = 1, 2, 4
 
 EXPORTS = (
     "tkphi_workspace_bytes", "tkphi_build_summaries", "tkphi_decode", "tkphi_decode_static", "tkphi_decode_stage_times",
     "tkphi_check_problems",
     "tkphi_read_device_status", "tkphi_budget_paper", "tkphi_budget_mid", "tkphi_status_string",
     "tkphi_last_error",
+    "tkphi_paged_workspace_bytes", "tkphi_kv_append", "tkphi_paged_attention", "tkphi_block_attention",
 )
 
 
@@ -76,6 +77,43 @@ class tkphi_problem(C.Structure):
     ]
 
 
+class tkphi_paged_config(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32), ("kv_dtype", C.c_int32),
+        ("score_scale", C.c_float), ("page_tokens", C.c_int32),
+        ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_tok", C.c_int64),
+        ("window", C.c_int32), ("rot_dim", C.c_int32), ("rot_adjacent", C.c_int32), ("block", C.c_int32),
+        ("first_blocks", C.c_int32), ("last_blocks", C.c_int32), ("top_blocks", C.c_int32), ("workgroups", C.c_int32),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
+class tkphi_step(C.Structure):
+    _fields_ = [
+        ("seqs", C.c_void_p), ("pages", C.c_void_p), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("rows", C.c_int32),
+        ("max_new", C.c_int32), ("max_len", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
+class tkphi_kv_pool(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("M", C.c_void_p), ("n_pages", C.c_int32), ("reserved", C.c_int32)]
+
+
+class tkphi_new_rows(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_rot", C.c_void_p), ("inv_freq", C.c_void_p),
+        ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+        ("v_row", C.c_int64), ("v_head", C.c_int64), ("q_rot_row", C.c_int64), ("q_rot_head", C.c_int64),
+    ]
+
+
+class tkphi_attention_rows(C.Structure):
+    _fields_ = [
+        ("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+        ("q_row", C.c_int64), ("q_head", C.c_int64), ("out_row", C.c_int64), ("out_head", C.c_int64),
+    ]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -115,6 +153,14 @@ def lib() -> C.CDLL:
         L.tkphi_status_string.argtypes = [C.c_int32]
         L.tkphi_last_error.restype = C.c_char_p
         L.tkphi_last_error.argtypes = []
+        pcfg, stepp, poolp = C.POINTER(tkphi_paged_config), C.POINTER(tkphi_step), C.POINTER(tkphi_kv_pool)
+        L.tkphi_paged_workspace_bytes.restype = C.c_size_t
+        L.tkphi_paged_workspace_bytes.argtypes = [pcfg, stepp]
+        for name, rows in (("tkphi_kv_append", tkphi_new_rows), ("tkphi_paged_attention", tkphi_attention_rows),
+                           ("tkphi_block_attention", tkphi_attention_rows)):
+            f = getattr(L, name)
+            f.restype = C.c_int
+            f.argtypes = [pcfg, stepp, poolp, C.POINTER(rows), C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
         return L
 
@@ -194,6 +240,25 @@ def tkphi_read_device_status(workspace_ptr: int, stream: int) -> int:
     return out.value
 
 
+def tkphi_paged_workspace_bytes(cfg: tkphi_paged_config, step: tkphi_step) -> int:
+    return lib().tkphi_paged_workspace_bytes(C.byref(cfg), C.byref(step))
+
+
+def tkphi_kv_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_new_rows, workspace_ptr: int,
+                    workspace_bytes: int, stream: int) -> None:
+    _check(lib().tkphi_kv_append(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
+
+
+def tkphi_paged_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_attention_rows, workspace_ptr: int,
+                          workspace_bytes: int, stream: int) -> None:
+    _check(lib().tkphi_paged_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
+
+
+def tkphi_block_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_attention_rows, workspace_ptr: int,
+                          workspace_bytes: int, stream: int) -> None:
+    _check(lib().tkphi_block_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
+
+
 # ---- marshalling helpers (device memory via torch) -----------------------------------------
 def make_config(n_q_heads, n_kv_heads, d_head, d_phi, n_sink, n_tail, dtype, score_scale, phi_in_scale,
                 phi_norm_coef, cache_features=0, phi_kind=0, d_emb=0, max_gen=0, tuning=None) -> tkphi_config:
@@ -246,6 +311,92 @@ def upload_problems(problems, device="cuda"):
 def alloc_workspace(nbytes: int, device="cuda"):
     import torch
     return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+
+
+# ---- the paged cache -----------------------------------------------------------------------
+# The structs hold addresses only: the caller keeps the tensors.
+def _tensor(name, t, dims, dtype=None, adjoin=True):
+    if t.dim() != dims or (adjoin and t.shape[-1] > 1 and t.stride(-1) != 1) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, {t.dtype}; needs {dims} dimensions"
+                         + (", the last one contiguous" if adjoin else "") + (f", {dtype}" if dtype is not None else ""))
+    return t
+
+
+def _storage_type(kv_dtype):
+    import torch
+    return {TKPHI_BF16: torch.bfloat16, TKPHI_F32: torch.float32}[kv_dtype]
+
+
+def make_paged_config(n_q_heads, n_kv_heads, d_head, dtype, score_scale, K, V, window=0, rot_dim=0, rot_adjacent=False, block=0,
+                      first_blocks=0, last_blocks=0, top_blocks=0, workgroups=0) -> tkphi_paged_config:
+    """K, V: the pool's tensors as [pages][KV heads][tokens per page][channels], in any memory order with adjoining channels and
+    the same strides."""
+    kv = {"bf16": TKPHI_BF16, "f32": TKPHI_F32}[dtype] if isinstance(dtype, str) else int(dtype)
+    for name, t in (("K", K), ("V", V)):
+        _tensor(name, t, 4, _storage_type(kv))
+        if t.shape != K.shape or t.stride() != K.stride() or t.shape[1] != n_kv_heads or t.shape[3] != d_head:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()} do not fit K and the heads")
+    return tkphi_paged_config(int(n_q_heads), int(n_kv_heads), int(d_head), kv, float(score_scale), K.shape[2], K.stride(0), K.stride(1),
+                              K.stride(2), int(window), int(rot_dim), int(bool(rot_adjacent)), int(block), int(first_blocks), int(last_blocks),
+                              int(top_blocks), int(workgroups))
+
+
+def make_step(seqs, pages, rows: int, max_new: int, max_len: int) -> tkphi_step:
+    """seqs: int32 [n][4] (cached, new tokens, first row, 0); pages: int32 [n][max_pages], both contiguous on the device."""
+    import torch
+    for name, t in (("seqs", seqs), ("pages", pages)):
+        _tensor(name, t, 2, torch.int32)
+        if not t.is_contiguous() or t.shape[0] != seqs.shape[0]:
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}; one contiguous row per sequence")
+    if seqs.shape[1] != 4:
+        raise ValueError("seqs: four words per sequence")
+    return tkphi_step(_ptr(seqs), _ptr(pages), seqs.shape[0], pages.shape[1], int(rows), int(max_new), int(max_len), 0)
+
+
+def make_pool(K, V, M=None) -> tkphi_kv_pool:
+    """M: mean keys [pages][KV heads][blocks per page][channels], contiguous, or None."""
+    if M is not None:
+        _tensor("M", M, 4, K.dtype)
+        if not M.is_contiguous() or M.shape[:2] != K.shape[:2] or M.shape[3] != K.shape[3]:
+            raise ValueError(f"M: shape {tuple(M.shape)}, strides {M.stride()} do not fit K")
+    return tkphi_kv_pool(_ptr(K), _ptr(V), _ptr(M), K.shape[0], 0)
+
+
+def make_new_rows(q, k, v, q_rot, inv_freq=None) -> tkphi_new_rows:
+    """[rows][heads][channels]; q and q_rot may both be None.  inv_freq: float64."""
+    import torch
+    st = []
+    for name, t in (("q", q), ("k", k), ("v", v), ("q_rot", q_rot)):
+        if t is None and name in ("q", "q_rot"):
+            st += [0, 0]
+            continue
+        _tensor(name, t, 3, k.dtype)
+        if t.shape[0] != k.shape[0] or t.shape[2] != k.shape[2] or (name == "v" and t.shape != k.shape) or (name == "q_rot" and t.shape != q.shape):
+            raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit k {tuple(k.shape)}")
+        st += [t.stride(0), t.stride(1)]
+    if inv_freq is not None:
+        _tensor("inv_freq", inv_freq, 1, torch.float64)
+    return tkphi_new_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(q_rot), _ptr(inv_freq), *st)
+
+
+def make_attention_rows(q, out, lse=None) -> tkphi_attention_rows:
+    """q, out: [rows][query heads][channels]; lse: contiguous float32 [rows][query heads] or None."""
+    import torch
+    _tensor("q", q, 3)
+    _tensor("out", out, 3, q.dtype)
+    if out.shape != q.shape:
+        raise ValueError(f"out: shape {tuple(out.shape)} does not fit q {tuple(q.shape)}")
+    if lse is not None:
+        _tensor("lse", lse, 2, torch.float32)
+        if not lse.is_contiguous() or lse.shape != q.shape[:2]:
+            raise ValueError(f"lse: shape {tuple(lse.shape)}, strides {lse.stride()} do not fit q")
+    return tkphi_attention_rows(_ptr(q), _ptr(out), _ptr(lse), q.stride(0), q.stride(1), out.stride(0), out.stride(1))
+
+
+def alloc_paged_workspace(nbytes: int, device="cuda"):
+    """A zeroed workspace, which the calls on the paged cache ask for (they leave it fit for the next call)."""
+    import torch
+    return torch.zeros(max(nbytes, 256), dtype=torch.uint8, device=device)
 
 
 def current_stream_ptr() -> int:

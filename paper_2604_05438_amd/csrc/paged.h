@@ -1,0 +1,145 @@
+// Shared by the kernels on the paged key/value cache (paged_append, paged_attention, paged_blocks) and their host layer (paged_api).
+#pragma once
+
+#include "tkphi_internal.h"
+
+namespace tkphi {
+
+constexpr int kPagedThreads = 256;
+constexpr int kPagedRows = 32;            // query rows (token x query head of one KV head) of a split item at most: two tiles of 16
+constexpr int kMaxSplit = 1024;           // workgroups that the work of one attention call is spread over, at most
+constexpr int kBlockRowGroup = 512;       // query tokens whose block scores the workspace holds at once, at most
+constexpr int kMaxKept = 1024;            // blocks a query sees, at most
+
+// Everything a kernel needs to know of one call, passed by value.
+struct PagedGeom {
+  int Hq, Hkv, G, d, dtype;
+  int page;                               // tokens per page
+  uint32_t page_mul, page_shift;          // t / page = (t * page_mul) >> page_shift for 0 <= t < 2^31
+  int64_t st_page, st_head, st_tok;       // bytes
+  int window, rot, adjacent, block, first, last, top;
+  int n_pages, n_seqs, max_pages, rows, max_new, max_len;
+  float scale, scale2, scale2_lo;         // score scale; scale log2(e) as the sum of two floats
+  const int4* seqs;
+  const int32_t* pages;
+  char *K, *V, *M;
+  const char *q, *k, *v;
+  char* out;                              // q_rot or out
+  float* lse;
+  const double* inv_freq;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;   // bytes
+  uint32_t* status;
+  // attention: the work of all items (sequence x tile of query rows x KV head) in units of a fixed number of tokens is
+  // cut into `splits` equal pieces, one per workgroup
+  int splits;
+  int unit;                               // tokens
+  int tile_rows;                          // query rows per item
+  int tiles;                              // most items of one sequence and KV head (1: no plan, every workgroup sums the units itself)
+  uint32_t* arrived;                      // [splits] or [row group][Hkv]: pieces of a split item that are done; zero between calls
+  float* partial;                         // [splits][2][tile_rows][d + 2]
+  int64_t* plan_end;                      // [items]: units up to and with this item
+  int2* plan_item;                        // (sequence, tile)
+  int* plan_count;
+  int plan_room;                          // items the plan has room for
+  // blocks
+  int row0, row_group;                    // query tokens of this launch
+  int max_blocks, kept;                   // bounds
+  uint64_t* keys;                         // [row group][Hkv][max_blocks] order-preserving keys of the block scores; 0: not to be retrieved
+  int2* list;                             // [row group][Hkv][kept] (page, block), ascending
+  int4* list_head;                        // [row group][Hkv] entries, position of the query, its sequence, 0
+};
+
+void launch_paged_append(const PagedGeom& g, hipStream_t s);
+void launch_paged_attention(const PagedGeom& g, hipStream_t s);
+void launch_block_select(const PagedGeom& g, hipStream_t s);
+void launch_block_attention(const PagedGeom& g, hipStream_t s);
+
+#ifdef __HIPCC__
+__device__ __forceinline__ int page_of(const PagedGeom& g, int t) {
+  return (int)(((uint64_t)(uint32_t)t * g.page_mul) >> g.page_shift);
+}
+
+// A sequence as the kernels take it: new_tokens 0 if its description is out of bounds.
+struct PagedSeq {
+  int cached, fresh, row;                 // tokens in the cache, new ones, first row
+};
+__device__ __forceinline__ PagedSeq check_seq(const PagedGeom& g, int4 w) {
+  PagedSeq s{w.x, w.y, w.z};
+  const bool bad = w.x < 0 || w.y < 0 || w.y > g.max_new || (int64_t)w.x + w.y > g.max_len || w.z < 0 || (int64_t)w.z + w.y > g.rows;
+  if (bad) {
+    s.fresh = 0;
+    atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
+  }
+  return s;
+}
+// page id of entry p of sequence i, -1 if absent
+__device__ __forceinline__ int page_id(const PagedGeom& g, int i, int p) {
+  if (p >= g.max_pages) return -1;
+  const int id = g.pages[(int64_t)i * g.max_pages + p];
+  if ((uint32_t)id < (uint32_t)g.n_pages) return id;
+  if (id != -1) atomicOr(g.status, TKPHI_DEV_BAD_PAGE);
+  return -1;
+}
+
+// The sequence that owns unit x when sequence i has count(seq) units and they are numbered in order; wave-uniform, every wavefront by
+// itself.  index: -1 if x is past the end; before: units of the sequences ahead of it; total: of all (only if x is past the end).
+struct FoundSeq {
+  PagedSeq s;
+  int index, before, total;
+};
+template <typename Count>
+__device__ __forceinline__ FoundSeq find_seq(const PagedGeom& g, int x, Count&& count) {
+  const int lane = threadIdx.x & 63;
+  FoundSeq f;
+  f.index = -1;
+  int base = 0;
+  for (int i0 = 0; i0 < g.n_seqs; i0 += 64) {
+    PagedSeq s{0, 0, 0};
+    int c = 0;
+    if (i0 + lane < g.n_seqs) {
+      s = check_seq(g, g.seqs[i0 + lane]);
+      c = s.fresh > 0 ? count(s) : 0;
+    }
+    const int incl = wave_scan_incl(c);
+    const int total = __builtin_amdgcn_readlane(incl, 63);
+    if (x < base + total) {
+      const int at = __builtin_ctzll(__ballot(base + incl > x));
+      f.index = i0 + at;
+      f.s.cached = __builtin_amdgcn_readlane(s.cached, at);
+      f.s.fresh = __builtin_amdgcn_readlane(s.fresh, at);
+      f.s.row = __builtin_amdgcn_readlane(s.row, at);
+      f.before = base + __builtin_amdgcn_readlane(incl - c, at);
+      f.total = 0;
+      return f;
+    }
+    base += total;
+  }
+  f.before = f.total = base;
+  f.s = PagedSeq{0, 0, 0};
+  return f;
+}
+// The sequence whose new tokens row x belongs to (index -1: none), wave-uniform
+__device__ __forceinline__ FoundSeq find_row(const PagedGeom& g, int x) {
+  const int lane = threadIdx.x & 63;
+  FoundSeq f;
+  f.index = -1;
+  f.before = f.total = 0;
+  f.s = PagedSeq{0, 0, 0};
+  for (int i0 = 0; i0 < g.n_seqs; i0 += 64) {
+    PagedSeq s{0, 0, 0};
+    if (i0 + lane < g.n_seqs) s = check_seq(g, g.seqs[i0 + lane]);
+    const uint64_t has = __ballot(s.fresh > 0 && s.row <= x && x - s.row < s.fresh);
+    if (has) {
+      const int at = __builtin_ctzll(has);
+      f.index = i0 + at;
+      f.s.cached = __builtin_amdgcn_readlane(s.cached, at);
+      f.s.fresh = __builtin_amdgcn_readlane(s.fresh, at);
+      f.s.row = __builtin_amdgcn_readlane(s.row, at);
+      break;
+    }
+  }
+  return f;
+}
+#endif
+
+}  // namespace tkphi

@@ -1,0 +1,602 @@
+// Attention of new tokens over the paged cache: tkphi_paged_attention, and the attention part of tkphi_block_attention.
+//
+// One pass over the keys and values with the running maximum and sum of the softmax, on the matrix cores: a wavefront takes tiles
+// of tokens against 16 (or 32) query rows, S^T = K Q^T, then O^T += V^T P^T.  The rows of S^T that a lane holds are exactly the inner
+// indices it has to deliver of P^T, so P never leaves its lane; V passes through LDS, where the bf16 form reads it transposed.
+// The query rows of an item are the new tokens times the query heads of one KV head (every cached row is read once for all of
+// them); the work of all items is cut into equal pieces along the tokens, and the workgroup that finishes an item last joins its pieces.
+#include "paged.h"
+
+namespace tkphi {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pa_bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short pa_s16x4;
+typedef __attribute__((__vector_size__(4 * sizeof(float)))) float pa_floatx4;
+typedef unsigned int pa_u32x2 __attribute__((ext_vector_type(2)));
+union PagedFrag {
+  u32x4 u;
+  pa_bf16x8 v;
+  pa_u32x2 h[2];
+};
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// 4 values of one channel out of 4 rows of LDS: the 16 lanes of a group point at 4 rows x 16 channels of bf16 (lane i at row i / 4, channels
+// 4 (i % 4) ..) and lane i gets channel i of the four rows
+__device__ __forceinline__ pa_u32x2 lds_read_transposed(const char* p) {
+  return __builtin_bit_cast(pa_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pa_s16x4*)p));
+}
+
+// One wavefront's share of an item piece.
+// T, D: storage, head dimension; RT: tiles of 16 query rows
+template <typename T, int D, int RT>
+struct WaveAttend {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int RB = D * (int)sizeof(T);                   // bytes of a row
+  static constexpr int SUB = BF ? 2 : 1;                          // subtiles of 16 tokens that are loaded and contracted together
+  static constexpr int TOK = 16 * SUB;
+  static constexpr int NF = RB / 64;                              // 16-byte pieces of a row per lane
+  static constexpr int VROW = RB + 32;                            // LDS row of V
+  static constexpr int LDS = TOK * VROW;                          // LDS bytes per wavefront
+  static constexpr int CT = D / 16;
+
+  PagedFrag q[RT][NF];
+  pa_floatx4 o[RT][CT];                                           // O^T: channels 16 ct + 4 kg + i of query row (lane & 15)
+  float m[RT], l[RT];                                             // running maximum (of the row) and sum (of this lane's tokens), base 2
+  int lim[RT], low[RT];                                           // tokens [low, lim] are seen by this lane's row
+
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      m[rt] = -INFINITY;
+      l[rt] = 0.f;
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) o[rt][ct] = (pa_floatx4){0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // The cached rows that a lane loads of a tile (slots lane & 15, + 16): byte offset, and the token's position; a position < 0 is seen by
+  // nobody (its offset is readable all the same).
+  struct Rows {
+    int64_t off[SUB];
+    int pos[SUB];
+  };
+
+  __device__ __forceinline__ void load(const char* base, const Rows& r, PagedFrag (&f)[SUB][NF]) {
+    const int kg = (threadIdx.x >> 4) & 3;
+#pragma unroll
+    for (int s = 0; s < SUB; ++s)
+#pragma unroll
+      for (int j = 0; j < NF; ++j) f[s][j].u = gload128(base + r.off[s] + kg * 16 + j * 64);
+  }
+
+  __device__ __forceinline__ pa_floatx4 score(const PagedFrag (&k)[NF], const PagedFrag (&qq)[NF]) {
+    pa_floatx4 p = (pa_floatx4){0.f, 0.f, 0.f, 0.f};
+    if constexpr (BF) {
+#pragma unroll
+      for (int j = 0; j < NF; ++j) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j].v, qq[j].v, p, 0, 0, 0);
+    } else {
+      pa_floatx4 p1 = p;
+#pragma unroll
+      for (int j = 0; j < NF; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+          p = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[j].u[e]), __uint_as_float(qq[j].u[e]), p, 0, 0, 0);
+          p1 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[j].u[e + 1]), __uint_as_float(qq[j].u[e + 1]), p1, 0, 0, 0);
+        }
+      p += p1;
+    }
+    return p;
+  }
+
+  static __device__ __forceinline__ bool not_finite(const u32x4 w) {
+    bool odd = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (BF) odd = odd || (w[e] & 0x7f80u) == 0x7f80u || (w[e] & 0x7f800000u) == 0x7f800000u;
+      else odd = odd || (w[e] & 0x7f800000u) == 0x7f800000u;
+    }
+    return odd;
+  }
+
+  // O^T += V^T P^T of a tile, token by token for the rows that see it
+  __device__ __forceinline__ void add_seen(const PagedFrag (&p)[RT][(SUB + 1) / 2], const Rows& rows, const char* vlds) {
+    const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
+#pragma unroll
+    for (int u = 0; u < SUB; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        for (int k = 0; k < 4; ++k) {
+          const int slot = 4 * k + e, pos = __shfl(rows.pos[u], slot);
+          const char* v = vlds + (u * 16 + slot) * VROW;
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const uint32_t word = __shfl(p[rt][0].u[BF ? 2 * u + e / 2 : e], 16 * k + r);
+            const float weight = __uint_as_float(!BF ? word : e & 1 ? word & 0xffff0000u : word << 16);
+            if (pos < low[rt] || pos > lim[rt]) continue;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[rt][ct][i] = fmaf(weight, Elem<T>::load1(v, ct * 16 + kg * 4 + i), o[rt][ct][i]);
+          }
+        }
+  }
+
+  // rows_of(i): the lane's rows (slots lane & 15, + 16) of its tile i; tiles 0 .. n - 1.  clean(i): every row sees every token of tile i.
+  template <typename RowsOf, typename Clean>
+  __device__ __forceinline__ void run(const PagedGeom& g, int h, char* vlds, int n, RowsOf&& rows_of, Clean&& clean) {
+    if (n <= 0) return;
+    const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
+    const char* Kb = g.K + h * g.st_head;
+    const char* Vb = g.V + h * g.st_head;
+    PagedFrag kf[SUB][NF], vf[SUB][NF];
+    Rows cur = rows_of(0);
+    load(Kb, cur, kf);
+    load(Vb, cur, vf);
+    Rows nxt = rows_of(min(1, n - 1));
+    for (int i = 0; i < n; ++i) {
+      const Rows here = cur;
+      cur = nxt;
+      // ---- scores
+      pa_floatx4 s[SUB][RT];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[u][rt] = score(kf[u], q[rt]);
+      if (i + 1 < n) load(Kb, cur, kf);
+      nxt = rows_of(min(i + 2, n - 1));
+      // ---- what nobody may see
+      bool all = clean(i);
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) all = all && __ballot(here.pos[u] < 0) == 0ull;
+      if (!all) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int pos = __shfl(here.pos[u], 4 * kg + e);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+              if (pos < low[rt] || pos > lim[rt]) s[u][rt][e] = -INFINITY;
+          }
+      }
+      // ---- running maximum and sum
+      PagedFrag p[RT][(SUB + 1) / 2];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        float x[SUB][4], mx = -INFINITY;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[u][rt][e]);
+        mx = across_32(across_16(mx, MaxOp()), MaxOp()) * g.scale2;
+        const float mn = fmaxf(m[rt], mx);
+        const float ref = mn == -INFINITY ? 0.f : mn;              // (nothing seen yet: exp2(-inf - 0) = 0)
+        const float fix = __builtin_amdgcn_exp2f(m[rt] - ref);
+        m[rt] = mn;
+        float sum = 0.f;
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if constexpr (BF) x[u][e] = __builtin_amdgcn_exp2f(fmaf(s[u][rt][e], g.scale2, -ref));
+            else x[u][e] = __builtin_amdgcn_exp2f(s[u][rt][e] == -INFINITY ? -INFINITY : fmaf(s[u][rt][e], g.scale2, fmaf(s[u][rt][e], g.scale2_lo, -ref)));
+            sum += x[u][e];
+          }
+        l[rt] = fmaf(l[rt], fix, sum);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) o[rt][ct] *= fix;
+        if constexpr (BF) {                                        // (the weights enter the product in the cache's own type; their sum does not)
+#pragma unroll
+          for (int u = 0; u < SUB; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              p[rt][0].u[2 * u + e] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)x[u][2 * e], (__bf16)x[u][2 * e + 1]});
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[rt][0].u[e] = __float_as_uint(x[0][e]);
+        }
+      }
+      // ---- V through LDS; rows that nobody sees as zeros, whatever they hold
+      bool odd = false;                                            // a value that is no number, or infinite, which some rows may not see
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int j = 0; j < NF; ++j) {
+          u32x4 w = vf[u][j].u;
+          if (!all) {
+            if (here.pos[u] < 0) w = (u32x4){0u, 0u, 0u, 0u};
+            odd = odd || not_finite(w);
+          }
+          *(u32x4*)(vlds + (u * 16 + r) * VROW + kg * 16 + j * 64) = w;
+        }
+      if (i + 1 < n) load(Vb, cur, vf);
+      if (!all && __ballot(odd)) {                                 // (0 times such a value is not 0: row by row, without what they do not see)
+        add_seen(p, here, vlds);
+        continue;
+      }
+      if constexpr (BF) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          PagedFrag a;
+          const char* at = vlds + (kg * 4 + (r >> 2)) * VROW + ct * 32 + (r & 3) * 8;
+          a.h[0] = lds_read_transposed(at);
+          a.h[1] = lds_read_transposed(at + 16 * VROW);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, p[rt][0].v, o[rt][ct], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            const float a = *(const float*)(vlds + (kg * 4 + e) * VROW + ct * 64 + r * 4);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, __uint_as_float(p[rt][0].u[e]), o[rt][ct], 0, 0, 0);
+          }
+      }
+    }
+  }
+};
+
+constexpr int pmax(int a, int b) { return a > b ? a : b; }
+template <typename T, int D, int RT>
+constexpr int attend_lds() { return pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64); }
+
+// Joins the wavefronts of the workgroup: comb [waves][rows][D + 2] (O, m, l) in LDS.  After it thread t holds the elements
+// t, t + 256, ... of [rows][D]; emit(row, channel, O, m, l).
+template <typename T, int D, int RT, typename Emit>
+__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, int rows, Emit&& emit) {
+  constexpr int W = kPagedThreads / 64, R = 16 * RT, STR = D + 2;
+  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = threadIdx.x >> 6;
+  float* mine = (float*)lds + (size_t)wave * R * STR;
+  __syncthreads();                                                 // (every wavefront is done with its V rows)
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float l = across_32(across_16(w.l[rt], AddOp()), AddOp());
+    float* row = mine + (rt * 16 + r) * STR;
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) row[ct * 16 + kg * 4 + i] = w.o[rt][ct][i];
+    if (kg == 0) { row[D] = w.m[rt]; row[D + 1] = l; }
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < rows * D; x += kPagedThreads) {
+    const int row = x / D, c = x % D;
+    const float* at = (const float*)lds + row * STR;
+    float m = -INFINITY, l = 0.f, o = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) m = fmaxf(m, at[k * R * STR + D]);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      const float f = __builtin_amdgcn_exp2f(at[k * R * STR + D] - ref);
+      l = fmaf(at[k * R * STR + D + 1], f, l);
+      o = fmaf(at[k * R * STR + c], f, o);
+    }
+    emit(row, c, o, m, l);
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float o, float m, float l) {
+  const float y = l == 0.f ? 0.f : o / l;                          // (l = 0: the row sees nothing)
+  char* dst = g.out + (int64_t)token_row * g.out_row + (int64_t)head * g.out_head;
+  if constexpr (sizeof(T) == 2) ((__bf16*)dst)[c] = (__bf16)y;
+  else ((float*)dst)[c] = y;
+  if (c == 0 && g.lse) g.lse[(int64_t)token_row * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Joins `pieces` partials of an item, piece p at slot(p); called by the last workgroup to arrive.
+template <typename T, int D, typename Slot, typename RowOf>
+__device__ __forceinline__ void join_pieces(const PagedGeom& g, int pieces, int rows, Slot&& slot, RowOf&& row_of) {
+  constexpr int STR = D + 2;
+  for (int x = threadIdx.x; x < rows * D; x += kPagedThreads) {
+    const int row = x / D, c = x % D;
+    float m = -INFINITY, l = 0.f, o = 0.f;
+    for (int p = 0; p < pieces; ++p) m = fmaxf(m, load_agent(slot(p) + row * STR + D));
+    const float ref = m == -INFINITY ? 0.f : m;
+    for (int p = 0; p < pieces; ++p) {
+      const float* at = slot(p) + row * STR;
+      const float f = __builtin_amdgcn_exp2f(load_agent(at + D) - ref);
+      l = fmaf(load_agent(at + D + 1), f, l);
+      o = fmaf(load_agent(at + c), f, o);
+    }
+    int token, head;
+    row_of(row, &token, &head);
+    store_out<T>(g, token, head, c, o, m, l);
+  }
+}
+
+// Counts the workgroup in at *arrived (its partial is stored); true in the last of `pieces`, which leaves the count at zero.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* arrived, int pieces, int* sh) {
+  wait_stores();                                                   // (every wavefront for its own GPU-coherent stores)
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last = atomicAdd(arrived, 1u) == (uint32_t)pieces - 1u;
+    if (last) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
+    *sh = last;
+  }
+  __syncthreads();
+  return *sh != 0;
+}
+
+// units of one item (tile j of the query rows of sequence s): the tokens any of its rows can see, from a multiple of the unit on
+struct ItemRange {
+  int begin, low, end, rows;                                       // first token of the units, first and last one seen, query rows
+};
+__device__ __forceinline__ ItemRange item_range(const PagedGeom& g, const PagedSeq& s, int j) {
+  ItemRange it;
+  const int r0 = j * g.tile_rows;
+  it.rows = min(g.tile_rows, s.fresh * g.G - r0);
+  const int i0 = r0 / g.G, i1 = (r0 + it.rows - 1) / g.G;
+  it.end = s.cached + i1 + 1;
+  it.low = g.window > 0 ? max(0, s.cached + i0 + 1 - g.window) : 0;
+  it.begin = it.low / g.unit * g.unit;
+  return it;
+}
+__device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& it) { return (it.end - it.begin + g.unit - 1) / g.unit; }
+
+// Where tiles > 1: the items in order with the running sum of their units, by one workgroup
+// (a sequence whose items would not fit, because sequences share rows, is skipped)
+__global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
+  __shared__ int64_t sums[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t base = 0;
+  int first = 0;
+  for (int i = 0; i < g.n_seqs; ++i) {
+    const PagedSeq s = check_seq(g, g.seqs[i]);
+    const int tiles = s.fresh > 0 ? (int)(((int64_t)s.fresh * g.G + g.tile_rows - 1) / g.tile_rows) : 0;
+    if (first + tiles > g.plan_room) {
+      if (threadIdx.x == 0) atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
+      continue;
+    }
+    for (int j0 = 0; j0 < tiles; j0 += 1024) {
+      const int j = j0 + threadIdx.x;
+      const int u = j < tiles ? item_units(g, item_range(g, s, j)) : 0;
+      int64_t x = u;
+      for (int k = 1; k < 64; k *= 2) {
+        const int64_t y = __shfl_up(x, k);
+        if (lane >= k) x += y;
+      }
+      if (lane == 63) sums[wave] = x;
+      __syncthreads();
+      int64_t ahead = 0, all = 0;
+      for (int k = 0; k < 16; ++k) {
+        if (k < wave) ahead += sums[k];
+        all += sums[k];
+      }
+      __syncthreads();
+      if (j < tiles) {
+        g.plan_end[first + j] = base + ahead + x;
+        g.plan_item[first + j] = make_int2(i, j);
+      }
+      base += all;
+    }
+    first += tiles;
+  }
+  if (threadIdx.x == 0) *g.plan_count = first;
+}
+
+template <typename T, int D, int RT>
+__global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g) {
+  using Wave = WaveAttend<T, D, RT>;
+  constexpr int WAVES = kPagedThreads / 64;
+  __shared__ __align__(16) char lds[attend_lds<T, D, RT>()];
+  __shared__ int sh_last;
+  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+
+  // the units of one KV head, and of all
+  const auto seq_units = [&](const PagedSeq& s) { return item_units(g, item_range(g, s, 0)); };
+  int64_t per_head;
+  int count = 0;
+  if (g.tiles == 1) {
+    per_head = find_seq(g, 0x7fffffff, seq_units).total;
+  } else {
+    count = *g.plan_count;
+    per_head = count > 0 ? g.plan_end[count - 1] : 0;
+  }
+  const int64_t all = per_head * g.Hkv;
+  const int64_t W = min((int64_t)g.splits, all);                   // every workgroup has at least one unit
+  const int w = blockIdx.x;
+  if (w >= W) return;
+  const int64_t begin = all * w / W, end = all * (w + 1) / W;
+
+  Wave at;
+  for (int64_t x = begin; x < end;) {
+    // ---- the item that unit x belongs to
+    const int h = (int)(x / per_head);
+    const int64_t y = x - h * per_head;
+    PagedSeq s;
+    int seq, j;
+    int64_t before;
+    if (g.tiles == 1) {
+      const FoundSeq f = find_seq(g, (int)y, seq_units);
+      s = f.s; seq = f.index; j = 0; before = f.before;
+    } else {
+      int a = 0, b = count - 1;                                    // first item whose end is past y
+      while (a < b) {
+        const int c = (a + b) / 2;
+        if (g.plan_end[c] > y) b = c;
+        else a = c + 1;
+      }
+      const int2 it = g.plan_item[a];
+      seq = it.x; j = it.y;
+      before = a > 0 ? g.plan_end[a - 1] : 0;
+      s = check_seq(g, g.seqs[seq]);
+    }
+    const ItemRange it = item_range(g, s, j);
+    const int units = item_units(g, it), u0 = (int)(y - before);
+    const int64_t item0 = h * per_head + before, item1 = item0 + units;          // units of the item
+    const int u1 = (int)(min(end, item1) - item0);
+    const int t0 = it.begin + u0 * g.unit, t1 = min(it.begin + u1 * g.unit, it.end);
+
+    // ---- this piece: tokens [t0, t1)
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = j * g.tile_rows + rt * 16 + r;
+      const bool live = rt * 16 + r < it.rows;
+      const int i = row / g.G, head = h * g.G + row - i * g.G;
+      at.lim[rt] = live ? s.cached + i : -1;
+      at.low[rt] = live ? (g.window > 0 ? max(0, s.cached + i + 1 - g.window) : 0) : 1;
+      const char* src = g.q + (int64_t)(s.row + i) * g.q_row + (int64_t)head * g.q_head;
+#pragma unroll
+      for (int f = 0; f < Wave::NF; ++f) {
+        at.q[rt][f].u = (u32x4){0u, 0u, 0u, 0u};
+        if (live) at.q[rt][f].u = gload128(src + f * 64 + kg * 16);
+      }
+    }
+    const int seen_all = s.cached + j * g.tile_rows / g.G;         // last token that every row sees
+    const int low_all = g.window > 0 ? it.end - g.window : 0;      // first one (rows of no query may come out as they like)
+    at.reset();
+    const int tiles = (t1 - t0 + Wave::TOK - 1) / Wave::TOK, mine = (tiles - wave + WAVES - 1) / WAVES;
+    const auto tile0 = [&](int i) { return t0 + (wave + i * WAVES) * Wave::TOK; };
+    at.run(g, h, lds + wave * Wave::LDS, mine,
+           [&](int i) {
+             typename Wave::Rows rows;
+#pragma unroll
+             for (int u = 0; u < Wave::SUB; ++u) {
+               const int t = tile0(i) + u * 16 + r, pt = page_of(g, t);
+               const int id = t >= it.low && t < t1 ? page_id(g, seq, pt) : -1;
+               rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.page) * g.st_tok;
+               rows.pos[u] = id >= 0 ? t : -1;
+             }
+             return rows;
+           },
+           [&](int i) { return tile0(i) >= low_all && tile0(i) + Wave::TOK - 1 <= seen_all; });
+
+    // ---- out, or a partial
+    const auto row_of = [&](int row, int* token, int* head) {
+      const int rr = j * g.tile_rows + row;
+      *token = s.row + rr / g.G;
+      *head = h * g.G + rr % g.G;
+    };
+    const bool whole = u0 == 0 && u1 == units;
+    float* slot = g.partial + ((int64_t)w * 2 + (x == begin ? 0 : 1)) * g.tile_rows * (D + 2);
+    join_waves<T, D, RT>(at, lds, it.rows, [&](int row, int c, float o, float m, float l) {
+      if (whole) {
+        int token, head;
+        row_of(row, &token, &head);
+        store_out<T>(g, token, head, c, o, m, l);
+      } else {
+        store_agent(slot + row * (D + 2) + c, o);
+        if (c == 0) {
+          store_agent(slot + row * (D + 2) + D, m);
+          store_agent(slot + row * (D + 2) + D + 1, l);
+        }
+      }
+    });
+    if (!whole) {
+      // workgroups with a part of the item: the last w with all w / W <= unit
+      const auto owner = [&](int64_t unit) { return (int)(((unit + 1) * W + all - 1) / all) - 1; };
+      const int w0 = owner(item0), w1 = owner(item1 - 1);
+      if (last_to_arrive(g.arrived + w0, w1 - w0 + 1, &sh_last)) {
+        const int64_t first_begin = all * w0 / W;
+        join_pieces<T, D>(g, w1 - w0 + 1, it.rows,
+                          [&](int p) {
+                            const int second = p == 0 && first_begin != item0;     // (the first workgroup had another item before this one)
+                            return g.partial + ((int64_t)(w0 + p) * 2 + second) * g.tile_rows * (D + 2);
+                          },
+                          row_of);
+      }
+    }
+    __syncthreads();
+    x = min(end, item1);
+  }
+}
+
+// ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens
+template <typename T, int D>
+__global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g) {
+  using Wave = WaveAttend<T, D, 1>;
+  constexpr int WAVES = kPagedThreads / 64;
+  __shared__ __align__(16) char lds[attend_lds<T, D, 1>()];
+  __shared__ int sh_last;
+  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int h = blockIdx.y, local = blockIdx.z, token = g.row0 + local, split = blockIdx.x;
+  const int64_t at_list = (int64_t)local * g.Hkv + h;
+  const int4 head = g.list_head[at_list];                          // entries, position of the query, its sequence; 0 entries: a row of no sequence
+  if (head.x <= 0) return;
+  const int2* list = g.list + at_list * g.kept;
+  const int n = head.x * g.block;                                  // slots: listed blocks times tokens
+  const int tiles = (n + Wave::TOK - 1) / Wave::TOK;
+  const int a = (int)((int64_t)tiles * split / g.splits), b = (int)((int64_t)tiles * (split + 1) / g.splits);
+
+  Wave at;
+  at.lim[0] = r < g.G ? head.y : -1;
+  at.low[0] = r < g.G ? 0 : 1;
+  const char* src = g.q + (int64_t)token * g.q_row + (int64_t)(h * g.G + min(r, g.G - 1)) * g.q_head;
+#pragma unroll
+  for (int f = 0; f < Wave::NF; ++f) {
+    at.q[0][f].u = (u32x4){0u, 0u, 0u, 0u};
+    if (r < g.G) at.q[0][f].u = gload128(src + f * 64 + kg * 16);
+  }
+  at.reset();
+  const int per = g.page / g.block;
+  const auto tile_slot = [&](int i) { return (a + wave + i * WAVES) * Wave::TOK; };
+  at.run(g, h, lds + wave * Wave::LDS, (b - a - wave + WAVES - 1) / WAVES,
+         [&](int i) {
+           typename Wave::Rows rows;
+#pragma unroll
+           for (int u = 0; u < Wave::SUB; ++u) {
+             const int t = tile_slot(i) + u * 16 + r, e = t / g.block;
+             const int2 blk = e < head.x ? list[e] : make_int2(-1, 0);
+             const int in = t - e * g.block;                       // token of the block
+             rows.off[u] = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)(blk.y % per * g.block + in) * g.st_tok;
+             const int pos = blk.y * g.block + in;
+             rows.pos[u] = blk.x >= 0 && pos <= head.y ? pos : -1;
+           }
+           return rows;
+         },
+         [&](int) { return true; });                               // (all rows are the same token's)
+  const int pieces = min(g.splits, tiles);
+  const bool whole = pieces == 1;
+  float* part = g.partial + at_list * g.splits * 16 * (D + 2);
+  // (with fewer tiles than workgroups some have none: piece p belongs to the p-th workgroup with one)
+  if (a == b) return;
+  const int piece = tiles < g.splits ? a : split;
+  float* slot = part + (int64_t)piece * 16 * (D + 2);
+  join_waves<T, D, 1>(at, lds, g.G, [&](int row, int c, float o, float m, float l) {
+    if (whole) {
+      store_out<T>(g, token, h * g.G + row, c, o, m, l);
+    } else {
+      store_agent(slot + row * (D + 2) + c, o);
+      if (c == 0) {
+        store_agent(slot + row * (D + 2) + D, m);
+        store_agent(slot + row * (D + 2) + D + 1, l);
+      }
+    }
+  });
+  if (!whole && last_to_arrive(g.arrived + at_list, pieces, &sh_last))
+    join_pieces<T, D>(g, pieces, g.G, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
+                      [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
+}
+
+template <typename T, int D>
+static void launch_attend(const PagedGeom& g, hipStream_t s) {
+  if (g.tiles > 1) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, s, g);
+  if (g.tile_rows <= 16) hipLaunchKernelGGL((paged_attend_kernel<T, D, 1>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  else hipLaunchKernelGGL((paged_attend_kernel<T, D, 2>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+}
+void launch_paged_attention(const PagedGeom& g, hipStream_t s) {
+  if (g.dtype == TKPHI_BF16) {
+    if (g.d == 64) launch_attend<uint16_t, 64>(g, s);
+    else launch_attend<uint16_t, 128>(g, s);
+  } else {
+    if (g.d == 64) launch_attend<float, 64>(g, s);
+    else launch_attend<float, 128>(g, s);
+  }
+}
+
+void launch_block_attention(const PagedGeom& g, hipStream_t s) {
+  const dim3 grid(g.splits, g.Hkv, g.row_group);
+  if (g.dtype == TKPHI_BF16) {
+    if (g.d == 64) hipLaunchKernelGGL((block_attend_kernel<uint16_t, 64>), grid, dim3(kPagedThreads), 0, s, g);
+    else hipLaunchKernelGGL((block_attend_kernel<uint16_t, 128>), grid, dim3(kPagedThreads), 0, s, g);
+  } else {
+    if (g.d == 64) hipLaunchKernelGGL((block_attend_kernel<float, 64>), grid, dim3(kPagedThreads), 0, s, g);
+    else hipLaunchKernelGGL((block_attend_kernel<float, 128>), grid, dim3(kPagedThreads), 0, s, g);
+  }
+}
+
+}  // namespace tkphi
