@@ -238,12 +238,13 @@ struct WaveAttend {
   }
 };
 
+constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
+constexpr int kJoinLds = kJoinPairs * 8 + kPagedThreads * 8 + kPagedRows * 8;
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
 template <typename T, int D, int RT>
-constexpr int attend_lds() { return pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64); }
+constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), kJoinLds); }
 
-// Joins the wavefronts of the workgroup: comb [waves][rows][D + 2] (O, m, l) in LDS.  After it thread t holds the elements
-// t, t + 256, ... of [rows][D]; emit(row, channel, O, m, l).
+// Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
 template <typename T, int D, int RT, typename Emit>
 __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, int rows, Emit&& emit) {
   constexpr int W = kPagedThreads / 64, R = 16 * RT, STR = D + 2;
@@ -261,10 +262,11 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, i
     if (kg == 0) { row[D] = w.m[rt]; row[D + 1] = l; }
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < rows * D; x += kPagedThreads) {
-    const int row = x / D, c = x % D;
+  for (int x = threadIdx.x; x < rows * (D / 2); x += kPagedThreads) {
+    const int row = x / (D / 2), c = x % (D / 2) * 2;
     const float* at = (const float*)lds + row * STR;
-    float m = -INFINITY, l = 0.f, o = 0.f;
+    float m = -INFINITY, l = 0.f;
+    float2 o = make_float2(0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < W; ++k) m = fmaxf(m, at[k * R * STR + D]);
     const float ref = m == -INFINITY ? 0.f : m;
@@ -272,7 +274,8 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, i
     for (int k = 0; k < W; ++k) {
       const float f = __builtin_amdgcn_exp2f(at[k * R * STR + D] - ref);
       l = fmaf(at[k * R * STR + D + 1], f, l);
-      o = fmaf(at[k * R * STR + c], f, o);
+      o.x = fmaf(at[k * R * STR + c], f, o.x);
+      o.y = fmaf(at[k * R * STR + c + 1], f, o.y);
     }
     emit(row, c, o, m, l);
   }
@@ -287,24 +290,85 @@ __device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int
   if (c == 0 && g.lse) g.lse[(int64_t)token_row * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Joins `pieces` partials of an item, piece p at slot(p); called by the last workgroup to arrive.
+// A partial in memory: O [rows][D], then (m, l) [rows]; GPU-coherent accesses of 8 bytes
+__device__ __forceinline__ void store_pair(float* p, float a, float b) {
+  store_agent((uint64_t*)p, (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a));
+}
+__device__ __forceinline__ float2 load_pair(const float* p) {
+  const uint64_t v = load_agent((const uint64_t*)p);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
+
+// Joins `pieces` partials of `rows` x D of an item, piece p at slot(p) with (m, l) behind `stride` rows; called by the last workgroup to
+// arrive.  Everything a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
+// took 30 us.
 template <typename T, int D, typename Slot, typename RowOf>
-__device__ __forceinline__ void join_pieces(const PagedGeom& g, int pieces, int rows, Slot&& slot, RowOf&& row_of) {
-  constexpr int STR = D + 2;
-  for (int x = threadIdx.x; x < rows * D; x += kPagedThreads) {
-    const int row = x / D, c = x % D;
-    float m = -INFINITY, l = 0.f, o = 0.f;
-    for (int p = 0; p < pieces; ++p) m = fmaxf(m, load_agent(slot(p) + row * STR + D));
-    const float ref = m == -INFINITY ? 0.f : m;
-    for (int p = 0; p < pieces; ++p) {
-      const float* at = slot(p) + row * STR;
-      const float f = __builtin_amdgcn_exp2f(load_agent(at + D) - ref);
-      l = fmaf(load_agent(at + D + 1), f, l);
-      o = fmaf(load_agent(at + c), f, o);
+__device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
+  constexpr int HALF = D / 2, BATCH = 8;
+  float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
+  float2* part = ml + kJoinPairs;                                  // [threads]
+  float2* sums = part + kPagedThreads;                             // [rows]: m, l of the whole
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int group = min(min(rows, kPagedRows), kJoinPairs / pieces);
+  for (int r0 = 0; r0 < rows; r0 += group) {
+    const int n = min(group, rows - r0);
+    __syncthreads();
+    for (int x = tid; x < n * pieces; x += kPagedThreads) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
+    __syncthreads();
+    for (int r = wave; r < n; r += kPagedThreads / 64) {
+      float2* row = ml + r * pieces;
+      float m = -INFINITY, l = 0.f;
+      for (int p = lane; p < pieces; p += 64) m = fmaxf(m, row[p].x);
+      m = wave_max(m);
+      const float ref = m == -INFINITY ? 0.f : m;
+      for (int p = lane; p < pieces; p += 64) {
+        const float f = __builtin_amdgcn_exp2f(row[p].x - ref);
+        l = fmaf(row[p].y, f, l);
+        row[p].x = f;
+      }
+      l = wave_sum(l);
+      if (lane == 0) sums[r] = make_float2(m, l);
     }
-    int token, head;
-    row_of(row, &token, &head);
-    store_out<T>(g, token, head, c, o, m, l);
+    __syncthreads();
+    // elements (row, pair of channels); where they are few, the pieces are shared by several threads
+    const int items = n * HALF, share = max(1, kPagedThreads / items);
+    for (int x0 = 0; x0 < items; x0 += kPagedThreads) {
+      const int x = share > 1 ? tid % items : x0 + tid, part_of = share > 1 ? tid / items : 0;
+      float2 o = make_float2(0.f, 0.f);
+      if (x < items && part_of < share) {
+        const int r = x / HALF, c = x % HALF;
+        for (int p0 = part_of; p0 < pieces; p0 += share * BATCH) {
+          float2 v[BATCH];
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) v[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + (r0 + r) * D + c * 2);
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) {
+            if (p0 + k * share >= pieces) continue;
+            const float f = ml[r * pieces + p0 + k * share].x;
+            o.x = fmaf(v[k].x, f, o.x);
+            o.y = fmaf(v[k].y, f, o.y);
+          }
+        }
+      }
+      if (share > 1) {
+        part[tid] = o;
+        __syncthreads();
+        if (part_of == 0)
+          for (int k = 1; k < share; ++k) {
+            o.x += part[k * items + x].x;
+            o.y += part[k * items + x].y;
+          }
+      }
+      if (x < items && part_of == 0) {
+        const int r = x / HALF, c = x % HALF;
+        int token, head;
+        row_of(r0 + r, &token, &head);
+        store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
+        store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
+      }
+    }
   }
 }
 
@@ -473,17 +537,15 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
     };
     const bool whole = u0 == 0 && u1 == units;
     float* slot = g.partial + ((int64_t)w * 2 + (x == begin ? 0 : 1)) * g.tile_rows * (D + 2);
-    join_waves<T, D, RT>(at, lds, it.rows, [&](int row, int c, float o, float m, float l) {
+    join_waves<T, D, RT>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
       if (whole) {
         int token, head;
         row_of(row, &token, &head);
-        store_out<T>(g, token, head, c, o, m, l);
+        store_out<T>(g, token, head, c, o.x, m, l);
+        store_out<T>(g, token, head, c + 1, o.y, m, l);
       } else {
-        store_agent(slot + row * (D + 2) + c, o);
-        if (c == 0) {
-          store_agent(slot + row * (D + 2) + D, m);
-          store_agent(slot + row * (D + 2) + D + 1, l);
-        }
+        store_pair(slot + row * D + c, o.x, o.y);
+        if (c == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     });
     if (!whole) {
@@ -492,7 +554,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
       const int w0 = owner(item0), w1 = owner(item1 - 1);
       if (last_to_arrive(g.arrived + w0, w1 - w0 + 1, &sh_last)) {
         const int64_t first_begin = all * w0 / W;
-        join_pieces<T, D>(g, w1 - w0 + 1, it.rows,
+        join_pieces<T, D>(g, w1 - w0 + 1, it.rows, g.tile_rows, lds,
                           [&](int p) {
                             const int second = p == 0 && first_begin != item0;     // (the first workgroup had another item before this one)
                             return g.partial + ((int64_t)(w0 + p) * 2 + second) * g.tile_rows * (D + 2);
@@ -556,19 +618,17 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   if (a == b) return;
   const int piece = tiles < g.splits ? a : split;
   float* slot = part + (int64_t)piece * 16 * (D + 2);
-  join_waves<T, D, 1>(at, lds, g.G, [&](int row, int c, float o, float m, float l) {
+  join_waves<T, D, 1>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
-      store_out<T>(g, token, h * g.G + row, c, o, m, l);
+      store_out<T>(g, token, h * g.G + row, c, o.x, m, l);
+      store_out<T>(g, token, h * g.G + row, c + 1, o.y, m, l);
     } else {
-      store_agent(slot + row * (D + 2) + c, o);
-      if (c == 0) {
-        store_agent(slot + row * (D + 2) + D, m);
-        store_agent(slot + row * (D + 2) + D + 1, l);
-      }
+      store_pair(slot + row * D + c, o.x, o.y);
+      if (c == 0) store_pair(slot + 16 * D + row * 2, m, l);
     }
   });
   if (!whole && last_to_arrive(g.arrived + at_list, pieces, &sh_last))
-    join_pieces<T, D>(g, pieces, g.G, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
+    join_pieces<T, D>(g, pieces, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
                       [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
 }
 
