@@ -7,6 +7,7 @@ namespace tkphi {
 
 constexpr int kPagedThreads = 256;
 constexpr int kPagedRows = 32;            // query rows (token x query head of one KV head) of a split item at most: two tiles of 16
+constexpr int kChunkRows = 128;           // and of an item of the chunk kernel
 constexpr int kMaxSplit = 1024;           // workgroups that the work of one attention call is spread over, at most
 constexpr int kBlockRowGroup = 512;       // query tokens whose block scores the workspace holds at once, at most
 constexpr int kMaxKept = 1024;            // blocks a query sees, at most
@@ -51,6 +52,7 @@ struct PagedGeom {
 
 void launch_paged_append(const PagedGeom& g, hipStream_t s);
 void launch_paged_attention(const PagedGeom& g, hipStream_t s);
+void launch_paged_chunk(const PagedGeom& g, hipStream_t s);
 void launch_block_select(const PagedGeom& g, hipStream_t s);
 void launch_block_attention(const PagedGeom& g, hipStream_t s);
 

@@ -1,0 +1,214 @@
+// What the attention kernels on the paged cache share: items and their cut into pieces, outputs, partials and their joining.
+#pragma once
+
+#include "paged.h"
+
+namespace tkphi {
+
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
+constexpr int kJoinLds = kJoinPairs * 8 + kPagedThreads * 8 + kPagedRows * 8;
+
+template <typename T>
+__device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float o, float m, float l) {
+  const float y = l == 0.f ? 0.f : o / l;                          // (l = 0: the row sees nothing)
+  char* dst = g.out + (int64_t)token_row * g.out_row + (int64_t)head * g.out_head;
+  if constexpr (sizeof(T) == 2) ((__bf16*)dst)[c] = (__bf16)y;
+  else ((float*)dst)[c] = y;
+  if (c == 0 && g.lse) g.lse[(int64_t)token_row * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// A partial in memory: O [rows][D], then (m, l) [rows]; GPU-coherent accesses of 8 bytes
+__device__ __forceinline__ void store_pair(float* p, float a, float b) {
+  store_agent((uint64_t*)p, (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a));
+}
+__device__ __forceinline__ float2 load_pair(const float* p) {
+  const uint64_t v = load_agent((const uint64_t*)p);
+  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
+}
+
+static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
+
+// Joins `pieces` partials of `rows` x D of an item, piece p at slot(p) with (m, l) behind `stride` rows; called by the last workgroup to
+// arrive.  Everything a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
+// took 30 us.
+template <typename T, int D, typename Slot, typename RowOf>
+__device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
+  constexpr int HALF = D / 2, BATCH = 8;
+  float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
+  float2* part = ml + kJoinPairs;                                  // [threads]
+  float2* sums = part + kPagedThreads;                             // [rows]: m, l of the whole
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int group = min(min(rows, kPagedRows), kJoinPairs / pieces);
+  for (int r0 = 0; r0 < rows; r0 += group) {
+    const int n = min(group, rows - r0);
+    __syncthreads();
+    for (int x = tid; x < n * pieces; x += kPagedThreads) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
+    __syncthreads();
+    for (int r = wave; r < n; r += kPagedThreads / 64) {
+      float2* row = ml + r * pieces;
+      float m = -INFINITY, l = 0.f;
+      for (int p = lane; p < pieces; p += 64) m = fmaxf(m, row[p].x);
+      m = wave_max(m);
+      const float ref = m == -INFINITY ? 0.f : m;
+      for (int p = lane; p < pieces; p += 64) {
+        const float f = __builtin_amdgcn_exp2f(row[p].x - ref);
+        l = fmaf(row[p].y, f, l);
+        row[p].x = f;
+      }
+      l = wave_sum(l);
+      if (lane == 0) sums[r] = make_float2(m, l);
+    }
+    __syncthreads();
+    // elements (row, pair of channels); where they are few, the pieces are shared by several threads
+    const int items = n * HALF, share = max(1, kPagedThreads / items);
+    for (int x0 = 0; x0 < items; x0 += kPagedThreads) {
+      const int x = share > 1 ? tid % items : x0 + tid, part_of = share > 1 ? tid / items : 0;
+      float2 o = make_float2(0.f, 0.f);
+      if (x < items && part_of < share) {
+        const int r = x / HALF, c = x % HALF;
+        for (int p0 = part_of; p0 < pieces; p0 += share * BATCH) {
+          float2 v[BATCH];
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) v[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + (r0 + r) * D + c * 2);
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) {
+            if (p0 + k * share >= pieces) continue;
+            const float f = ml[r * pieces + p0 + k * share].x;
+            o.x = fmaf(v[k].x, f, o.x);
+            o.y = fmaf(v[k].y, f, o.y);
+          }
+        }
+      }
+      if (share > 1) {
+        part[tid] = o;
+        __syncthreads();
+        if (part_of == 0)
+          for (int k = 1; k < share; ++k) {
+            o.x += part[k * items + x].x;
+            o.y += part[k * items + x].y;
+          }
+      }
+      if (x < items && part_of == 0) {
+        const int r = x / HALF, c = x % HALF;
+        int token, head;
+        row_of(r0 + r, &token, &head);
+        store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
+        store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
+      }
+    }
+  }
+}
+
+// Counts the workgroup in at *arrived (its partial is stored); true in the last of `pieces`, which leaves the count at zero.
+__device__ __forceinline__ bool last_to_arrive(uint32_t* arrived, int pieces, int* sh) {
+  wait_stores();                                                   // (every wavefront for its own GPU-coherent stores)
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const bool last = atomicAdd(arrived, 1u) == (uint32_t)pieces - 1u;
+    if (last) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
+    *sh = last;
+  }
+  __syncthreads();
+  return *sh != 0;
+}
+
+// units of one item (tile j of the query rows of sequence s): the tokens any of its rows can see, from a multiple of the unit on
+struct ItemRange {
+  int begin, low, end, rows;                                       // first token of the units, first and last one seen, query rows
+};
+__device__ __forceinline__ ItemRange item_range(const PagedGeom& g, const PagedSeq& s, int j) {
+  ItemRange it;
+  const int r0 = j * g.tile_rows;
+  it.rows = min(g.tile_rows, s.fresh * g.G - r0);
+  const int i0 = r0 / g.G, i1 = (r0 + it.rows - 1) / g.G;
+  it.end = s.cached + i1 + 1;
+  it.low = g.window > 0 ? max(0, s.cached + i0 + 1 - g.window) : 0;
+  it.begin = it.low / g.unit * g.unit;
+  return it;
+}
+__device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& it) { return (it.end - it.begin + g.unit - 1) / g.unit; }
+
+// The work of a call in order: KV heads outermost, then items, then units of an item.  Workgroup w of W takes the units
+// [all w / W, all (w + 1) / W).
+struct Share {
+  int64_t per_head, all, W, begin, end;    // units of a KV head, of all; workgroups; this one's
+  int count;                               // planned items
+};
+// least: units that a workgroup gets at least where there are more workgroups than that
+__device__ __forceinline__ Share share_of(const PagedGeom& g, int w, int least) {
+  Share r;
+  r.count = 0;
+  if (g.tiles == 1) {
+    r.per_head = find_seq(g, 0x7fffffff, [&](const PagedSeq& s) { return item_units(g, item_range(g, s, 0)); }).total;
+  } else {
+    r.count = *g.plan_count;
+    r.per_head = r.count > 0 ? g.plan_end[r.count - 1] : 0;
+  }
+  r.all = r.per_head * g.Hkv;
+  r.W = min((int64_t)g.splits, (r.all + least - 1) / least);
+  r.begin = w < r.W ? r.all * w / r.W : 0;
+  r.end = w < r.W ? r.all * (w + 1) / r.W : 0;
+  return r;
+}
+
+// The part of an item that unit x and those after it, up to the end of the share, belong to
+struct Piece {
+  PagedSeq s;
+  ItemRange it;
+  int seq, tile, h;
+  int u0, u1, units;                       // this piece's units of the item's
+  int64_t item0, item1;                    // the item's units among all
+  __device__ __forceinline__ bool whole() const { return u0 == 0 && u1 == units; }
+  __device__ __forceinline__ void place(const PagedGeom& g, int row, int* token, int* head) const {
+    const int r = tile * g.tile_rows + row, i = r / g.G;
+    *token = s.row + i;
+    *head = h * g.G + r - i * g.G;
+  }
+};
+__device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, int64_t x) {
+  Piece p;
+  p.h = (int)(x / sh.per_head);
+  const int64_t y = x - p.h * sh.per_head;
+  int64_t before;
+  if (g.tiles == 1) {
+    const FoundSeq f = find_seq(g, (int)y, [&](const PagedSeq& s) { return item_units(g, item_range(g, s, 0)); });
+    p.s = f.s; p.seq = f.index; p.tile = 0;
+    before = f.before;
+  } else {
+    int a = 0, b = sh.count - 1;           // first item whose end is past y
+    while (a < b) {
+      const int c = (a + b) / 2;
+      if (g.plan_end[c] > y) b = c;
+      else a = c + 1;
+    }
+    const int2 it = g.plan_item[a];
+    p.seq = it.x; p.tile = it.y;
+    before = a > 0 ? g.plan_end[a - 1] : 0;
+    p.s = check_seq(g, g.seqs[p.seq]);
+  }
+  p.it = item_range(g, p.s, p.tile);
+  p.units = item_units(g, p.it);
+  p.u0 = (int)(y - before);
+  p.item0 = p.h * sh.per_head + before;
+  p.item1 = p.item0 + p.units;
+  p.u1 = (int)(min(sh.end, p.item1) - p.item0);
+  return p;
+}
+// where workgroup w keeps its partial of the piece that starts at unit x: of its first piece, or of its last
+__device__ __forceinline__ float* partial_slot(const PagedGeom& g, int w, bool first) {
+  return g.partial + ((int64_t)w * 2 + (first ? 0 : 1)) * g.tile_rows * (g.d + 2);
+}
+// After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.
+template <typename T, int D>
+__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share& sh, const Piece& p, char* lds, int* sh_last) {
+  // the workgroup of a unit is the last w with all w / W <= unit
+  const auto owner = [&](int64_t unit) { return (int)(((unit + 1) * sh.W + sh.all - 1) / sh.all) - 1; };
+  const int w0 = owner(p.item0), w1 = owner(p.item1 - 1);
+  if (!last_to_arrive(g.arrived + w0, w1 - w0 + 1, sh_last)) return;
+  const bool first = sh.all * w0 / sh.W == p.item0;       // the first workgroup's share starts with this item
+  join_pieces<T, D>(g, w1 - w0 + 1, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
+                    [&](int row, int* token, int* head) { p.place(g, row, token, head); });
+}
+
+}  // namespace tkphi

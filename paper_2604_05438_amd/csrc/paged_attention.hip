@@ -5,7 +5,7 @@
 // indices it has to deliver of P^T, so P never leaves its lane; V passes through LDS, where the bf16 form reads it transposed.
 // The query rows of an item are the new tokens times the query heads of one KV head (every cached row is read once for all of
 // them); the work of all items is cut into equal pieces along the tokens, and the workgroup that finishes an item last joins its pieces.
-#include "paged.h"
+#include "paged_attention.h"
 
 namespace tkphi {
 
@@ -18,7 +18,6 @@ union PagedFrag {
   pa_bf16x8 v;
   pa_u32x2 h[2];
 };
-constexpr float kLn2 = 0.69314718055994530942f;
 
 // 4 values of one channel out of 4 rows of LDS: the 16 lanes of a group point at 4 rows x 16 channels of bf16 (lane i at row i / 4, channels
 // 4 (i % 4) ..) and lane i gets channel i of the four rows
@@ -238,8 +237,6 @@ struct WaveAttend {
   }
 };
 
-constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
-constexpr int kJoinLds = kJoinPairs * 8 + kPagedThreads * 8 + kPagedRows * 8;
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
 template <typename T, int D, int RT>
 constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), kJoinLds); }
@@ -280,126 +277,6 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, i
     emit(row, c, o, m, l);
   }
 }
-
-template <typename T>
-__device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float o, float m, float l) {
-  const float y = l == 0.f ? 0.f : o / l;                          // (l = 0: the row sees nothing)
-  char* dst = g.out + (int64_t)token_row * g.out_row + (int64_t)head * g.out_head;
-  if constexpr (sizeof(T) == 2) ((__bf16*)dst)[c] = (__bf16)y;
-  else ((float*)dst)[c] = y;
-  if (c == 0 && g.lse) g.lse[(int64_t)token_row * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
-}
-
-// A partial in memory: O [rows][D], then (m, l) [rows]; GPU-coherent accesses of 8 bytes
-__device__ __forceinline__ void store_pair(float* p, float a, float b) {
-  store_agent((uint64_t*)p, (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a));
-}
-__device__ __forceinline__ float2 load_pair(const float* p) {
-  const uint64_t v = load_agent((const uint64_t*)p);
-  return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
-}
-
-static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
-
-// Joins `pieces` partials of `rows` x D of an item, piece p at slot(p) with (m, l) behind `stride` rows; called by the last workgroup to
-// arrive.  Everything a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
-// took 30 us.
-template <typename T, int D, typename Slot, typename RowOf>
-__device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
-  constexpr int HALF = D / 2, BATCH = 8;
-  float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
-  float2* part = ml + kJoinPairs;                                  // [threads]
-  float2* sums = part + kPagedThreads;                             // [rows]: m, l of the whole
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int group = min(min(rows, kPagedRows), kJoinPairs / pieces);
-  for (int r0 = 0; r0 < rows; r0 += group) {
-    const int n = min(group, rows - r0);
-    __syncthreads();
-    for (int x = tid; x < n * pieces; x += kPagedThreads) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
-    __syncthreads();
-    for (int r = wave; r < n; r += kPagedThreads / 64) {
-      float2* row = ml + r * pieces;
-      float m = -INFINITY, l = 0.f;
-      for (int p = lane; p < pieces; p += 64) m = fmaxf(m, row[p].x);
-      m = wave_max(m);
-      const float ref = m == -INFINITY ? 0.f : m;
-      for (int p = lane; p < pieces; p += 64) {
-        const float f = __builtin_amdgcn_exp2f(row[p].x - ref);
-        l = fmaf(row[p].y, f, l);
-        row[p].x = f;
-      }
-      l = wave_sum(l);
-      if (lane == 0) sums[r] = make_float2(m, l);
-    }
-    __syncthreads();
-    // elements (row, pair of channels); where they are few, the pieces are shared by several threads
-    const int items = n * HALF, share = max(1, kPagedThreads / items);
-    for (int x0 = 0; x0 < items; x0 += kPagedThreads) {
-      const int x = share > 1 ? tid % items : x0 + tid, part_of = share > 1 ? tid / items : 0;
-      float2 o = make_float2(0.f, 0.f);
-      if (x < items && part_of < share) {
-        const int r = x / HALF, c = x % HALF;
-        for (int p0 = part_of; p0 < pieces; p0 += share * BATCH) {
-          float2 v[BATCH];
-#pragma unroll
-          for (int k = 0; k < BATCH; ++k) v[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + (r0 + r) * D + c * 2);
-#pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
-            if (p0 + k * share >= pieces) continue;
-            const float f = ml[r * pieces + p0 + k * share].x;
-            o.x = fmaf(v[k].x, f, o.x);
-            o.y = fmaf(v[k].y, f, o.y);
-          }
-        }
-      }
-      if (share > 1) {
-        part[tid] = o;
-        __syncthreads();
-        if (part_of == 0)
-          for (int k = 1; k < share; ++k) {
-            o.x += part[k * items + x].x;
-            o.y += part[k * items + x].y;
-          }
-      }
-      if (x < items && part_of == 0) {
-        const int r = x / HALF, c = x % HALF;
-        int token, head;
-        row_of(r0 + r, &token, &head);
-        store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
-        store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
-      }
-    }
-  }
-}
-
-// Counts the workgroup in at *arrived (its partial is stored); true in the last of `pieces`, which leaves the count at zero.
-__device__ __forceinline__ bool last_to_arrive(uint32_t* arrived, int pieces, int* sh) {
-  wait_stores();                                                   // (every wavefront for its own GPU-coherent stores)
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    const bool last = atomicAdd(arrived, 1u) == (uint32_t)pieces - 1u;
-    if (last) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
-    *sh = last;
-  }
-  __syncthreads();
-  return *sh != 0;
-}
-
-// units of one item (tile j of the query rows of sequence s): the tokens any of its rows can see, from a multiple of the unit on
-struct ItemRange {
-  int begin, low, end, rows;                                       // first token of the units, first and last one seen, query rows
-};
-__device__ __forceinline__ ItemRange item_range(const PagedGeom& g, const PagedSeq& s, int j) {
-  ItemRange it;
-  const int r0 = j * g.tile_rows;
-  it.rows = min(g.tile_rows, s.fresh * g.G - r0);
-  const int i0 = r0 / g.G, i1 = (r0 + it.rows - 1) / g.G;
-  it.end = s.cached + i1 + 1;
-  it.low = g.window > 0 ? max(0, s.cached + i0 + 1 - g.window) : 0;
-  it.begin = it.low / g.unit * g.unit;
-  return it;
-}
-__device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& it) { return (it.end - it.begin + g.unit - 1) / g.unit; }
 
 // Where tiles > 1: the items in order with the running sum of their units, by one workgroup
 // (a sequence whose items would not fit, because sequences share rows, is skipped)
@@ -450,50 +327,15 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
-  // the units of one KV head, and of all
-  const auto seq_units = [&](const PagedSeq& s) { return item_units(g, item_range(g, s, 0)); };
-  int64_t per_head;
-  int count = 0;
-  if (g.tiles == 1) {
-    per_head = find_seq(g, 0x7fffffff, seq_units).total;
-  } else {
-    count = *g.plan_count;
-    per_head = count > 0 ? g.plan_end[count - 1] : 0;
-  }
-  const int64_t all = per_head * g.Hkv;
-  const int64_t W = min((int64_t)g.splits, all);                   // every workgroup has at least one unit
   const int w = blockIdx.x;
-  if (w >= W) return;
-  const int64_t begin = all * w / W, end = all * (w + 1) / W;
-
+  const Share sh = share_of(g, w, 1);
   Wave at;
-  for (int64_t x = begin; x < end;) {
-    // ---- the item that unit x belongs to
-    const int h = (int)(x / per_head);
-    const int64_t y = x - h * per_head;
-    PagedSeq s;
-    int seq, j;
-    int64_t before;
-    if (g.tiles == 1) {
-      const FoundSeq f = find_seq(g, (int)y, seq_units);
-      s = f.s; seq = f.index; j = 0; before = f.before;
-    } else {
-      int a = 0, b = count - 1;                                    // first item whose end is past y
-      while (a < b) {
-        const int c = (a + b) / 2;
-        if (g.plan_end[c] > y) b = c;
-        else a = c + 1;
-      }
-      const int2 it = g.plan_item[a];
-      seq = it.x; j = it.y;
-      before = a > 0 ? g.plan_end[a - 1] : 0;
-      s = check_seq(g, g.seqs[seq]);
-    }
-    const ItemRange it = item_range(g, s, j);
-    const int units = item_units(g, it), u0 = (int)(y - before);
-    const int64_t item0 = h * per_head + before, item1 = item0 + units;          // units of the item
-    const int u1 = (int)(min(end, item1) - item0);
-    const int t0 = it.begin + u0 * g.unit, t1 = min(it.begin + u1 * g.unit, it.end);
+  for (int64_t x = sh.begin; x < sh.end;) {
+    const Piece p = piece_at(g, sh, x);
+    const PagedSeq s = p.s;
+    const ItemRange it = p.it;
+    const int h = p.h, j = p.tile, seq = p.seq;
+    const int t0 = it.begin + p.u0 * g.unit, t1 = min(it.begin + p.u1 * g.unit, it.end);
 
     // ---- this piece: tokens [t0, t1)
 #pragma unroll
@@ -530,17 +372,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
            [&](int i) { return tile0(i) >= low_all && tile0(i) + Wave::TOK - 1 <= seen_all; });
 
     // ---- out, or a partial
-    const auto row_of = [&](int row, int* token, int* head) {
-      const int rr = j * g.tile_rows + row;
-      *token = s.row + rr / g.G;
-      *head = h * g.G + rr % g.G;
-    };
-    const bool whole = u0 == 0 && u1 == units;
-    float* slot = g.partial + ((int64_t)w * 2 + (x == begin ? 0 : 1)) * g.tile_rows * (D + 2);
+    const bool whole = p.whole();
+    float* slot = partial_slot(g, w, x == sh.begin);
     join_waves<T, D, RT>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
       if (whole) {
         int token, head;
-        row_of(row, &token, &head);
+        p.place(g, row, &token, &head);
         store_out<T>(g, token, head, c, o.x, m, l);
         store_out<T>(g, token, head, c + 1, o.y, m, l);
       } else {
@@ -548,22 +385,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
         if (c == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     });
-    if (!whole) {
-      // workgroups with a part of the item: the last w with all w / W <= unit
-      const auto owner = [&](int64_t unit) { return (int)(((unit + 1) * W + all - 1) / all) - 1; };
-      const int w0 = owner(item0), w1 = owner(item1 - 1);
-      if (last_to_arrive(g.arrived + w0, w1 - w0 + 1, &sh_last)) {
-        const int64_t first_begin = all * w0 / W;
-        join_pieces<T, D>(g, w1 - w0 + 1, it.rows, g.tile_rows, lds,
-                          [&](int p) {
-                            const int second = p == 0 && first_begin != item0;     // (the first workgroup had another item before this one)
-                            return g.partial + ((int64_t)(w0 + p) * 2 + second) * g.tile_rows * (D + 2);
-                          },
-                          row_of);
-      }
-    }
+    if (!whole) finish_item<T, D>(g, sh, p, lds, &sh_last);
     __syncthreads();
-    x = min(end, item1);
+    x = min(sh.end, p.item1);
   }
 }
 
@@ -635,7 +459,8 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
 template <typename T, int D>
 static void launch_attend(const PagedGeom& g, hipStream_t s) {
   if (g.tiles > 1) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, s, g);
-  if (g.tile_rows <= 16) hipLaunchKernelGGL((paged_attend_kernel<T, D, 1>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  if (g.tile_rows == kChunkRows) launch_paged_chunk(g, s);
+  else if (g.tile_rows <= 16) hipLaunchKernelGGL((paged_attend_kernel<T, D, 1>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
   else hipLaunchKernelGGL((paged_attend_kernel<T, D, 2>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
 }
 void launch_paged_attention(const PagedGeom& g, hipStream_t s) {

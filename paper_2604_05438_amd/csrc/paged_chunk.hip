@@ -1,0 +1,305 @@
+// tkphi_paged_attention for many query rows per KV head (chunks, prompts), bf16.
+//
+// One pass over the keys and values with the running maximum and sum of the softmax.  A workgroup holds 128 query rows (new tokens
+// times the query heads of one KV head, a wavefront 32 of them in registers) and passes over tiles of 64 cached tokens, which go from memory straight to
+// LDS, one tile ahead; S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds all of S^T for one query row but the half
+// its partner lane 32 further has, and exactly what it has to deliver of P^T: maximum and sum take one exchange, P none.
+// Two workgroups per CU: while the wavefronts of one exponentiate, those of the other multiply.
+#include "paged_attention.h"
+
+namespace tkphi {
+
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 pc_bf16x8;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short pc_s16x4;
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float pc_floatx16;
+typedef unsigned int pc_u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) char* lds_ptr;
+union ChunkFrag {
+  u32x4 u;
+  pc_bf16x8 v;
+  pc_u32x2 h[2];
+};
+
+constexpr int kChunkTokens = 64;
+constexpr int kChunkWaves = kPagedThreads / 64;
+constexpr float kSlack = 8.f;             // the reference of the exponentials is raised when a score passes it by 2^8 (sums stay far from overflow)
+
+// LDS of one tile: rows of D bf16 in 16-byte pieces, piece c of row r at place c ^ key_swap(r) or c ^ value_swap(r).  Keys are read as 16 bytes of 32
+// rows, values as 64 bytes of 8 rows: either way the rows spread over the banks.
+template <int D> __device__ __forceinline__ int key_swap(int r) { return r & (D / 8 - 1); }
+template <int D> __device__ __forceinline__ int value_swap(int r) {
+  return D == 128 ? (r & 3) << 2 | ((r >> 2) & 3) : ((r >> 1) & 1) << 2 | ((r >> 2) & 3);
+}
+
+template <int D>
+struct ChunkTile {
+  static constexpr int RB = D * 2, PIECES = RB / 16, BYTES = kChunkTokens * RB;
+  static constexpr int ROWS = 1024 / RB;                           // rows that one load of a wavefront covers
+  static constexpr int LOADS = kChunkTokens / kChunkWaves / ROWS;  // loads per wavefront of K, and of V
+};
+
+template <int D, bool UNIFORM>
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom g) {
+  using Tile = ChunkTile<D>;
+  constexpr int RB = Tile::RB, NF = D / 16, CT = D / 32;
+  // two tiles of K and V each; later the join's scratch
+  __shared__ __align__(1024) char lds[4 * Tile::BYTES];
+  __shared__ int sh_last, sh_odd[2];
+  __shared__ uint32_t sh_present[2][kChunkWaves];                  // which tokens of the tile anyone may see, 16 per wavefront
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int col = lane & 31, hi = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
+  const uint32_t lds0 = (uint32_t)(size_t)(lds_ptr)lds;
+  if (tid < 2) sh_odd[tid] = 0;
+
+  // where this lane reads: keys of row col, channels 16 f + 8 hi ..; values of 4 rows (see lds_read_transposed's use below)
+  int ka[NF], va[CT][2];
+#pragma unroll
+  for (int f = 0; f < NF; ++f) ka[f] = col * RB + ((2 * f + hi) ^ key_swap<D>(col)) * 16;
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int r = 8 * x + 4 * hi + (i16 >> 2), c = 4 * ct + 2 * grp + ((i16 & 3) >> 1);
+      va[ct][x] = r * RB + (c ^ value_swap<D>(r)) * 16 + (i16 & 1) * 8;
+    }
+  // and what it loads: pieces of rows 16 wave + ROWS k + lane / PIECES of the tile
+  const int lrow = lane / Tile::PIECES, lplace = lane % Tile::PIECES;
+
+  // keep consecutive shares, which pass over the same KV head, on one XCD (workgroup b runs on XCD b % 8)
+  const int nb = gridDim.x, b = blockIdx.x;
+  const int w = nb % 8 == 0 ? (b % 8) * (nb / 8) + b / 8 : b;
+  const Share sh = share_of(g, w, 4);
+  for (int64_t x = sh.begin; x < sh.end;) {
+    const Piece p = piece_at(g, sh, x);
+    const PagedSeq s = p.s;
+    const ItemRange it = p.it;
+    const int t0 = it.begin + p.u0 * kChunkTokens, t1 = min(it.begin + p.u1 * kChunkTokens, it.end);
+    const int n = (t1 - t0 + kChunkTokens - 1) / kChunkTokens;
+
+    // ---- query rows
+    ChunkFrag q[NF];
+    const int row = wave * 32 + col;
+    const bool live = row < it.rows;
+    int token, head;
+    p.place(g, min(row, it.rows - 1), &token, &head);
+    const int lim = s.cached + token - s.row, low = g.window > 0 ? max(0, lim + 1 - g.window) : 0;      // tokens [low, lim] are seen
+    const char* qsrc = g.q + (int64_t)token * g.q_row + (int64_t)head * g.q_head;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) q[f].u = gload128(qsrc + f * 32 + hi * 16);
+    const int lim_lo = __builtin_amdgcn_readlane(lim, 0), lim_hi = __builtin_amdgcn_readlane(lim, 31);   // rows ascend by token
+    const int low_lo = __builtin_amdgcn_readlane(low, 0), low_hi = __builtin_amdgcn_readlane(low, 31);
+    const bool idle = wave * 32 >= it.rows;
+
+    pc_floatx16 o[CT];
+    float m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[ct][e] = 0.f;
+
+    const auto own_page = [&](int i) {       // the page of this wavefront's 16 tokens of tile i, or of the lane's token lane & 15 of them
+      const int t = t0 + i * kChunkTokens + wave * 16 + (UNIFORM ? 0 : i16);
+      return t < t1 && t + (UNIFORM ? 15 : 0) >= it.low ? page_id(g, p.seq, page_of(g, t)) : -1;
+    };
+    const auto request = [&](int i, int id) {
+      const int buf = i & 1, tw = t0 + i * kChunkTokens + wave * 16;
+      const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * 16 * RB, vdst = kdst + Tile::BYTES;
+      uint32_t present;
+      if constexpr (UNIFORM) {
+        const int uid = __builtin_amdgcn_readfirstlane(id);
+        const int64_t at = (int64_t)max(uid, 0) * g.st_page + p.h * g.st_head + (int64_t)(tw - page_of(g, tw) * g.page) * g.st_tok;
+        const int a = max(it.low - tw, 0), z = min(t1 - tw, 16);         // tokens [a, z) of the 16
+        present = uid < 0 || a >= z ? 0u : ((1u << z) - 1u) & ~((1u << a) - 1u);
+#pragma unroll
+        for (int k = 0; k < Tile::LOADS; ++k) {
+          const int r = k * Tile::ROWS + lrow;
+          load_to_lds16(g.K + at, (uint32_t)(r * (int)g.st_tok + (lplace ^ key_swap<D>(r)) * 16), kdst + k * 1024);
+        }
+#pragma unroll
+        for (int k = 0; k < Tile::LOADS; ++k) {
+          const int r = k * Tile::ROWS + lrow;
+          load_to_lds16(g.V + at, (uint32_t)(r * (int)g.st_tok + (lplace ^ value_swap<D>(r)) * 16), vdst + k * 1024);
+        }
+      } else {
+        const int t = tw + i16;
+        present = (uint32_t)__ballot(id >= 0 && t >= it.low && t < t1) & 0xffffu;
+        const int64_t at = (int64_t)max(id, 0) * g.st_page + p.h * g.st_head + (int64_t)(t - page_of(g, t) * g.page) * g.st_tok;
+#pragma unroll
+        for (int k = 0; k < Tile::LOADS; ++k) {
+          const int r = k * Tile::ROWS + lrow;
+          const int64_t from = (int64_t)(uint32_t)__shfl((int)(uint32_t)at, r) | (int64_t)__shfl((int)(at >> 32), r) << 32;
+          load_to_lds16(g.K + from + (lplace ^ key_swap<D>(r)) * 16, kdst + k * 1024);
+          load_to_lds16(g.V + from + (lplace ^ value_swap<D>(r)) * 16, vdst + k * 1024);
+        }
+      }
+      if (lane == 0) sh_present[buf][wave] = present;
+    };
+
+    __syncthreads();                                               // (the join of the item before is done with LDS)
+    request(0, own_page(0));
+    int next_id = own_page(1);
+    for (int i = 0; i < n; ++i) {
+      wait_vm_loads<0>();
+      lds_barrier();                                               // tile i is there, tile i - 1 is done with
+      const int buf = i & 1, tb = t0 + i * kChunkTokens;
+      if (tid == 0) sh_odd[1 - buf] = 0;
+      if (i + 1 < n) request(i + 1, next_id);
+      next_id = own_page(i + 2);
+      uint64_t present = 0;
+#pragma unroll
+      for (int k = 0; k < kChunkWaves; ++k) present |= (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)sh_present[buf][k]) << (16 * k);
+      char* const kt = lds + buf * 2 * Tile::BYTES;
+      char* const vt = kt + Tile::BYTES;
+
+      // ---- a tile that some row of the workgroup does not see all of: values that nobody sees are zeros, whatever they hold, and one that is no
+      // number, or infinite, must not meet the zero weights of the rows that do not see it
+      const int seen_first = s.cached + p.tile * g.tile_rows / g.G;                // limit of the workgroup's first row
+      bool odd = false;
+      if (present != ~0ull || tb + kChunkTokens - 1 > seen_first || (g.window > 0 && tb < it.end - g.window)) {
+        bool mine = false;
+        for (int k = tid; k < kChunkTokens * Tile::PIECES; k += kPagedThreads) {
+          const int r = k / Tile::PIECES;
+          u32x4* at = (u32x4*)(vt + k * 16);
+          if (!((present >> r) & 1)) {
+            *at = (u32x4){0u, 0u, 0u, 0u};
+          } else {
+            const u32x4 v = *at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mine = mine || (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+          }
+        }
+        if (mine) sh_odd[buf] = 1;
+        lds_barrier();
+        odd = __builtin_amdgcn_readfirstlane(sh_odd[buf]) != 0;
+      }
+      if (idle || tb > lim_hi || tb + kChunkTokens <= low_lo) continue;
+
+      // ---- S^T: token 32 u + 8 a + 4 hi + b in element 4 a + b of sc[u]
+      pc_floatx16 sc[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          ChunkFrag k;
+          k.u = *(const u32x4*)(kt + ka[f] + u * 32 * RB);
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[f].v, sc[u], 0, 0, 0);
+        }
+      }
+      if (present != ~0ull || tb + kChunkTokens - 1 > lim_lo || tb < low_hi) {
+        const uint64_t mine = present >> (4 * hi);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int slot = 32 * u + 8 * (e / 4) + e % 4, t = tb + slot + 4 * hi;
+            if (!((mine >> slot) & 1) || t > lim || t < low) sc[u][e] = -INFINITY;
+          }
+      }
+      // ---- running maximum and sum
+      float mx = sc[0][0];
+#pragma unroll
+      for (int e = 1; e < 32; ++e) mx = fmaxf(mx, sc[e / 16][e % 16]);
+      mx = across_32(mx, MaxOp()) * g.scale2;
+      if (__any(mx > m + kSlack || (m == -INFINITY && mx > -INFINITY))) {
+        const float mn = fmaxf(m, mx), fix = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= fix;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[ct][e] *= fix;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      ChunkFrag pr[4];                                             // P^T of 16 tokens each, in the cache's own type (their sum is not)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const float a = __builtin_amdgcn_exp2f(fmaf(sc[u][e], g.scale2, -ref)), c = __builtin_amdgcn_exp2f(fmaf(sc[u][e + 1], g.scale2, -ref));
+          l += a + c;
+          pr[2 * u + e / 8].u[e % 8 / 2] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)a, (__bf16)c});
+        }
+      if (odd) {
+        // token by token, for the rows that see it
+        for (int slot = 0; slot < kChunkTokens; ++slot) {
+          const int from = (slot >> 2 & 1) * 32 + col, t = tb + slot;
+          uint32_t word = 0;
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            if (k == (slot >> 5) * 8 + ((slot >> 3) & 3) * 2 + ((slot >> 1) & 1)) word = pr[k / 4].u[k % 4];
+          word = (uint32_t)__shfl((int)word, from);
+          const float weight = __uint_as_float(slot & 1 ? word & 0xffff0000u : word << 16);
+          if (!((present >> slot) & 1) || t > lim || t < low) continue;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int c = 32 * ct + 8 * (e / 4) + 4 * hi + e % 4;
+              const uint16_t* at = (const uint16_t*)(vt + slot * RB + ((c / 8) ^ value_swap<D>(slot)) * 16);
+              o[ct][e] = fmaf(weight, bf16_bits_to_float(at[c % 8]), o[ct][e]);
+            }
+        }
+        continue;
+      }
+      // ---- O^T: the inner indices of step k are tokens 16 k + 4 hi + {0 .. 3} and 16 k + 8 + 4 hi + {0 .. 3}
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          ChunkFrag v;
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            v.h[y] = __builtin_bit_cast(pc_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pc_s16x4*)(vt + va[ct][y] + k * 16 * RB)));
+          o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, pr[k].v, o[ct], 0, 0, 0);
+        }
+    }
+
+    // ---- out, or a partial
+    l = across_32(l, AddOp());
+    const bool whole = p.whole();
+    if (live) {
+      if (whole) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        char* dst = g.out + (int64_t)token * g.out_row + (int64_t)head * g.out_head;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = l == 0.f ? 0.f : o[ct][4 * a + e] * inv;
+            pc_u32x2 v;
+            v[0] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)y[0], (__bf16)y[1]});
+            v[1] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)y[2], (__bf16)y[3]});
+            *(__attribute__((address_space(1))) pc_u32x2*)(dst + (32 * ct + 8 * a + 4 * hi) * 2) = v;
+          }
+        if (hi == 0 && g.lse) g.lse[(int64_t)token * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+      } else {
+        float* slot = partial_slot(g, w, x == sh.begin);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) store_pair(slot + row * D + 32 * ct + 8 * (e / 4) + 4 * hi + e % 4, o[ct][e], o[ct][e + 1]);
+        if (hi == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
+      }
+    }
+    if (!whole) finish_item<uint16_t, D>(g, sh, p, lds, &sh_last);
+    x = min(sh.end, p.item1);
+  }
+}
+
+void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
+  // 16 tokens of one page, at offsets of 32 bits
+  const bool uniform = g.page % 16 == 0 && g.st_tok < (1ll << 26);
+  if (g.d == 64) {
+    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<64, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+    else hipLaunchKernelGGL((paged_chunk_kernel<64, false>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  } else {
+    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<128, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+    else hipLaunchKernelGGL((paged_chunk_kernel<128, false>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  }
+}
+
+}  // namespace tkphi
