@@ -151,8 +151,8 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
       char* const kt = lds + buf * 2 * Tile::BYTES;
       char* const vt = kt + Tile::BYTES;
 
-      // ---- a tile that some row of the workgroup does not see all of: values that nobody sees are zeros, whatever they hold, and one that is no
-      // number, or infinite, must not meet the zero weights of the rows that do not see it
+      // ---- a tile that some row of the workgroup does not see all of: values that nobody sees become zeros, whatever they hold, and so do those
+      // that are no numbers, or infinite, lest they meet the zero weights of rows that do not see them (add_odd puts them back)
       const int seen_first = s.cached + p.tile * g.tile_rows / g.G;                // limit of the workgroup's first row
       bool odd = false;
       if (present != ~0ull || tb + kChunkTokens - 1 > seen_first || (g.window > 0 && tb < it.end - g.window)) {
@@ -163,9 +163,17 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
           if (!((present >> r) & 1)) {
             *at = (u32x4){0u, 0u, 0u, 0u};
           } else {
-            const u32x4 v = *at;
+            u32x4 v = *at;
+            bool bad = false;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) mine = mine || (v[e] & 0x7f80u) == 0x7f80u || (v[e] & 0x7f800000u) == 0x7f800000u;
+            for (int e = 0; e < 4; ++e) {
+              const bool a = (v[e] & 0x7f80u) == 0x7f80u, c = (v[e] & 0x7f800000u) == 0x7f800000u;
+              if (a) v[e] &= 0xffff0000u;
+              if (c) v[e] &= 0xffffu;
+              bad = bad || a || c;
+            }
+            if (bad) *at = v;
+            mine = mine || bad;
           }
         }
         if (mine) sh_odd[buf] = 1;
@@ -177,15 +185,21 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
       // ---- S^T: token 32 u + 8 a + 4 hi + b in element 4 a + b of sc[u]
       pc_floatx16 sc[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
+      for (int e = 0; e < 16; ++e) sc[0][e] = sc[1][e] = 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
+      for (int f = 0; f < NF; ++f)
 #pragma unroll
-        for (int f = 0; f < NF; ++f) {
+        for (int u = 0; u < 2; ++u) {
           ChunkFrag k;
           k.u = *(const u32x4*)(kt + ka[f] + u * 32 * RB);
           sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[f].v, sc[u], 0, 0, 0);
         }
+      // the LDS reads run four ahead of the products that take them
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int k = 0; k < 2 * NF; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (k < 2 * NF - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       if (present != ~0ull || tb + kChunkTokens - 1 > lim_lo || tb < low_hi) {
         const uint64_t mine = present >> (4 * hi);
@@ -212,40 +226,21 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
           for (int e = 0; e < 16; ++e) o[ct][e] *= fix;
       }
       const float ref = m == -INFINITY ? 0.f : m;
-      ChunkFrag pr[4];                                             // P^T of 16 tokens each, in the cache's own type (their sum is not)
+      // ---- P^T of 16 tokens at a time, in the cache's own type (their sum is not), and O^T: the inner indices of step k are the tokens
+      // 16 k + 4 hi + {0 .. 3} and 16 k + 8 + 4 hi + {0 .. 3}
+      ChunkFrag pr[4];
+      float sum[4];
+      const auto weigh = [&](int k) {
+        float e[8];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+        for (int y = 0; y < 8; ++y) e[y] = __builtin_amdgcn_exp2f(fmaf(sc[k / 2][8 * (k & 1) + y], g.scale2, -ref));
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          const float a = __builtin_amdgcn_exp2f(fmaf(sc[u][e], g.scale2, -ref)), c = __builtin_amdgcn_exp2f(fmaf(sc[u][e + 1], g.scale2, -ref));
-          l += a + c;
-          pr[2 * u + e / 8].u[e % 8 / 2] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)a, (__bf16)c});
-        }
-      if (odd) {
-        // token by token, for the rows that see it
-        for (int slot = 0; slot < kChunkTokens; ++slot) {
-          const int from = (slot >> 2 & 1) * 32 + col, t = tb + slot;
-          uint32_t word = 0;
+        for (int y = 0; y < 4; ++y) pr[k].u[y] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)e[2 * y], (__bf16)e[2 * y + 1]});
+        sum[k] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
+      };
+      weigh(0);
 #pragma unroll
-          for (int k = 0; k < 16; ++k)
-            if (k == (slot >> 5) * 8 + ((slot >> 3) & 3) * 2 + ((slot >> 1) & 1)) word = pr[k / 4].u[k % 4];
-          word = (uint32_t)__shfl((int)word, from);
-          const float weight = __uint_as_float(slot & 1 ? word & 0xffff0000u : word << 16);
-          if (!((present >> slot) & 1) || t > lim || t < low) continue;
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int c = 32 * ct + 8 * (e / 4) + 4 * hi + e % 4;
-              const uint16_t* at = (const uint16_t*)(vt + slot * RB + ((c / 8) ^ value_swap<D>(slot)) * 16);
-              o[ct][e] = fmaf(weight, bf16_bits_to_float(at[c % 8]), o[ct][e]);
-            }
-        }
-        continue;
-      }
-      // ---- O^T: the inner indices of step k are tokens 16 k + 4 hi + {0 .. 3} and 16 k + 8 + 4 hi + {0 .. 3}
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) {
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
           ChunkFrag v;
@@ -254,6 +249,41 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
             v.h[y] = __builtin_bit_cast(pc_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pc_s16x4*)(vt + va[ct][y] + k * 16 * RB)));
           o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, pr[k].v, o[ct], 0, 0, 0);
         }
+        if (k < 3) weigh(k + 1);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      // the next step's weights between this one's products
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, 20, 0);
+#pragma unroll
+      for (int k = 0; k < 4 * CT; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (k < 4 * CT - 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        if (k < 3 * CT) __builtin_amdgcn_sched_group_barrier(0x002, 28 / CT, 0);
+      }
+      if (odd) {                                                   // token by token: what was taken out of the values, for the rows that see it
+#pragma unroll 1
+        for (int slot = 0; slot < kChunkTokens; ++slot) {
+          const int t = tb + slot;
+          uint32_t word = 0;
+#pragma unroll
+          for (int k = 0; k < 16; ++k)
+            if (k == (slot >> 5) * 8 + ((slot >> 3) & 3) * 2 + ((slot >> 1) & 1)) word = pr[k / 4].u[k % 4];
+          word = (uint32_t)__shfl((int)word, (slot >> 2 & 1) * 32 + col);
+          const float weight = __uint_as_float(slot & 1 ? word & 0xffff0000u : word << 16);
+          if (!((present >> slot) & 1)) continue;
+          const int pt = page_of(g, t), id = max(page_id(g, p.seq, pt), 0);
+          const uint16_t* v = (const uint16_t*)(g.V + (int64_t)id * g.st_page + p.h * g.st_head + (int64_t)(t - pt * g.page) * g.st_tok);
+          const bool sees = t <= lim && t >= low;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint16_t bits = v[32 * ct + 8 * (e / 4) + 4 * hi + e % 4];
+              if (sees && (bits & 0x7f80) == 0x7f80) o[ct][e] = fmaf(weight, bf16_bits_to_float(bits), o[ct][e]);
+            }
+        }
+      }
     }
 
     // ---- out, or a partial
