@@ -7,7 +7,8 @@ namespace tkphi {
 
 constexpr int kPagedThreads = 256;
 constexpr int kPagedRows = 32;            // query rows (token x query head of one KV head) of a split item at most: two tiles of 16
-constexpr int kChunkRows = 128;           // and of an item of the chunk kernel
+constexpr int kChunkRows = 256;           // and of an item of the chunk kernel
+constexpr int kChunkSplit = 256;          // workgroups of the chunk kernel: one per CU
 constexpr int kMaxSplit = 1024;           // workgroups that the work of one attention call is spread over, at most
 constexpr int kBlockRowGroup = 512;       // query tokens whose block scores the workspace holds at once, at most
 constexpr int kMaxKept = 1024;            // blocks a query sees, at most

@@ -61,7 +61,7 @@ tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, Pag
               st->reserved);
     return TKPHI_EINVAL;
   }
-  if (st->n_seqs > 65535 || st->rows > (1 << 27) || (int64_t)st->n_seqs * (st->max_len / 16 + 2) >= (1ll << 31)) {
+  if (st->n_seqs > 65535 || st->rows > (1 << 27) || st->max_len > (1 << 30) || (int64_t)st->n_seqs * (st->max_len / 16 + 2) >= (1ll << 31)) {
     set_error("step: n_seqs=%d rows=%d max_len=%d too large", st->n_seqs, st->rows, st->max_len);
     return TKPHI_ESHAPE;
   }
@@ -96,7 +96,7 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   g->unit = chunk ? 64 : kPagedThreads / 64 * (g->dtype == TKPHI_BF16 ? 32 : 16);
   g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * g->tiles);
   const int64_t units = (int64_t)g->n_seqs * g->tiles * g->Hkv * up(std::max(g->max_len, 1), g->unit);      // at most
-  g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? 512 : 768));
+  g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? kChunkSplit : 768));
 }
 
 void plan_blocks(const tkphi_paged_config* c, PagedGeom* g) {
@@ -124,7 +124,7 @@ PagedSpace space_of(const tkphi_paged_config* c, const PagedGeom& g0) {
   if (g.block) block_slots = heads * (c->workgroups ? std::min(c->workgroups, 64) : 1) + (c->workgroups ? 0 : 2 * 512 + g.Hkv * 64);
   s.arrived = 256;
   s.partial = s.arrived + padded(std::max<size_t>(kMaxSplit, heads) * sizeof(uint32_t));
-  s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, (c->workgroups ? c->workgroups : 512) * kChunkRows) * 2, (size_t)block_slots * 16) * row_bytes);
+  s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, (c->workgroups ? c->workgroups : kChunkSplit) * kChunkRows) * 2, (size_t)block_slots * 16) * row_bytes);
   s.plan_item = s.plan_end + padded((size_t)items * sizeof(int64_t));
   s.keys = s.plan_item + padded((size_t)items * sizeof(int2) + 256);
   s.list = s.keys + padded(g.block ? (size_t)heads * g.max_blocks * sizeof(uint64_t) : 0);

@@ -7,7 +7,7 @@ namespace tkphi {
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
-constexpr int kJoinLds = kJoinPairs * 8 + kPagedThreads * 8 + kPagedRows * 8;
+constexpr int join_lds(int threads) { return kJoinPairs * 8 + threads * 8 + kPagedRows * 8; }
 
 template <typename T>
 __device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float o, float m, float l) {
@@ -32,20 +32,20 @@ static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
 // Joins `pieces` partials of `rows` x D of an item, piece p at slot(p) with (m, l) behind `stride` rows; called by the last workgroup to
 // arrive.  Everything a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
 // took 30 us.
-template <typename T, int D, typename Slot, typename RowOf>
+template <typename T, int D, int NT, typename Slot, typename RowOf>
 __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
   constexpr int HALF = D / 2, BATCH = 8;
   float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
   float2* part = ml + kJoinPairs;                                  // [threads]
-  float2* sums = part + kPagedThreads;                             // [rows]: m, l of the whole
+  float2* sums = part + NT;                             // [rows]: m, l of the whole
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int group = min(min(rows, kPagedRows), kJoinPairs / pieces);
   for (int r0 = 0; r0 < rows; r0 += group) {
     const int n = min(group, rows - r0);
     __syncthreads();
-    for (int x = tid; x < n * pieces; x += kPagedThreads) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
+    for (int x = tid; x < n * pieces; x += NT) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
     __syncthreads();
-    for (int r = wave; r < n; r += kPagedThreads / 64) {
+    for (int r = wave; r < n; r += NT / 64) {
       float2* row = ml + r * pieces;
       float m = -INFINITY, l = 0.f;
       for (int p = lane; p < pieces; p += 64) m = fmaxf(m, row[p].x);
@@ -61,8 +61,8 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
     }
     __syncthreads();
     // elements (row, pair of channels); where they are few, the pieces are shared by several threads
-    const int items = n * HALF, share = max(1, kPagedThreads / items);
-    for (int x0 = 0; x0 < items; x0 += kPagedThreads) {
+    const int items = n * HALF, share = max(1, NT / items);
+    for (int x0 = 0; x0 < items; x0 += NT) {
       const int x = share > 1 ? tid % items : x0 + tid, part_of = share > 1 ? tid / items : 0;
       float2 o = make_float2(0.f, 0.f);
       if (x < items && part_of < share) {
@@ -128,6 +128,9 @@ __device__ __forceinline__ ItemRange item_range(const PagedGeom& g, const PagedS
   return it;
 }
 __device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& it) { return (it.end - it.begin + g.unit - 1) / g.unit; }
+
+// Workgroup b of n -> its share's number: consecutive shares, which pass over the same KV head, on one XCD (workgroup b runs on XCD b % 8)
+__device__ __forceinline__ int share_number(int b, int n) { return n % 8 == 0 ? b % 8 * (n / 8) + b / 8 : b; }
 
 // The work of a call in order: KV heads outermost, then items, then units of an item.  Workgroup w of W takes the units
 // [all w / W, all (w + 1) / W).
@@ -200,14 +203,14 @@ __device__ __forceinline__ float* partial_slot(const PagedGeom& g, int w, bool f
   return g.partial + ((int64_t)w * 2 + (first ? 0 : 1)) * g.tile_rows * (g.d + 2);
 }
 // After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.
-template <typename T, int D>
+template <typename T, int D, int NT>
 __device__ __forceinline__ void finish_item(const PagedGeom& g, const Share& sh, const Piece& p, char* lds, int* sh_last) {
   // the workgroup of a unit is the last w with all w / W <= unit
   const auto owner = [&](int64_t unit) { return (int)(((unit + 1) * sh.W + sh.all - 1) / sh.all) - 1; };
   const int w0 = owner(p.item0), w1 = owner(p.item1 - 1);
   if (!last_to_arrive(g.arrived + w0, w1 - w0 + 1, sh_last)) return;
   const bool first = sh.all * w0 / sh.W == p.item0;       // the first workgroup's share starts with this item
-  join_pieces<T, D>(g, w1 - w0 + 1, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
+  join_pieces<T, D, NT>(g, w1 - w0 + 1, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
                     [&](int row, int* token, int* head) { p.place(g, row, token, head); });
 }
 

@@ -239,7 +239,7 @@ struct WaveAttend {
 
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
 template <typename T, int D, int RT>
-constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), kJoinLds); }
+constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads)); }
 
 // Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
 template <typename T, int D, int RT, typename Emit>
@@ -385,7 +385,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
         if (c == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     });
-    if (!whole) finish_item<T, D>(g, sh, p, lds, &sh_last);
+    if (!whole) finish_item<T, D, kPagedThreads>(g, sh, p, lds, &sh_last);
     __syncthreads();
     x = min(sh.end, p.item1);
   }
@@ -452,7 +452,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
     }
   });
   if (!whole && last_to_arrive(g.arrived + at_list, pieces, &sh_last))
-    join_pieces<T, D>(g, pieces, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
+    join_pieces<T, D, kPagedThreads>(g, pieces, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
                       [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
 }
 

@@ -1,10 +1,9 @@
 // tkphi_paged_attention for many query rows per KV head (chunks, prompts), bf16.
 //
-// One pass over the keys and values with the running maximum and sum of the softmax.  A workgroup holds 128 query rows (new tokens
+// One pass over the keys and values with the running maximum and sum of the softmax.  A workgroup holds 256 query rows (new tokens
 // times the query heads of one KV head, a wavefront 32 of them in registers) and passes over tiles of 64 cached tokens, which go from memory straight to
-// LDS, one tile ahead; S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds all of S^T for one query row but the half
+// LDS, a few tiles ahead; S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds all of S^T for one query row but the half
 // its partner lane 32 further has, and exactly what it has to deliver of P^T: maximum and sum take one exchange, P none.
-// Two workgroups per CU: while the wavefronts of one exponentiate, those of the other multiply.
 #include "paged_attention.h"
 
 namespace tkphi {
@@ -21,7 +20,9 @@ union ChunkFrag {
 };
 
 constexpr int kChunkTokens = 64;
-constexpr int kChunkWaves = kPagedThreads / 64;
+constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
+constexpr int kWaveTokens = kChunkTokens / kChunkWaves;            // rows of a tile that a wavefront loads
+constexpr int kPageCache = 4096;                                   // entries of the page table in LDS
 constexpr float kSlack = 8.f;             // the reference of the exponentials is raised when a score passes it by 2^8 (sums stay far from overflow)
 
 // LDS of one tile: rows of D bf16 in 16-byte pieces, piece c of row r at place c ^ key_swap(r) or c ^ value_swap(r).  Keys are read as 16 bytes of 32
@@ -34,24 +35,29 @@ template <int D> __device__ __forceinline__ int value_swap(int r) {
 template <int D>
 struct ChunkTile {
   static constexpr int RB = D * 2, PIECES = RB / 16, BYTES = kChunkTokens * RB;
+  static constexpr int BUFS = 4;                                   // tiles in LDS: one that is worked on, the others on their way
   static constexpr int ROWS = 1024 / RB;                           // rows that one load of a wavefront covers
-  static constexpr int LOADS = kChunkTokens / kChunkWaves / ROWS;  // loads per wavefront of K, and of V
+  static constexpr int LOADS = kWaveTokens / ROWS;                 // loads per wavefront of K, and of V
 };
+static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 8, "");
 
+// UNIFORM: 8 tokens always lie in one page
 template <int D, bool UNIFORM>
-__global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom g) {
+__global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g) {
   using Tile = ChunkTile<D>;
-  constexpr int RB = Tile::RB, NF = D / 16, CT = D / 32;
-  // two tiles of K and V each; later the join's scratch
-  __shared__ __align__(1024) char lds[4 * Tile::BYTES];
+  constexpr int RB = Tile::RB, NF = D / 16, CT = D / 32, BUFS = Tile::BUFS;
+  // tiles of K and V each; later the join's scratch
+  __shared__ __align__(1024) char lds[BUFS * 2 * Tile::BYTES];
+  __shared__ int sh_page[kPageCache];
+  __shared__ __align__(8) uint8_t sh_present[BUFS][kChunkWaves];   // which tokens of the tile anyone may see, 8 per wavefront
   __shared__ int sh_last, sh_odd[2];
-  __shared__ uint32_t sh_present[2][kChunkWaves];                  // which tokens of the tile anyone may see, 16 per wavefront
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
   const uint32_t lds0 = (uint32_t)(size_t)(lds_ptr)lds;
   if (tid < 2) sh_odd[tid] = 0;
 
-  // where this lane reads: keys of row col, channels 16 f + 8 hi ..; values of 4 rows (see lds_read_transposed's use below)
+  // where this lane reads: keys of row col, channels 16 f + 8 hi ..; values of 4 rows, transposed by the read (lane i of 16 points at
+  // row i / 4, channels 4 (i % 4) .. and gets channel i of the four)
   int ka[NF], va[CT][2];
 #pragma unroll
   for (int f = 0; f < NF; ++f) ka[f] = col * RB + ((2 * f + hi) ^ key_swap<D>(col)) * 16;
@@ -62,19 +68,24 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
       const int r = 8 * x + 4 * hi + (i16 >> 2), c = 4 * ct + 2 * grp + ((i16 & 3) >> 1);
       va[ct][x] = r * RB + (c ^ value_swap<D>(r)) * 16 + (i16 & 1) * 8;
     }
-  // and what it loads: pieces of rows 16 wave + ROWS k + lane / PIECES of the tile
+  // and what it loads: places lane % PIECES of rows 8 wave + ROWS k + lane / PIECES of the tile
   const int lrow = lane / Tile::PIECES, lplace = lane % Tile::PIECES;
+  uint32_t kat[Tile::LOADS], vat[Tile::LOADS];                     // byte offsets from the row, where rows adjoin from the wavefront's first
+#pragma unroll
+  for (int k = 0; k < Tile::LOADS; ++k) {
+    const int r = k * Tile::ROWS + lrow, rt = wave * kWaveTokens + r;
+    const uint32_t row = UNIFORM ? (uint32_t)(r * (int)g.st_tok) : 0u;
+    kat[k] = row + (lplace ^ key_swap<D>(rt)) * 16;
+    vat[k] = row + (lplace ^ value_swap<D>(rt)) * 16;
+  }
 
-  // keep consecutive shares, which pass over the same KV head, on one XCD (workgroup b runs on XCD b % 8)
-  const int nb = gridDim.x, b = blockIdx.x;
-  const int w = nb % 8 == 0 ? (b % 8) * (nb / 8) + b / 8 : b;
+  const int w = share_number(blockIdx.x, gridDim.x);
   const Share sh = share_of(g, w, 4);
   for (int64_t x = sh.begin; x < sh.end;) {
     const Piece p = piece_at(g, sh, x);
     const PagedSeq s = p.s;
     const ItemRange it = p.it;
     const int t0 = it.begin + p.u0 * kChunkTokens, t1 = min(it.begin + p.u1 * kChunkTokens, it.end);
-    const int n = (t1 - t0 + kChunkTokens - 1) / kChunkTokens;
 
     // ---- query rows
     ChunkFrag q[NF];
@@ -97,67 +108,77 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[ct][e] = 0.f;
 
-    const auto own_page = [&](int i) {       // the page of this wavefront's 16 tokens of tile i, or of the lane's token lane & 15 of them
-      const int t = t0 + i * kChunkTokens + wave * 16 + (UNIFORM ? 0 : i16);
-      return t < t1 && t + (UNIFORM ? 15 : 0) >= it.low ? page_id(g, p.seq, page_of(g, t)) : -1;
-    };
-    const auto request = [&](int i, int id) {
-      const int buf = i & 1, tw = t0 + i * kChunkTokens + wave * 16;
-      const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * 16 * RB, vdst = kdst + Tile::BYTES;
-      uint32_t present;
+    const char* const Kh = g.K + p.h * g.st_head;
+    const char* const Vh = g.V + p.h * g.st_head;
+    const int seen_first = s.cached + p.tile * g.tile_rows / g.G;  // limit of the workgroup's first row
+    const int low_last = g.window > 0 ? it.end - g.window : 0;     // first token that its last row sees
+
+    // Stretches of the piece whose part of the page table fits LDS
+    const int stretch = (int)min((int64_t)16384, (int64_t)(kPageCache - 2) * g.page / kChunkTokens * kChunkTokens);
+    for (int ts = t0; ts < t1; ts += stretch) {
+    const int te = min(ts + stretch, t1), n = (te - ts + kChunkTokens - 1) / kChunkTokens;
+    const int page0 = page_of(g, ts), page_lo = page_of(g, max(ts, it.low)), page_hi = page_of(g, te - 1);
+    __syncthreads();                                               // (the stretch before, or the join of the item before, is done with LDS)
+    for (int e = page_lo + tid; e <= page_hi; e += kChunkThreads) sh_page[e - page0] = page_id(g, p.seq, e);
+    __syncthreads();
+
+    const auto request = [&](int i) {
+      const int buf = i % BUFS, tw = ts + i * kChunkTokens + wave * kWaveTokens;
+      const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * kWaveTokens * RB, vdst = kdst + Tile::BYTES;
+      const int a = max(it.low - tw, 0), z = min(te - tw, kWaveTokens);          // tokens [a, z) of the 8
+      uint32_t present = a >= z ? 0u : ((1u << z) - 1u) & ~((1u << a) - 1u);
       if constexpr (UNIFORM) {
-        const int uid = __builtin_amdgcn_readfirstlane(id);
-        const int64_t at = (int64_t)max(uid, 0) * g.st_page + p.h * g.st_head + (int64_t)(tw - page_of(g, tw) * g.page) * g.st_tok;
-        const int a = max(it.low - tw, 0), z = min(t1 - tw, 16);         // tokens [a, z) of the 16
-        present = uid < 0 || a >= z ? 0u : ((1u << z) - 1u) & ~((1u << a) - 1u);
+        const int pt = page_of(g, tw);
+        const int id = present ? __builtin_amdgcn_readfirstlane(sh_page[pt - page0]) : -1;
+        if (id < 0) present = 0;
+        const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(tw - pt * g.page) * g.st_tok;
 #pragma unroll
-        for (int k = 0; k < Tile::LOADS; ++k) {
-          const int r = k * Tile::ROWS + lrow;
-          load_to_lds16(g.K + at, (uint32_t)(r * (int)g.st_tok + (lplace ^ key_swap<D>(r)) * 16), kdst + k * 1024);
-        }
+        for (int k = 0; k < Tile::LOADS; ++k) load_to_lds16(Kh + at, kat[k], kdst + k * 1024);
 #pragma unroll
-        for (int k = 0; k < Tile::LOADS; ++k) {
-          const int r = k * Tile::ROWS + lrow;
-          load_to_lds16(g.V + at, (uint32_t)(r * (int)g.st_tok + (lplace ^ value_swap<D>(r)) * 16), vdst + k * 1024);
-        }
+        for (int k = 0; k < Tile::LOADS; ++k) load_to_lds16(Vh + at, vat[k], vdst + k * 1024);
       } else {
-        const int t = tw + i16;
-        present = (uint32_t)__ballot(id >= 0 && t >= it.low && t < t1) & 0xffffu;
-        const int64_t at = (int64_t)max(id, 0) * g.st_page + p.h * g.st_head + (int64_t)(t - page_of(g, t) * g.page) * g.st_tok;
+        uint32_t here = 0;
 #pragma unroll
         for (int k = 0; k < Tile::LOADS; ++k) {
-          const int r = k * Tile::ROWS + lrow;
-          const int64_t from = (int64_t)(uint32_t)__shfl((int)(uint32_t)at, r) | (int64_t)__shfl((int)(at >> 32), r) << 32;
-          load_to_lds16(g.K + from + (lplace ^ key_swap<D>(r)) * 16, kdst + k * 1024);
-          load_to_lds16(g.V + from + (lplace ^ value_swap<D>(r)) * 16, vdst + k * 1024);
+          const int r = k * Tile::ROWS + lrow, t = tw + r, pt = page_of(g, t);
+          const int id = (present >> r) & 1 ? sh_page[pt - page0] : -1;
+          const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.page) * g.st_tok;
+          load_to_lds16(Kh + at + kat[k], kdst + k * 1024);
+          load_to_lds16(Vh + at + vat[k], vdst + k * 1024);
+          const uint64_t there = __ballot(id >= 0);
+#pragma unroll
+          for (int y = 0; y < Tile::ROWS; ++y) here |= (uint32_t)((there >> (y * Tile::PIECES)) & 1) << (k * Tile::ROWS + y);
         }
+        present = here;
       }
-      if (lane == 0) sh_present[buf][wave] = present;
+      if (lane == 0) sh_present[buf][wave] = (uint8_t)present;
     };
 
-    __syncthreads();                                               // (the join of the item before is done with LDS)
-    request(0, own_page(0));
-    int next_id = own_page(1);
-    for (int i = 0; i < n; ++i) {
-      wait_vm_loads<0>();
-      lds_barrier();                                               // tile i is there, tile i - 1 is done with
-      const int buf = i & 1, tb = t0 + i * kChunkTokens;
-      if (tid == 0) sh_odd[1 - buf] = 0;
-      if (i + 1 < n) request(i + 1, next_id);
-      next_id = own_page(i + 2);
-      uint64_t present = 0;
 #pragma unroll
-      for (int k = 0; k < kChunkWaves; ++k) present |= (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)sh_present[buf][k]) << (16 * k);
+    for (int i = 0; i < BUFS - 1; ++i)
+      if (i < n) request(i);
+    for (int i = 0; i < n; ++i) {
+      // tile i is there (loads come back in order), tile i - 1 is done with
+      const int ahead = min(n - 1 - i, BUFS - 2);
+      if (ahead == BUFS - 2) wait_vm_loads<(BUFS - 2) * 2 * Tile::LOADS>();
+      else if (ahead == 1) wait_vm_loads<2 * Tile::LOADS>();
+      else wait_vm_loads<0>();
+      lds_barrier();
+      const int buf = i % BUFS, tb = ts + i * kChunkTokens;
+      if (tid == 0) sh_odd[1 - (i & 1)] = 0;
+      const uint64_t in_lds = *(const uint64_t*)sh_present[buf];
+      const uint64_t present = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)in_lds) |
+                               (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(in_lds >> 32)) << 32;
+      if (i + BUFS - 1 < n) request(i + BUFS - 1);
       char* const kt = lds + buf * 2 * Tile::BYTES;
       char* const vt = kt + Tile::BYTES;
 
       // ---- a tile that some row of the workgroup does not see all of: values that nobody sees become zeros, whatever they hold, and so do those
       // that are no numbers, or infinite, lest they meet the zero weights of rows that do not see them (add_odd puts them back)
-      const int seen_first = s.cached + p.tile * g.tile_rows / g.G;                // limit of the workgroup's first row
       bool odd = false;
-      if (present != ~0ull || tb + kChunkTokens - 1 > seen_first || (g.window > 0 && tb < it.end - g.window)) {
+      if (present != ~0ull || tb + kChunkTokens - 1 > seen_first || tb < low_last) {
         bool mine = false;
-        for (int k = tid; k < kChunkTokens * Tile::PIECES; k += kPagedThreads) {
+        for (int k = tid; k < kChunkTokens * Tile::PIECES; k += kChunkThreads) {
           const int r = k / Tile::PIECES;
           u32x4* at = (u32x4*)(vt + k * 16);
           if (!((present >> r) & 1)) {
@@ -176,9 +197,9 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
             mine = mine || bad;
           }
         }
-        if (mine) sh_odd[buf] = 1;
+        if (mine) sh_odd[i & 1] = 1;
         lds_barrier();
-        odd = __builtin_amdgcn_readfirstlane(sh_odd[buf]) != 0;
+        odd = __builtin_amdgcn_readfirstlane(sh_odd[i & 1]) != 0;
       }
       if (idle || tb > lim_hi || tb + kChunkTokens <= low_lo) continue;
 
@@ -286,6 +307,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
       }
     }
 
+    }
     // ---- out, or a partial
     l = across_32(l, AddOp());
     const bool whole = p.whole();
@@ -315,20 +337,19 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_chunk_kernel(PagedGeom
         if (hi == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     }
-    if (!whole) finish_item<uint16_t, D>(g, sh, p, lds, &sh_last);
+    if (!whole) finish_item<uint16_t, D, kChunkThreads>(g, sh, p, lds, &sh_last);
     x = min(sh.end, p.item1);
   }
 }
 
 void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
-  // 16 tokens of one page, at offsets of 32 bits
-  const bool uniform = g.page % 16 == 0 && g.st_tok < (1ll << 26);
+  const bool uniform = g.page % kWaveTokens == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
   if (g.d == 64) {
-    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<64, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
-    else hipLaunchKernelGGL((paged_chunk_kernel<64, false>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<64, true>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
+    else hipLaunchKernelGGL((paged_chunk_kernel<64, false>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
   } else {
-    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<128, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
-    else hipLaunchKernelGGL((paged_chunk_kernel<128, false>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<128, true>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
+    else hipLaunchKernelGGL((paged_chunk_kernel<128, false>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
   }
 }
 
