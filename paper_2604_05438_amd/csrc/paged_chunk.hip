@@ -1,8 +1,8 @@
 // tkphi_paged_attention for many query rows per KV head (chunks, prompts), bf16.
 //
 // One pass over the keys and values with the running maximum and sum of the softmax.  A workgroup holds 256 query rows (new tokens
-// times the query heads of one KV head, a wavefront 32 of them in registers) and passes over tiles of 64 cached tokens, which go from memory straight to
-// LDS, a few tiles ahead; S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds all of S^T for one query row but the half
+// times the query heads of one KV head, a wavefront 32 of them in registers) and passes over tiles of 128 cached tokens, which go from memory straight to
+// LDS a tile or more ahead, 64 of them at a time; S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds all of S^T for one query row but the half
 // its partner lane 32 further has, and exactly what it has to deliver of P^T: maximum and sum take one exchange, P none.
 #include "paged_attention.h"
 
@@ -19,9 +19,10 @@ union ChunkFrag {
   pc_u32x2 h[2];
 };
 
-constexpr int kChunkTokens = 64;
+constexpr int kChunkTokens = 64;                                   // that a wavefront takes at a time
+constexpr int kTileTokens = 128;                                   // that go to LDS at a time
 constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
-constexpr int kWaveTokens = kChunkTokens / kChunkWaves;            // rows of a tile that a wavefront loads
+constexpr int kWaveTokens = kTileTokens / kChunkWaves;            // rows of a tile that a wavefront loads
 constexpr int kPageCache = 4096;                                   // entries of the page table in LDS
 constexpr float kSlack = 8.f;             // the reference of the exponentials is raised when a score passes it by 2^8 (sums stay far from overflow)
 
@@ -34,14 +35,14 @@ template <int D> __device__ __forceinline__ int value_swap(int r) {
 
 template <int D>
 struct ChunkTile {
-  static constexpr int RB = D * 2, PIECES = RB / 16, BYTES = kChunkTokens * RB;
-  static constexpr int BUFS = 4;                                   // tiles in LDS: one that is worked on, the others on their way
+  static constexpr int RB = D * 2, PIECES = RB / 16, BYTES = kTileTokens * RB;
+  static constexpr int BUFS = 65536 / BYTES;                       // tiles in LDS: one that is worked on, the others on their way
   static constexpr int ROWS = 1024 / RB;                           // rows that one load of a wavefront covers
   static constexpr int LOADS = kWaveTokens / ROWS;                 // loads per wavefront of K, and of V
 };
-static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 8, "");
+static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 16, "");
 
-// UNIFORM: 8 tokens always lie in one page
+// UNIFORM: 16 tokens always lie in one page
 template <int D, bool UNIFORM>
 __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g) {
   using Tile = ChunkTile<D>;
@@ -49,12 +50,12 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
   // tiles of K and V each; later the join's scratch
   __shared__ __align__(1024) char lds[BUFS * 2 * Tile::BYTES];
   __shared__ int sh_page[kPageCache];
-  __shared__ __align__(8) uint8_t sh_present[BUFS][kChunkWaves];   // which tokens of the tile anyone may see, 8 per wavefront
-  __shared__ int sh_last, sh_odd[2];
+  __shared__ __align__(8) uint16_t sh_present[BUFS][kChunkWaves];  // which tokens of the tile anyone may see, 16 per wavefront
+  __shared__ int sh_last, sh_odd[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
   const uint32_t lds0 = (uint32_t)(size_t)(lds_ptr)lds;
-  if (tid < 2) sh_odd[tid] = 0;
+  if (tid < 4) sh_odd[tid] = 0;
 
   // where this lane reads: keys of row col, channels 16 f + 8 hi ..; values of 4 rows, transposed by the read (lane i of 16 points at
   // row i / 4, channels 4 (i % 4) .. and gets channel i of the four)
@@ -68,7 +69,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
       const int r = 8 * x + 4 * hi + (i16 >> 2), c = 4 * ct + 2 * grp + ((i16 & 3) >> 1);
       va[ct][x] = r * RB + (c ^ value_swap<D>(r)) * 16 + (i16 & 1) * 8;
     }
-  // and what it loads: places lane % PIECES of rows 8 wave + ROWS k + lane / PIECES of the tile
+  // and what it loads: places lane % PIECES of rows 16 wave + ROWS k + lane / PIECES of the tile
   const int lrow = lane / Tile::PIECES, lplace = lane % Tile::PIECES;
   uint32_t kat[Tile::LOADS], vat[Tile::LOADS];                     // byte offsets from the row, where rows adjoin from the wavefront's first
 #pragma unroll
@@ -116,16 +117,16 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
     // Stretches of the piece whose part of the page table fits LDS
     const int stretch = (int)min((int64_t)16384, (int64_t)(kPageCache - 2) * g.page / kChunkTokens * kChunkTokens);
     for (int ts = t0; ts < t1; ts += stretch) {
-    const int te = min(ts + stretch, t1), n = (te - ts + kChunkTokens - 1) / kChunkTokens;
+    const int te = min(ts + stretch, t1), n = (te - ts + kTileTokens - 1) / kTileTokens;
     const int page0 = page_of(g, ts), page_lo = page_of(g, max(ts, it.low)), page_hi = page_of(g, te - 1);
     __syncthreads();                                               // (the stretch before, or the join of the item before, is done with LDS)
     for (int e = page_lo + tid; e <= page_hi; e += kChunkThreads) sh_page[e - page0] = page_id(g, p.seq, e);
     __syncthreads();
 
     const auto request = [&](int i) {
-      const int buf = i % BUFS, tw = ts + i * kChunkTokens + wave * kWaveTokens;
+      const int buf = i % BUFS, tw = ts + i * kTileTokens + wave * kWaveTokens;
       const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * kWaveTokens * RB, vdst = kdst + Tile::BYTES;
-      const int a = max(it.low - tw, 0), z = min(te - tw, kWaveTokens);          // tokens [a, z) of the 8
+      const int a = max(it.low - tw, 0), z = min(te - tw, kWaveTokens);          // tokens [a, z) of the 16
       uint32_t present = a >= z ? 0u : ((1u << z) - 1u) & ~((1u << a) - 1u);
       if constexpr (UNIFORM) {
         const int pt = page_of(g, tw);
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         }
         present = here;
       }
-      if (lane == 0) sh_present[buf][wave] = (uint8_t)present;
+      if (lane == 0) sh_present[buf][wave] = (uint16_t)present;
     };
 
 #pragma unroll
@@ -160,18 +161,45 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
     for (int i = 0; i < n; ++i) {
       // tile i is there (loads come back in order), tile i - 1 is done with
       const int ahead = min(n - 1 - i, BUFS - 2);
-      if (ahead == BUFS - 2) wait_vm_loads<(BUFS - 2) * 2 * Tile::LOADS>();
+      if (ahead == 0) wait_vm_loads<0>();
       else if (ahead == 1) wait_vm_loads<2 * Tile::LOADS>();
-      else wait_vm_loads<0>();
+      else wait_vm_loads<4 * Tile::LOADS>();
       lds_barrier();
-      const int buf = i % BUFS, tb = ts + i * kChunkTokens;
-      if (tid == 0) sh_odd[1 - (i & 1)] = 0;
-      const uint64_t in_lds = *(const uint64_t*)sh_present[buf];
+      if (tid < 2) sh_odd[2 * (1 - (i & 1)) + tid] = 0;
+      const int buf = i % BUFS;
+      if (i + BUFS - 1 < n) request(i + BUFS - 1);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+      const int tb = ts + i * kTileTokens + half * kChunkTokens;
+      if (tb >= te) break;
+      const bool skip = idle || tb > lim_hi || tb + kChunkTokens <= low_lo;        // (nothing here for this wavefront)
+      char* const kt = lds + buf * 2 * Tile::BYTES + half * kChunkTokens * RB;
+      char* const vt = kt + Tile::BYTES;
+      const uint64_t in_lds = *(const uint64_t*)(sh_present[buf] + half * 4);
+
+      // ---- S^T: token 32 u + 8 a + 4 hi + b in element 4 a + b of sc[u]
+      pc_floatx16 sc[2];
+      if (!skip) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[0][e] = sc[1][e] = 0.f;
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          ChunkFrag k;
+          k.u = *(const u32x4*)(kt + ka[f] + u * 32 * RB);
+          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[f].v, sc[u], 0, 0, 0);
+        }
+      // the LDS reads run four ahead of the products that take them
+      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+      for (int k = 0; k < 2 * NF; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        if (k < 2 * NF - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      }
       const uint64_t present = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)in_lds) |
                                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(in_lds >> 32)) << 32;
-      if (i + BUFS - 1 < n) request(i + BUFS - 1);
-      char* const kt = lds + buf * 2 * Tile::BYTES;
-      char* const vt = kt + Tile::BYTES;
 
       // ---- a tile that some row of the workgroup does not see all of: values that nobody sees become zeros, whatever they hold, and so do those
       // that are no numbers, or infinite, lest they meet the zero weights of rows that do not see them (add_odd puts them back)
@@ -197,31 +225,12 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
             mine = mine || bad;
           }
         }
-        if (mine) sh_odd[i & 1] = 1;
+        if (mine) sh_odd[2 * (i & 1) + half] = 1;
         lds_barrier();
-        odd = __builtin_amdgcn_readfirstlane(sh_odd[i & 1]) != 0;
+        odd = __builtin_amdgcn_readfirstlane(sh_odd[2 * (i & 1) + half]) != 0;
       }
-      if (idle || tb > lim_hi || tb + kChunkTokens <= low_lo) continue;
+      if (skip) continue;
 
-      // ---- S^T: token 32 u + 8 a + 4 hi + b in element 4 a + b of sc[u]
-      pc_floatx16 sc[2];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) sc[0][e] = sc[1][e] = 0.f;
-#pragma unroll
-      for (int f = 0; f < NF; ++f)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          ChunkFrag k;
-          k.u = *(const u32x4*)(kt + ka[f] + u * 32 * RB);
-          sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[f].v, sc[u], 0, 0, 0);
-        }
-      // the LDS reads run four ahead of the products that take them
-      __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
-#pragma unroll
-      for (int k = 0; k < 2 * NF; ++k) {
-        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-        if (k < 2 * NF - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      }
       if (present != ~0ull || tb + kChunkTokens - 1 > lim_lo || tb < low_hi) {
         const uint64_t mine = present >> (4 * hi);
 #pragma unroll
@@ -305,8 +314,8 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
             }
         }
       }
+      }
     }
-
     }
     // ---- out, or a partial
     l = across_32(l, AddOp());
