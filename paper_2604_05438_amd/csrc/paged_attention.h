@@ -7,7 +7,7 @@ namespace tkphi {
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
-constexpr int join_lds(int threads) { return kJoinPairs * 8 + threads * 8 + kPagedRows * 8; }
+constexpr int join_lds(int threads, int rows) { return (kJoinPairs + threads + rows) * 8; }
 
 template <typename T>
 __device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float o, float m, float l) {
@@ -30,44 +30,65 @@ __device__ __forceinline__ float2 load_pair(const float* p) {
 static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
 
 // Joins `pieces` partials of `rows` x D of an item, piece p at slot(p) with (m, l) behind `stride` rows; called by the last workgroup to
-// arrive.  Everything a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
-// took 30 us.
+// arrive.  What a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
+// of one row took 30 us, and one of 2 pieces of 256 rows as much.
 template <typename T, int D, int NT, typename Slot, typename RowOf>
 __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
   constexpr int HALF = D / 2, BATCH = 8;
   float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
   float2* part = ml + kJoinPairs;                                  // [threads]
-  float2* sums = part + NT;                             // [rows]: m, l of the whole
+  float2* sums = part + NT;                                        // [rows]: m, l of the whole
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int group = min(min(rows, kPagedRows), kJoinPairs / pieces);
+  const int group = min(rows, kJoinPairs / pieces);
   for (int r0 = 0; r0 < rows; r0 += group) {
     const int n = min(group, rows - r0);
     __syncthreads();
     for (int x = tid; x < n * pieces; x += NT) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
     __syncthreads();
-    for (int r = wave; r < n; r += NT / 64) {
-      float2* row = ml + r * pieces;
-      float m = -INFINITY, l = 0.f;
-      for (int p = lane; p < pieces; p += 64) m = fmaxf(m, row[p].x);
-      m = wave_max(m);
-      const float ref = m == -INFINITY ? 0.f : m;
-      for (int p = lane; p < pieces; p += 64) {
-        const float f = __builtin_amdgcn_exp2f(row[p].x - ref);
-        l = fmaf(row[p].y, f, l);
-        row[p].x = f;
+    if (pieces <= 8) {
+      for (int r = tid; r < n; r += NT) {
+        float2* row = ml + r * pieces;
+        float m = -INFINITY, l = 0.f;
+        for (int p = 0; p < pieces; ++p) m = fmaxf(m, row[p].x);
+        const float ref = m == -INFINITY ? 0.f : m;
+        for (int p = 0; p < pieces; ++p) {
+          const float f = __builtin_amdgcn_exp2f(row[p].x - ref);
+          l = fmaf(row[p].y, f, l);
+          row[p].x = f;
+        }
+        sums[r] = make_float2(m, l);
       }
-      l = wave_sum(l);
-      if (lane == 0) sums[r] = make_float2(m, l);
+    } else {
+      for (int r = wave; r < n; r += NT / 64) {
+        float2* row = ml + r * pieces;
+        float m = -INFINITY, l = 0.f;
+        for (int p = lane; p < pieces; p += 64) m = fmaxf(m, row[p].x);
+        m = wave_max(m);
+        const float ref = m == -INFINITY ? 0.f : m;
+        for (int p = lane; p < pieces; p += 64) {
+          const float f = __builtin_amdgcn_exp2f(row[p].x - ref);
+          l = fmaf(row[p].y, f, l);
+          row[p].x = f;
+        }
+        l = wave_sum(l);
+        if (lane == 0) sums[r] = make_float2(m, l);
+      }
     }
     __syncthreads();
-    // elements (row, pair of channels); where they are few, the pieces are shared by several threads
-    const int items = n * HALF, share = max(1, NT / items);
-    for (int x0 = 0; x0 < items; x0 += NT) {
-      const int x = share > 1 ? tid % items : x0 + tid, part_of = share > 1 ? tid / items : 0;
+    const auto finish = [&](int x, float2 o) {                     // element x: a row and a pair of its channels
+      const int r = x / HALF, c = x % HALF;
+      int token, head;
+      row_of(r0 + r, &token, &head);
+      store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
+      store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
+    };
+    const int items = n * HALF;
+    if (items <= NT) {                                             // few elements: the pieces are shared by several threads
+      const int share = NT / items, x = tid % items, first = tid / items;
       float2 o = make_float2(0.f, 0.f);
-      if (x < items && part_of < share) {
+      if (first < share) {
         const int r = x / HALF, c = x % HALF;
-        for (int p0 = part_of; p0 < pieces; p0 += share * BATCH) {
+        for (int p0 = first; p0 < pieces; p0 += share * BATCH) {
           float2 v[BATCH];
 #pragma unroll
           for (int k = 0; k < BATCH; ++k) v[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + (r0 + r) * D + c * 2);
@@ -80,21 +101,43 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
           }
         }
       }
-      if (share > 1) {
-        part[tid] = o;
-        __syncthreads();
-        if (part_of == 0)
-          for (int k = 1; k < share; ++k) {
-            o.x += part[k * items + x].x;
-            o.y += part[k * items + x].y;
-          }
+      part[tid] = o;
+      __syncthreads();
+      if (first == 0) {
+        for (int k = 1; k < share; ++k) {
+          o.x += part[k * items + x].x;
+          o.y += part[k * items + x].y;
+        }
+        finish(x, o);
       }
-      if (x < items && part_of == 0) {
-        const int r = x / HALF, c = x % HALF;
-        int token, head;
-        row_of(r0 + r, &token, &head);
-        store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
-        store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
+    } else {                                                       // many: several elements of two pieces at a time
+      for (int x0 = tid; x0 < items; x0 += NT * BATCH) {
+        float2 o[BATCH];
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) o[k] = make_float2(0.f, 0.f);
+        for (int p = 0; p < pieces; p += 2) {
+          const int p1 = min(p + 1, pieces - 1);
+          float2 a[BATCH], b[BATCH];
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) {
+            const int x = min(x0 + k * NT, items - 1);
+            a[k] = load_pair(slot(p) + r0 * D + x * 2);
+            b[k] = load_pair(slot(p1) + r0 * D + x * 2);
+          }
+#pragma unroll
+          for (int k = 0; k < BATCH; ++k) {
+            const int r = min(x0 + k * NT, items - 1) / HALF;
+            const float f = ml[r * pieces + p].x, h = ml[r * pieces + p1].x;
+            o[k].x = fmaf(a[k].x, f, o[k].x);
+            o[k].y = fmaf(a[k].y, f, o[k].y);
+            if (p1 == p) continue;
+            o[k].x = fmaf(b[k].x, h, o[k].x);
+            o[k].y = fmaf(b[k].y, h, o[k].y);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+          if (x0 + k * NT < items) finish(x0 + k * NT, o[k]);
       }
     }
   }
@@ -169,7 +212,8 @@ struct Piece {
     *head = h * g.G + r - i * g.G;
   }
 };
-__device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, int64_t x) {
+// hint: the planned item before (-1: none); set to this one
+__device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, int64_t x, int* hint) {
   Piece p;
   p.h = (int)(x / sh.per_head);
   const int64_t y = x - p.h * sh.per_head;
@@ -179,12 +223,20 @@ __device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, i
     p.s = f.s; p.seq = f.index; p.tile = 0;
     before = f.before;
   } else {
-    int a = 0, b = sh.count - 1;           // first item whose end is past y
-    while (a < b) {
-      const int c = (a + b) / 2;
-      if (g.plan_end[c] > y) b = c;
-      else a = c + 1;
+    int a = y == 0 ? 0 : *hint + 1;        // the next one; to begin with, 64 ends at a time, the first item whose end is past y
+    if (*hint < 0 && y > 0) {
+      int n = sh.count, step = 1;          // among items [a, a + n)
+      a = 0;
+      while (n > 1) {
+        step = (n + 63) / 64;
+        const int at = a + min(((int)(threadIdx.x & 63) + 1) * step, n) - 1;
+        const uint64_t past = __ballot(g.plan_end[at] > y);
+        const int k = __builtin_ctzll(past);
+        n = min(step, n - k * step);
+        a += k * step;
+      }
     }
+    *hint = a;
     const int2 it = g.plan_item[a];
     p.seq = it.x; p.tile = it.y;
     before = a > 0 ? g.plan_end[a - 1] : 0;

@@ -239,7 +239,7 @@ struct WaveAttend {
 
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
 template <typename T, int D, int RT>
-constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads)); }
+constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
 
 // Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
 template <typename T, int D, int RT, typename Emit>
@@ -330,8 +330,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g
   const int w = blockIdx.x;
   const Share sh = share_of(g, w, 1);
   Wave at;
+  int hint = -1;
   for (int64_t x = sh.begin; x < sh.end;) {
-    const Piece p = piece_at(g, sh, x);
+    const Piece p = piece_at(g, sh, x, &hint);
     const PagedSeq s = p.s;
     const ItemRange it = p.it;
     const int h = p.h, j = p.tile, seq = p.seq;

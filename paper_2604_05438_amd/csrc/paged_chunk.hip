@@ -40,6 +40,7 @@ struct ChunkTile {
   static constexpr int ROWS = 1024 / RB;                           // rows that one load of a wavefront covers
   static constexpr int LOADS = kWaveTokens / ROWS;                 // loads per wavefront of K, and of V
 };
+static_assert(join_lds(kChunkThreads, kChunkRows) <= 65536, "");
 static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 16, "");
 
 // UNIFORM: 16 tokens always lie in one page
@@ -82,8 +83,9 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
 
   const int w = share_number(blockIdx.x, gridDim.x);
   const Share sh = share_of(g, w, 4);
+  int hint = -1;
   for (int64_t x = sh.begin; x < sh.end;) {
-    const Piece p = piece_at(g, sh, x);
+    const Piece p = piece_at(g, sh, x, &hint);
     const PagedSeq s = p.s;
     const ItemRange it = p.it;
     const int t0 = it.begin + p.u0 * kChunkTokens, t1 = min(it.begin + p.u1 * kChunkTokens, it.end);
