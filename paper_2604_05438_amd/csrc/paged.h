@@ -13,6 +13,10 @@ constexpr int kMaxSplit = 1024;           // workgroups that the work of one att
 constexpr int kBlockRowGroup = 512;       // query tokens whose block scores the workspace holds at once, at most
 constexpr int kMaxKept = 1024;            // blocks a query sees, at most
 
+// Workgroups of the split kernel that a CU holds (by their registers); the work is cut into as many pieces as the GPU's 256 CUs hold, so that
+// none waits for another to end: with 768 pieces where 256 ran at once the last ones ended three times later.
+constexpr int attend_per_cu(int d, int row_tiles) { return d == 128 && row_tiles == 2 ? 1 : 2; }
+
 // Everything a kernel needs to know of one call, passed by value.
 struct PagedGeom {
   int Hq, Hkv, G, d, dtype;

@@ -96,7 +96,7 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   g->unit = chunk ? 64 : kPagedThreads / 64 * (g->dtype == TKPHI_BF16 ? 32 : 16);
   g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * g->tiles);
   const int64_t units = (int64_t)g->n_seqs * g->tiles * g->Hkv * up(std::max(g->max_len, 1), g->unit);      // at most
-  g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? kChunkSplit : 768));
+  g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? kChunkSplit : 256 * attend_per_cu(g->d, g->tile_rows / 16)));
 }
 
 void plan_blocks(const tkphi_paged_config* c, PagedGeom* g) {

@@ -34,7 +34,7 @@ static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
 // of one row took 30 us, and one of 2 pieces of 256 rows as much.
 template <typename T, int D, int NT, typename Slot, typename RowOf>
 __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
-  constexpr int HALF = D / 2, BATCH = 8;
+  constexpr int HALF = D / 2, BATCH = 8, WIDE = 16;
   float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
   float2* part = ml + kJoinPairs;                                  // [threads]
   float2* sums = part + NT;                                        // [rows]: m, l of the whole
@@ -42,6 +42,15 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
   const int group = min(rows, kJoinPairs / pieces);
   for (int r0 = 0; r0 < rows; r0 += group) {
     const int n = min(group, rows - r0);
+    const int items = n * HALF;
+    // few elements: the pieces are shared by several threads, and the first loads go out at once
+    const int share = max(1, NT / items), first = tid / items;
+    const bool few = items <= NT && first < share;
+    float2 fv[WIDE];
+    if (few) {
+#pragma unroll
+      for (int k = 0; k < WIDE; ++k) fv[k] = load_pair(slot(min(first + k * share, pieces - 1)) + r0 * D + tid % items * 2);
+    }
     __syncthreads();
     for (int x = tid; x < n * pieces; x += NT) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
     __syncthreads();
@@ -82,25 +91,23 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
       store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
       store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
     };
-    const int items = n * HALF;
-    if (items <= NT) {                                             // few elements: the pieces are shared by several threads
-      const int share = NT / items, x = tid % items, first = tid / items;
+    if (items <= NT) {
+      const int x = tid % items, r = x / HALF;
       float2 o = make_float2(0.f, 0.f);
-      if (first < share) {
-        const int r = x / HALF, c = x % HALF;
-        for (int p0 = first; p0 < pieces; p0 += share * BATCH) {
-          float2 v[BATCH];
+      if (few)
+        for (int p0 = first;;) {
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k) v[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + (r0 + r) * D + c * 2);
-#pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
+          for (int k = 0; k < WIDE; ++k) {
             if (p0 + k * share >= pieces) continue;
             const float f = ml[r * pieces + p0 + k * share].x;
-            o.x = fmaf(v[k].x, f, o.x);
-            o.y = fmaf(v[k].y, f, o.y);
+            o.x = fmaf(fv[k].x, f, o.x);
+            o.y = fmaf(fv[k].y, f, o.y);
           }
+          p0 += share * WIDE;
+          if (p0 >= pieces) break;
+#pragma unroll
+          for (int k = 0; k < WIDE; ++k) fv[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + r0 * D + x * 2);
         }
-      }
       part[tid] = o;
       __syncthreads();
       if (first == 0) {
@@ -176,25 +183,57 @@ __device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& i
 __device__ __forceinline__ int share_number(int b, int n) { return n % 8 == 0 ? b % 8 * (n / 8) + b / 8 : b; }
 
 // The work of a call in order: KV heads outermost, then items, then units of an item.  Workgroup w of W takes the units
-// [all w / W, all (w + 1) / W).
+// [all w / W, all (w + 1) / W).  (Divisions of 64-bit numbers take 0.3 us each, and here they are all in a row: none where the numbers are small.)
 struct Share {
-  int64_t per_head, all, W, begin, end;    // units of a KV head, of all; workgroups; this one's
+  int64_t per_head, all, begin, end;       // units of a KV head, of all; this workgroup's
+  int64_t each;                            // all / W
+  int W, rest;                             // workgroups; all % W
   int count;                               // planned items
+  PagedSeq s;                              // without a plan, for up to 64 sequences: the lane's, its units, and up to with it
+  int units, units_incl;
+  __device__ __forceinline__ int64_t first_of(int w) const { return each * w + (int64_t)((uint32_t)(rest * w) / (uint32_t)W); }
+  // the workgroup of a unit: the last w with first_of(w) <= unit
+  __device__ __forceinline__ int owner(int64_t unit) const {
+    int w = min((int)((float)unit * ((float)W / (float)all)), W - 1);
+    while (w > 0 && first_of(w) > unit) --w;
+    while (w + 1 < W && first_of(w + 1) <= unit) ++w;
+    return w;
+  }
 };
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return a >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);   // (0 <= a, 0 < b; b > a if b is the larger)
+}
+__device__ __forceinline__ int first_item_units(const PagedGeom& g, const PagedSeq& s) { return s.fresh > 0 ? item_units(g, item_range(g, s, 0)) : 0; }
 // least: units that a workgroup gets at least where there are more workgroups than that
 __device__ __forceinline__ Share share_of(const PagedGeom& g, int w, int least) {
   Share r;
   r.count = 0;
-  if (g.tiles == 1) {
-    r.per_head = find_seq(g, 0x7fffffff, [&](const PagedSeq& s) { return item_units(g, item_range(g, s, 0)); }).total;
-  } else {
+  r.s = PagedSeq{0, 0, 0};
+  r.units = r.units_incl = 0;
+  if (g.tiles > 1) {
     r.count = *g.plan_count;
     r.per_head = r.count > 0 ? g.plan_end[r.count - 1] : 0;
+  } else if (g.n_seqs <= 64) {
+    const int lane = threadIdx.x & 63;
+    if (lane < g.n_seqs) {
+      r.s = check_seq(g, g.seqs[lane]);
+      r.units = first_item_units(g, r.s);
+    }
+    r.units_incl = wave_scan_incl(r.units);
+    r.per_head = __builtin_amdgcn_readlane(r.units_incl, 63);
+  } else {
+    r.per_head = find_seq(g, 0x7fffffff, [&](const PagedSeq& s) { return first_item_units(g, s); }).total;
   }
   r.all = r.per_head * g.Hkv;
-  r.W = min((int64_t)g.splits, (r.all + least - 1) / least);
-  r.begin = w < r.W ? r.all * w / r.W : 0;
-  r.end = w < r.W ? r.all * (w + 1) / r.W : 0;
+  r.W = (int)min((int64_t)g.splits, (r.all + least - 1) / least);
+  r.begin = r.end = r.each = 0;
+  r.rest = 0;
+  if (w < r.W) {
+    r.each = quotient(r.all, r.W);
+    r.rest = (int)(r.all - r.each * r.W);
+    r.begin = r.first_of(w);
+    r.end = r.first_of(w + 1);
+  }
   return r;
 }
 
@@ -215,14 +254,10 @@ struct Piece {
 // hint: the planned item before (-1: none); set to this one
 __device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, int64_t x, int* hint) {
   Piece p;
-  p.h = (int)(x / sh.per_head);
+  p.h = __builtin_amdgcn_readfirstlane((int)quotient(x, sh.per_head));
   const int64_t y = x - p.h * sh.per_head;
   int64_t before;
-  if (g.tiles == 1) {
-    const FoundSeq f = find_seq(g, (int)y, [&](const PagedSeq& s) { return item_units(g, item_range(g, s, 0)); });
-    p.s = f.s; p.seq = f.index; p.tile = 0;
-    before = f.before;
-  } else {
+  if (g.tiles > 1) {
     int a = y == 0 ? 0 : *hint + 1;        // the next one; to begin with, 64 ends at a time, the first item whose end is past y
     if (*hint < 0 && y > 0) {
       int n = sh.count, step = 1;          // among items [a, a + n)
@@ -241,6 +276,17 @@ __device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, i
     p.seq = it.x; p.tile = it.y;
     before = a > 0 ? g.plan_end[a - 1] : 0;
     p.s = check_seq(g, g.seqs[p.seq]);
+  } else if (g.n_seqs <= 64) {
+    p.seq = __builtin_ctzll(__ballot((int64_t)sh.units_incl > y));
+    p.tile = 0;
+    p.s.cached = __builtin_amdgcn_readlane(sh.s.cached, p.seq);
+    p.s.fresh = __builtin_amdgcn_readlane(sh.s.fresh, p.seq);
+    p.s.row = __builtin_amdgcn_readlane(sh.s.row, p.seq);
+    before = __builtin_amdgcn_readlane(sh.units_incl - sh.units, p.seq);
+  } else {
+    const FoundSeq f = find_seq(g, (int)y, [&](const PagedSeq& s) { return first_item_units(g, s); });
+    p.s = f.s; p.seq = f.index; p.tile = 0;
+    before = f.before;
   }
   p.it = item_range(g, p.s, p.tile);
   p.units = item_units(g, p.it);
@@ -257,11 +303,9 @@ __device__ __forceinline__ float* partial_slot(const PagedGeom& g, int w, bool f
 // After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.
 template <typename T, int D, int NT>
 __device__ __forceinline__ void finish_item(const PagedGeom& g, const Share& sh, const Piece& p, char* lds, int* sh_last) {
-  // the workgroup of a unit is the last w with all w / W <= unit
-  const auto owner = [&](int64_t unit) { return (int)(((unit + 1) * sh.W + sh.all - 1) / sh.all) - 1; };
-  const int w0 = owner(p.item0), w1 = owner(p.item1 - 1);
+  const int w0 = sh.owner(p.item0), w1 = sh.owner(p.item1 - 1);
   if (!last_to_arrive(g.arrived + w0, w1 - w0 + 1, sh_last)) return;
-  const bool first = sh.all * w0 / sh.W == p.item0;       // the first workgroup's share starts with this item
+  const bool first = sh.first_of(w0) == p.item0;          // the first workgroup's share starts with this item
   join_pieces<T, D, NT>(g, w1 - w0 + 1, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
                     [&](int row, int* token, int* head) { p.place(g, row, token, head); });
 }

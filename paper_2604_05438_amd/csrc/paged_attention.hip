@@ -320,7 +320,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
 }
 
 template <typename T, int D, int RT>
-__global__ __launch_bounds__(kPagedThreads) void paged_attend_kernel(PagedGeom g) {
+__global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
   using Wave = WaveAttend<T, D, RT>;
   constexpr int WAVES = kPagedThreads / 64;
   __shared__ __align__(16) char lds[attend_lds<T, D, RT>()];
