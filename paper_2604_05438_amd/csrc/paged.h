@@ -17,37 +17,57 @@ constexpr int kMaxKept = 1024;            // blocks a query sees, at most
 // none waits for another to end: with 768 pieces where 256 ran at once the last ones ended three times later.
 constexpr int attend_per_cu(int d, int row_tiles) { return d == 128 && row_tiles == 2 ? 1 : 2; }
 
+// n / d by a multiplication, for 0 <= n < 2^31: with 2^(l-1) < d <= 2^l, ceil(2^(31 + l) / d) fits 32 bits and is exact there
+struct Divisor {
+  int d;
+  uint32_t mul, shift;
+  void set(int value) {
+    int l = 0;
+    while ((1ll << l) < value) ++l;
+    d = value;
+    mul = (uint32_t)((((uint64_t)1 << (31 + l)) + value - 1) / value);
+    shift = 31 + l;
+  }
+#ifdef __HIPCC__
+  __host__ __device__ __forceinline__ int operator()(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+#endif
+};
+
 // Everything a kernel needs to know of one call, passed by value.
 struct PagedGeom {
-  int Hq, Hkv, G, d, dtype;
-  int page;                               // tokens per page
-  uint32_t page_mul, page_shift;          // t / page = (t * page_mul) >> page_shift for 0 <= t < 2^31
-  int64_t st_page, st_head, st_tok;       // bytes
-  int window, rot, adjacent, block, first, last, top;
-  int n_pages, n_seqs, max_pages, rows, max_new, max_len;
-  float scale, scale2, scale2_lo;         // score scale; scale log2(e) as the sum of two floats
   const int4* seqs;
   const int32_t* pages;
-  char *K, *V, *M;
-  const char *q, *k, *v;
+  char *K, *V;
+  const char* q;
   char* out;                              // q_rot or out
-  float* lse;
-  const double* inv_freq;
-  int64_t q_row, q_head, k_row, k_head, v_row, v_head, out_row, out_head;   // bytes
+  int64_t st_page, st_head, st_tok;       // bytes
+  int64_t q_row, q_head, out_row, out_head;
   uint32_t* status;
+  float* lse;
   // attention: the work of all items (sequence x tile of query rows x KV head) in units of a fixed number of tokens is
-  // cut into `splits` equal pieces, one per workgroup
-  int splits;
-  int unit;                               // tokens
-  int tile_rows;                          // query rows per item
-  int tiles;                              // most items of one sequence and KV head (1: no plan, every workgroup sums the units itself)
+  // cut into `splits` equal shares, one per workgroup
   uint32_t* arrived;                      // [splits] or [row group][Hkv]: pieces of a split item that are done; zero between calls
   float* partial;                         // [splits][2][tile_rows][d + 2]
+  int n_pages, n_seqs, max_pages, rows, max_new, max_len;
+  int Hkv, G, Hq, d;
+  Divisor by_page, by_group;              // tokens per page; G
+  int window, splits;
+  int unit_shift;                         // log2 of the tokens
+  int tile_rows;                          // query rows per item
+  float scale2, scale2_lo;                // score scale times log2(e), as the sum of two floats
+  // the plan: items in order, where there are more than one per sequence and KV head, or many sequences
   int64_t* plan_end;                      // [items]: units up to and with this item
   int2* plan_item;                        // (sequence, tile)
   int* plan_count;
-  int plan_room;                          // items the plan has room for
+  int plan_room;                          // items the plan has room for; 0: none needed
+  // append
+  int dtype, rot, adjacent;
+  const char *k, *v;
+  const double* inv_freq;
+  int64_t k_row, k_head, v_row, v_head;
   // blocks
+  char* M;
+  int block, first, last, top;
   int row0, row_group;                    // query tokens of this launch
   int max_blocks, kept;                   // bounds
   uint64_t* keys;                         // [row group][Hkv][max_blocks] order-preserving keys of the block scores; 0: not to be retrieved
@@ -62,9 +82,7 @@ void launch_block_select(const PagedGeom& g, hipStream_t s);
 void launch_block_attention(const PagedGeom& g, hipStream_t s);
 
 #ifdef __HIPCC__
-__device__ __forceinline__ int page_of(const PagedGeom& g, int t) {
-  return (int)(((uint64_t)(uint32_t)t * g.page_mul) >> g.page_shift);
-}
+__device__ __forceinline__ int page_of(const PagedGeom& g, int t) { return g.by_page(t); }
 
 // A sequence as the kernels take it: new_tokens 0 if its description is out of bounds.
 struct PagedSeq {
@@ -79,13 +97,21 @@ __device__ __forceinline__ PagedSeq check_seq(const PagedGeom& g, int4 w) {
   }
   return s;
 }
-// page id of entry p of sequence i, -1 if absent
+// Page id of entry p of sequence i, -1 if absent (also behind the table's end); *bad: whether it is no page id
+__device__ __forceinline__ int page_id(const PagedGeom& g, int i, int p, bool* bad) {
+  const int id = g.pages[(int64_t)i * g.max_pages + min(p, g.max_pages - 1)];
+  const bool there = p < g.max_pages, valid = (uint32_t)id < (uint32_t)g.n_pages;
+  *bad = *bad || (there && !valid && id != -1);
+  return there && valid ? id : -1;
+}
+__device__ __forceinline__ void report_pages(const PagedGeom& g, bool bad) {
+  if (__any(bad) && (threadIdx.x & 63) == 0) atomicOr(g.status, TKPHI_DEV_BAD_PAGE);
+}
 __device__ __forceinline__ int page_id(const PagedGeom& g, int i, int p) {
-  if (p >= g.max_pages) return -1;
-  const int id = g.pages[(int64_t)i * g.max_pages + p];
-  if ((uint32_t)id < (uint32_t)g.n_pages) return id;
-  if (id != -1) atomicOr(g.status, TKPHI_DEV_BAD_PAGE);
-  return -1;
+  bool bad = false;
+  const int id = page_id(g, i, p, &bad);
+  if (bad) atomicOr(g.status, TKPHI_DEV_BAD_PAGE);
+  return id;
 }
 
 // The sequence that owns unit x when sequence i has count(seq) units and they are numbered in order; wave-uniform, every wavefront by

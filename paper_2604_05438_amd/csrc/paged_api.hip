@@ -68,19 +68,14 @@ tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, Pag
   memset(g, 0, sizeof(*g));
   g->Hq = c->n_q_heads; g->Hkv = c->n_kv_heads; g->G = g->Hq / g->Hkv;
   g->d = c->d_head; g->dtype = c->kv_dtype;
-  g->page = c->page_tokens;
-  // t / page by a multiplication: with 2^(l-1) < page <= 2^l, ceil(2^(31 + l) / page) fits 32 bits and is exact below 2^31
-  int l = 0;
-  while ((1ll << l) < g->page) ++l;
-  g->page_mul = (uint32_t)((((uint64_t)1 << (31 + l)) + g->page - 1) / g->page);
-  g->page_shift = 31 + l;
+  g->by_page.set(c->page_tokens);
+  g->by_group.set(g->G);
   g->st_page = c->stride_page * es; g->st_head = c->stride_head * es; g->st_tok = c->stride_tok * es;
   g->window = c->window; g->rot = c->rot_dim; g->adjacent = c->rot_adjacent;
   g->block = c->block; g->first = c->first_blocks; g->last = c->last_blocks; g->top = c->top_blocks;
   g->n_seqs = st->n_seqs; g->max_pages = st->max_pages; g->rows = st->rows;
   g->max_new = std::min(st->max_new, st->rows); g->max_len = st->max_len;
   g->seqs = (const int4*)st->seqs; g->pages = st->pages;
-  g->scale = c->score_scale;
   const double s2 = (double)c->score_scale * 1.4426950408889634074;
   g->scale2 = (float)s2;
   g->scale2_lo = (float)(s2 - (double)g->scale2);
@@ -92,10 +87,11 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   const int64_t rows = (int64_t)g->max_new * g->G;
   const bool chunk = g->dtype == TKPHI_BF16 && rows > kPagedRows;
   g->tile_rows = chunk ? kChunkRows : rows <= 16 ? 16 : kPagedRows;
-  g->tiles = (int)std::max<int64_t>(1, up(rows, g->tile_rows));
-  g->unit = chunk ? 64 : kPagedThreads / 64 * (g->dtype == TKPHI_BF16 ? 32 : 16);
-  g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * g->tiles);
-  const int64_t units = (int64_t)g->n_seqs * g->tiles * g->Hkv * up(std::max(g->max_len, 1), g->unit);      // at most
+  const int64_t tiles = std::max<int64_t>(1, up(rows, g->tile_rows));
+  g->unit_shift = g->dtype == TKPHI_BF16 && !chunk ? 7 : 6;
+  const int64_t units = (int64_t)g->n_seqs * tiles * g->Hkv * up(std::max(g->max_len, 1), 1 << g->unit_shift);      // at most
+  if (chunk || tiles > 1 || g->n_seqs > 64 || units >= (1ll << 31))
+    g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * tiles);
   g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? kChunkSplit : 256 * attend_per_cu(g->d, g->tile_rows / 16)));
 }
 
@@ -117,7 +113,7 @@ PagedSpace space_of(const tkphi_paged_config* c, const PagedGeom& g0) {
   const int rg = std::min(g.rows, kBlockRowGroup);
   const int64_t heads = (int64_t)rg * g.Hkv;
   plan_attention(c, &g);
-  const int64_t items = g.tiles > 1 ? g.plan_room : 0;
+  const int64_t items = (int64_t)g.rows * g.G / 16 + g.n_seqs;        // (a plan is at most that long, whichever kernel runs)
   int64_t block_slots = 0;
   g.row_group = rg;
   plan_blocks(c, &g);
@@ -169,7 +165,8 @@ tkphi_status check_call(const tkphi_paged_config* c, const tkphi_step* st, const
   if (*empty) return TKPHI_OK;
   if (pool->n_pages < 1) { set_error("pool without pages"); return TKPHI_EINVAL; }
   if ((r = check_pointer(st->seqs, "seqs", 16)) != TKPHI_OK) return r;
-  if (st->max_pages > 0 && (r = check_pointer(st->pages, "pages", 4)) != TKPHI_OK) return r;
+  if (st->max_pages < 1) { set_error("page table without entries"); return TKPHI_EINVAL; }
+  if ((r = check_pointer(st->pages, "pages", 4)) != TKPHI_OK) return r;
   if ((r = check_pointer(pool->K, "K", 16)) != TKPHI_OK) return r;
   if ((r = check_pointer(pool->V, "V", 16)) != TKPHI_OK) return r;
   g->n_pages = pool->n_pages;

@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
 
   if (fills && lo > t0) {                                        // older keys of the block: one page
     const int pt = page_of(g, t0), id = page_id(g, f.index, pt);
-    const char* src = g.K + (int64_t)max(id, 0) * g.st_page + h * g.st_head + (int64_t)(t0 - pt * g.page) * g.st_tok;
+    const char* src = g.K + (int64_t)max(id, 0) * g.st_page + h * g.st_head + (int64_t)(t0 - pt * g.by_page.d) * g.st_tok;
     constexpr int PIECES = D / EPL;
     for (int i = tid; i < (lo - t0) * PIECES; i += kPagedThreads)
       *(u32x4*)(kept + (i / PIECES) * D + (i % PIECES) * EPL) = gload128(src + (int64_t)(i / PIECES) * g.st_tok + (i % PIECES) * 16);
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
       dst = g.out + (int64_t)(first_row + t) * g.out_row + (int64_t)(h * g.G + line) * g.out_head;
     } else {
       const int pt = page_of(g, lo + t), id = page_id(g, f.index, pt);
-      dst = id < 0 ? nullptr : (is_v ? g.V : g.K) + (int64_t)id * g.st_page + h * g.st_head + (int64_t)(lo + t - pt * g.page) * g.st_tok;
+      dst = id < 0 ? nullptr : (is_v ? g.V : g.K) + (int64_t)id * g.st_page + h * g.st_head + (int64_t)(lo + t - pt * g.by_page.d) * g.st_tok;
       if (id < 0) atomicOr(g.status, TKPHI_DEV_BAD_PAGE);
     }
     if (turns) {
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
   __syncthreads();
   const int pt = page_of(g, t0), id = page_id(g, f.index, pt);
   if (id < 0) return;
-  const int per = g.page / g.block, b = (t0 - pt * g.page) / g.block;
+  const int per = g.by_page.d / g.block, b = (t0 - pt * g.by_page.d) / g.block;
   for (int c = tid; c < D; c += kPagedThreads) {
     float sum = 0.f;
     for (int t = 0; t < tile; ++t) sum += Elem<T>::load1(kept, t * D + c);

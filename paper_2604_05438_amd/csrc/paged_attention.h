@@ -1,6 +1,8 @@
 // What the attention kernels on the paged cache share: items and their cut into pieces, outputs, partials and their joining.
 #pragma once
 
+#include <type_traits>
+
 #include "paged.h"
 
 namespace tkphi {
@@ -10,12 +12,12 @@ constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at o
 constexpr int join_lds(int threads, int rows) { return (kJoinPairs + threads + rows) * 8; }
 
 template <typename T>
-__device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float o, float m, float l) {
-  const float y = l == 0.f ? 0.f : o / l;                          // (l = 0: the row sees nothing)
-  char* dst = g.out + (int64_t)token_row * g.out_row + (int64_t)head * g.out_head;
-  if constexpr (sizeof(T) == 2) ((__bf16*)dst)[c] = (__bf16)y;
-  else ((float*)dst)[c] = y;
-  if (c == 0 && g.lse) g.lse[(int64_t)token_row * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+__device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float2 o, float m, float l) {
+  const float inv = l == 0.f ? 0.f : 1.f / l;                      // (l = 0: the row sees nothing, and o is 0)
+  char* dst = g.out + (int64_t)token_row * g.out_row + (int64_t)head * g.out_head + c * sizeof(T);
+  if constexpr (sizeof(T) == 2) *(__attribute__((address_space(1))) uint32_t*)dst = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)(o.x * inv), (__bf16)(o.y * inv)});
+  else *(__attribute__((address_space(1))) uint64_t*)dst = (uint64_t)__float_as_uint(o.y * inv) << 32 | __float_as_uint(o.x * inv);
+  if (c == 0 && g.lse) g.lse[(int64_t)token_row * g.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // A partial in memory: O [rows][D], then (m, l) [rows]; GPU-coherent accesses of 8 bytes
@@ -88,8 +90,7 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
       const int r = x / HALF, c = x % HALF;
       int token, head;
       row_of(r0 + r, &token, &head);
-      store_out<T>(g, token, head, 2 * c, o.x, sums[r].x, sums[r].y);
-      store_out<T>(g, token, head, 2 * c + 1, o.y, sums[r].x, sums[r].y);
+      store_out<T>(g, token, head, 2 * c, o, sums[r].x, sums[r].y);
     };
     if (items <= NT) {
       const int x = tid % items, r = x / HALF;
@@ -98,10 +99,10 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
         for (int p0 = first;;) {
 #pragma unroll
           for (int k = 0; k < WIDE; ++k) {
-            if (p0 + k * share >= pieces) continue;
-            const float f = ml[r * pieces + p0 + k * share].x;
-            o.x = fmaf(fv[k].x, f, o.x);
-            o.y = fmaf(fv[k].y, f, o.y);
+            const bool in = p0 + k * share < pieces;
+            const float f = ml[r * pieces + min(p0 + k * share, pieces - 1)].x;
+            o.x = fmaf(in ? fv[k].x : 0.f, f, o.x);
+            o.y = fmaf(in ? fv[k].y : 0.f, f, o.y);
           }
           p0 += share * WIDE;
           if (p0 >= pieces) break;
@@ -171,65 +172,67 @@ __device__ __forceinline__ ItemRange item_range(const PagedGeom& g, const PagedS
   ItemRange it;
   const int r0 = j * g.tile_rows;
   it.rows = min(g.tile_rows, s.fresh * g.G - r0);
-  const int i0 = r0 / g.G, i1 = (r0 + it.rows - 1) / g.G;
+  const int i0 = g.by_group(r0), i1 = g.by_group(r0 + it.rows - 1);
   it.end = s.cached + i1 + 1;
   it.low = g.window > 0 ? max(0, s.cached + i0 + 1 - g.window) : 0;
-  it.begin = it.low / g.unit * g.unit;
+  it.begin = it.low >> g.unit_shift << g.unit_shift;
   return it;
 }
-__device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& it) { return (it.end - it.begin + g.unit - 1) / g.unit; }
+__device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& it) { return (it.end - it.begin + (1 << g.unit_shift) - 1) >> g.unit_shift; }
 
 // Workgroup b of n -> its share's number: consecutive shares, which pass over the same KV head, on one XCD (workgroup b runs on XCD b % 8)
 __device__ __forceinline__ int share_number(int b, int n) { return n % 8 == 0 ? b % 8 * (n / 8) + b / 8 : b; }
 
-// The work of a call in order: KV heads outermost, then items, then units of an item.  Workgroup w of W takes the units
-// [all w / W, all (w + 1) / W).  (Divisions of 64-bit numbers take 0.3 us each, and here they are all in a row: none where the numbers are small.)
+// The work of a call in order: KV heads outermost, then items, then units of an item, in W equal shares (the first ones one unit longer).
+// PLAN: the items have been listed by paged_plan_kernel.  Otherwise there are at most 64 sequences of one item per KV head, a lane holds each,
+// and the numbers fit 32 bits: a launch over short contexts lasts as long as its longest chain of instructions and loads, and 64-bit divisions, searches
+// and loads one after another made 3 us of it.
+template <bool PLAN>
 struct Share {
-  int64_t per_head, all, begin, end;       // units of a KV head, of all; this workgroup's
-  int64_t each;                            // all / W
+  using Int = std::conditional_t<PLAN, int64_t, int>;
+  Int per_head, all, begin, end, each;     // units of a KV head, of all; this workgroup's; all / W
   int W, rest;                             // workgroups; all % W
   int count;                               // planned items
-  PagedSeq s;                              // without a plan, for up to 64 sequences: the lane's, its units, and up to with it
+  PagedSeq s;                              // (no plan) the lane's sequence, its units, and up to with it
   int units, units_incl;
-  __device__ __forceinline__ int64_t first_of(int w) const { return each * w + (int64_t)((uint32_t)(rest * w) / (uint32_t)W); }
-  // the workgroup of a unit: the last w with first_of(w) <= unit
-  __device__ __forceinline__ int owner(int64_t unit) const {
-    int w = min((int)((float)unit * ((float)W / (float)all)), W - 1);
-    while (w > 0 && first_of(w) > unit) --w;
-    while (w + 1 < W && first_of(w + 1) <= unit) ++w;
-    return w;
+  static __device__ __forceinline__ Int quotient(Int a, Int b) {
+    if constexpr (PLAN) {
+      if (a >> 32 || b >> 32) return a / b;
+    }
+    return (Int)((uint32_t)a / (uint32_t)b);
+  }
+  __device__ __forceinline__ Int first_of(int w) const { return each * w + min(w, rest); }
+  __device__ __forceinline__ int owner(Int unit) const {                // the workgroup whose share has this unit
+    const Int longer = (each + 1) * rest;
+    return __builtin_amdgcn_readfirstlane((int)(unit < longer ? quotient(unit, each + 1) : rest + quotient(unit - longer, each)));
   }
 };
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  return a >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);   // (0 <= a, 0 < b; b > a if b is the larger)
-}
-__device__ __forceinline__ int first_item_units(const PagedGeom& g, const PagedSeq& s) { return s.fresh > 0 ? item_units(g, item_range(g, s, 0)) : 0; }
 // least: units that a workgroup gets at least where there are more workgroups than that
-__device__ __forceinline__ Share share_of(const PagedGeom& g, int w, int least) {
-  Share r;
+template <bool PLAN>
+__device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w, int least) {
+  using Int = typename Share<PLAN>::Int;
+  Share<PLAN> r;
   r.count = 0;
   r.s = PagedSeq{0, 0, 0};
   r.units = r.units_incl = 0;
-  if (g.tiles > 1) {
+  if constexpr (PLAN) {
     r.count = *g.plan_count;
     r.per_head = r.count > 0 ? g.plan_end[r.count - 1] : 0;
-  } else if (g.n_seqs <= 64) {
+  } else {
     const int lane = threadIdx.x & 63;
     if (lane < g.n_seqs) {
       r.s = check_seq(g, g.seqs[lane]);
-      r.units = first_item_units(g, r.s);
+      r.units = r.s.fresh > 0 ? item_units(g, item_range(g, r.s, 0)) : 0;
     }
     r.units_incl = wave_scan_incl(r.units);
     r.per_head = __builtin_amdgcn_readlane(r.units_incl, 63);
-  } else {
-    r.per_head = find_seq(g, 0x7fffffff, [&](const PagedSeq& s) { return first_item_units(g, s); }).total;
   }
   r.all = r.per_head * g.Hkv;
-  r.W = (int)min((int64_t)g.splits, (r.all + least - 1) / least);
+  r.W = (int)min((Int)g.splits, least == 1 ? r.all : (r.all + least - 1) / least);
   r.begin = r.end = r.each = 0;
   r.rest = 0;
   if (w < r.W) {
-    r.each = quotient(r.all, r.W);
+    r.each = Share<PLAN>::quotient(r.all, r.W);
     r.rest = (int)(r.all - r.each * r.W);
     r.begin = r.first_of(w);
     r.end = r.first_of(w + 1);
@@ -238,26 +241,30 @@ __device__ __forceinline__ Share share_of(const PagedGeom& g, int w, int least) 
 }
 
 // The part of an item that unit x and those after it, up to the end of the share, belong to
+template <bool PLAN>
 struct Piece {
+  using Int = typename Share<PLAN>::Int;
   PagedSeq s;
   ItemRange it;
   int seq, tile, h;
   int u0, u1, units;                       // this piece's units of the item's
-  int64_t item0, item1;                    // the item's units among all
+  Int item0, item1;                        // the item's units among all
   __device__ __forceinline__ bool whole() const { return u0 == 0 && u1 == units; }
   __device__ __forceinline__ void place(const PagedGeom& g, int row, int* token, int* head) const {
-    const int r = tile * g.tile_rows + row, i = r / g.G;
+    const int r = (PLAN ? tile * g.tile_rows : 0) + row, i = g.by_group(r);
     *token = s.row + i;
     *head = h * g.G + r - i * g.G;
   }
 };
 // hint: the planned item before (-1: none); set to this one
-__device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, int64_t x, int* hint) {
-  Piece p;
-  p.h = __builtin_amdgcn_readfirstlane((int)quotient(x, sh.per_head));
-  const int64_t y = x - p.h * sh.per_head;
-  int64_t before;
-  if (g.tiles > 1) {
+template <bool PLAN>
+__device__ __forceinline__ Piece<PLAN> piece_at(const PagedGeom& g, const Share<PLAN>& sh, typename Share<PLAN>::Int x, int* hint) {
+  using Int = typename Share<PLAN>::Int;
+  Piece<PLAN> p;
+  p.h = __builtin_amdgcn_readfirstlane((int)Share<PLAN>::quotient(x, sh.per_head));
+  const Int y = x - p.h * sh.per_head;
+  Int before;
+  if constexpr (PLAN) {
     int a = y == 0 ? 0 : *hint + 1;        // the next one; to begin with, 64 ends at a time, the first item whose end is past y
     if (*hint < 0 && y > 0) {
       int n = sh.count, step = 1;          // among items [a, a + n)
@@ -273,24 +280,21 @@ __device__ __forceinline__ Piece piece_at(const PagedGeom& g, const Share& sh, i
     }
     *hint = a;
     const int2 it = g.plan_item[a];
-    p.seq = it.x; p.tile = it.y;
+    p.seq = __builtin_amdgcn_readfirstlane(it.x);
+    p.tile = __builtin_amdgcn_readfirstlane(it.y);
     before = a > 0 ? g.plan_end[a - 1] : 0;
     p.s = check_seq(g, g.seqs[p.seq]);
-  } else if (g.n_seqs <= 64) {
-    p.seq = __builtin_ctzll(__ballot((int64_t)sh.units_incl > y));
+  } else {
+    p.seq = __builtin_ctzll(__ballot(sh.units_incl > y));
     p.tile = 0;
     p.s.cached = __builtin_amdgcn_readlane(sh.s.cached, p.seq);
     p.s.fresh = __builtin_amdgcn_readlane(sh.s.fresh, p.seq);
     p.s.row = __builtin_amdgcn_readlane(sh.s.row, p.seq);
     before = __builtin_amdgcn_readlane(sh.units_incl - sh.units, p.seq);
-  } else {
-    const FoundSeq f = find_seq(g, (int)y, [&](const PagedSeq& s) { return first_item_units(g, s); });
-    p.s = f.s; p.seq = f.index; p.tile = 0;
-    before = f.before;
   }
   p.it = item_range(g, p.s, p.tile);
   p.units = item_units(g, p.it);
-  p.u0 = (int)(y - before);
+  p.u0 = __builtin_amdgcn_readfirstlane((int)(y - before));
   p.item0 = p.h * sh.per_head + before;
   p.item1 = p.item0 + p.units;
   p.u1 = (int)(min(sh.end, p.item1) - p.item0);
@@ -301,8 +305,8 @@ __device__ __forceinline__ float* partial_slot(const PagedGeom& g, int w, bool f
   return g.partial + ((int64_t)w * 2 + (first ? 0 : 1)) * g.tile_rows * (g.d + 2);
 }
 // After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.
-template <typename T, int D, int NT>
-__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share& sh, const Piece& p, char* lds, int* sh_last) {
+template <typename T, int D, int NT, bool PLAN>
+__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share<PLAN>& sh, const Piece<PLAN>& p, char* lds, int* sh_last) {
   const int w0 = sh.owner(p.item0), w1 = sh.owner(p.item1 - 1);
   if (!last_to_arrive(g.arrived + w0, w1 - w0 + 1, sh_last)) return;
   const bool first = sh.first_of(w0) == p.item0;          // the first workgroup's share starts with this item

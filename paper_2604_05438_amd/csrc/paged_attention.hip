@@ -278,48 +278,75 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, i
   }
 }
 
-// Where tiles > 1: the items in order with the running sum of their units, by one workgroup
-// (a sequence whose items would not fit, because sequences share rows, is skipped)
+// The items in order with the running sum of their units, by one workgroup.  (Items past the plan's room, as there are if sequences share
+// rows, are left out.)
 __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
-  __shared__ int64_t sums[16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t base = 0;
-  int first = 0;
-  for (int i = 0; i < g.n_seqs; ++i) {
-    const PagedSeq s = check_seq(g, g.seqs[i]);
-    const int tiles = s.fresh > 0 ? (int)(((int64_t)s.fresh * g.G + g.tile_rows - 1) / g.tile_rows) : 0;
-    if (first + tiles > g.plan_room) {
-      if (threadIdx.x == 0) atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
-      continue;
+  __shared__ int first[1025], sums[16];
+  __shared__ int64_t sums64[16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int items = 0;
+  for (int i0 = 0; i0 < g.n_seqs; i0 += 1024) {                    // 1024 sequences: where their items start, then all items at once
+    int tiles = 0;
+    if (i0 + tid < g.n_seqs) {
+      const PagedSeq s = check_seq(g, g.seqs[i0 + tid]);
+      tiles = s.fresh > 0 ? (s.fresh * g.G + g.tile_rows - 1) / g.tile_rows : 0;
     }
-    for (int j0 = 0; j0 < tiles; j0 += 1024) {
-      const int j = j0 + threadIdx.x;
-      const int u = j < tiles ? item_units(g, item_range(g, s, j)) : 0;
-      int64_t x = u;
-      for (int k = 1; k < 64; k *= 2) {
-        const int64_t y = __shfl_up(x, k);
-        if (lane >= k) x += y;
-      }
-      if (lane == 63) sums[wave] = x;
-      __syncthreads();
-      int64_t ahead = 0, all = 0;
-      for (int k = 0; k < 16; ++k) {
-        if (k < wave) ahead += sums[k];
-        all += sums[k];
-      }
-      __syncthreads();
-      if (j < tiles) {
-        g.plan_end[first + j] = base + ahead + x;
-        g.plan_item[first + j] = make_int2(i, j);
-      }
-      base += all;
+    const int x = wave_scan_incl(tiles);
+    if (lane == 63) sums[wave] = x;
+    __syncthreads();
+    int ahead = 0, all = 0;
+    for (int k = 0; k < 16; ++k) {
+      if (k < wave) ahead += sums[k];
+      all += sums[k];
     }
-    first += tiles;
+    first[tid + 1] = min(ahead + x, g.plan_room - items);
+    if (tid == 0) first[0] = 0;
+    __syncthreads();
+    if (items + all > g.plan_room) {
+      if (tid == 0) atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
+      all = g.plan_room - items;
+    }
+    for (int j = tid; j < all; j += 1024) {
+      int a = 0, b = min(1024, g.n_seqs - i0) - 1;                 // last sequence that starts at or before j (and has items)
+      while (a < b) {
+        const int c = (a + b + 1) / 2;
+        if (first[c] <= j) a = c;
+        else b = c - 1;
+      }
+      g.plan_item[items + j] = make_int2(i0 + a, j - first[a]);
+    }
+    items += all;
+    __syncthreads();
   }
-  if (threadIdx.x == 0) *g.plan_count = first;
+  __threadfence_block();
+  __syncthreads();
+  int64_t base = 0;
+  for (int j0 = 0; j0 < items; j0 += 1024) {
+    const int j = j0 + tid;
+    int64_t x = 0;
+    if (j < items) {
+      const int2 it = g.plan_item[j];
+      x = item_units(g, item_range(g, check_seq(g, g.seqs[it.x]), it.y));
+    }
+    for (int k = 1; k < 64; k *= 2) {
+      const int64_t y = __shfl_up(x, k);
+      if (lane >= k) x += y;
+    }
+    if (lane == 63) sums64[wave] = x;
+    __syncthreads();
+    int64_t ahead = 0, all = 0;
+    for (int k = 0; k < 16; ++k) {
+      if (k < wave) ahead += sums64[k];
+      all += sums64[k];
+    }
+    __syncthreads();
+    if (j < items) g.plan_end[j] = base + ahead + x;
+    base += all;
+  }
+  if (tid == 0) *g.plan_count = items;
 }
 
-template <typename T, int D, int RT>
+template <typename T, int D, int RT, bool PLAN>
 __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
   using Wave = WaveAttend<T, D, RT>;
   constexpr int WAVES = kPagedThreads / 64;
@@ -328,32 +355,34 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
   const int w = blockIdx.x;
-  const Share sh = share_of(g, w, 1);
+  const auto sh = share_of<PLAN>(g, w, 1);
   Wave at;
   int hint = -1;
-  for (int64_t x = sh.begin; x < sh.end;) {
-    const Piece p = piece_at(g, sh, x, &hint);
+  for (auto x = sh.begin; x < sh.end;) {
+    const auto p = piece_at<PLAN>(g, sh, x, &hint);
     const PagedSeq s = p.s;
     const ItemRange it = p.it;
-    const int h = p.h, j = p.tile, seq = p.seq;
-    const int t0 = it.begin + p.u0 * g.unit, t1 = min(it.begin + p.u1 * g.unit, it.end);
+    const int h = p.h, seq = p.seq;
+    const int t0 = it.begin + (p.u0 << g.unit_shift), t1 = min(it.begin + (p.u1 << g.unit_shift), it.end);
+    bool bad = false;
 
     // ---- this piece: tokens [t0, t1)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int row = j * g.tile_rows + rt * 16 + r;
       const bool live = rt * 16 + r < it.rows;
-      const int i = row / g.G, head = h * g.G + row - i * g.G;
+      int token, head;
+      p.place(g, rt * 16 + r, &token, &head);
+      const int i = token - s.row;
       at.lim[rt] = live ? s.cached + i : -1;
       at.low[rt] = live ? (g.window > 0 ? max(0, s.cached + i + 1 - g.window) : 0) : 1;
-      const char* src = g.q + (int64_t)(s.row + i) * g.q_row + (int64_t)head * g.q_head;
+      const char* src = g.q + (int64_t)token * g.q_row + (int64_t)head * g.q_head;
 #pragma unroll
       for (int f = 0; f < Wave::NF; ++f) {
         at.q[rt][f].u = (u32x4){0u, 0u, 0u, 0u};
         if (live) at.q[rt][f].u = gload128(src + f * 64 + kg * 16);
       }
     }
-    const int seen_all = s.cached + j * g.tile_rows / g.G;         // last token that every row sees
+    const int seen_all = s.cached + (PLAN ? g.by_group(p.tile * g.tile_rows) : 0);         // last token that every row sees
     const int low_all = g.window > 0 ? it.end - g.window : 0;      // first one (rows of no query may come out as they like)
     at.reset();
     const int tiles = (t1 - t0 + Wave::TOK - 1) / Wave::TOK, mine = (tiles - wave + WAVES - 1) / WAVES;
@@ -364,8 +393,8 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
 #pragma unroll
              for (int u = 0; u < Wave::SUB; ++u) {
                const int t = tile0(i) + u * 16 + r, pt = page_of(g, t);
-               const int id = t >= it.low && t < t1 ? page_id(g, seq, pt) : -1;
-               rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.page) * g.st_tok;
+               const int id = t >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
+               rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
                rows.pos[u] = id >= 0 ? t : -1;
              }
              return rows;
@@ -379,14 +408,14 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
       if (whole) {
         int token, head;
         p.place(g, row, &token, &head);
-        store_out<T>(g, token, head, c, o.x, m, l);
-        store_out<T>(g, token, head, c + 1, o.y, m, l);
+        store_out<T>(g, token, head, c, o, m, l);
       } else {
         store_pair(slot + row * D + c, o.x, o.y);
         if (c == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     });
-    if (!whole) finish_item<T, D, kPagedThreads>(g, sh, p, lds, &sh_last);
+    report_pages(g, bad);
+    if (!whole) finish_item<T, D, kPagedThreads, PLAN>(g, sh, p, lds, &sh_last);
     __syncthreads();
     x = min(sh.end, p.item1);
   }
@@ -419,7 +448,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
     if (r < g.G) at.q[0][f].u = gload128(src + f * 64 + kg * 16);
   }
   at.reset();
-  const int per = g.page / g.block;
+  const int per = g.by_page.d / g.block;
   const auto tile_slot = [&](int i) { return (a + wave + i * WAVES) * Wave::TOK; };
   at.run(g, h, lds + wave * Wave::LDS, (b - a - wave + WAVES - 1) / WAVES,
          [&](int i) {
@@ -445,8 +474,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   float* slot = part + (int64_t)piece * 16 * (D + 2);
   join_waves<T, D, 1>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
-      store_out<T>(g, token, h * g.G + row, c, o.x, m, l);
-      store_out<T>(g, token, h * g.G + row, c + 1, o.y, m, l);
+      store_out<T>(g, token, h * g.G + row, c, o, m, l);
     } else {
       store_pair(slot + row * D + c, o.x, o.y);
       if (c == 0) store_pair(slot + 16 * D + row * 2, m, l);
@@ -457,12 +485,17 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
                       [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
 }
 
+template <typename T, int D, int RT>
+static void launch_split(const PagedGeom& g, hipStream_t s) {
+  if (g.plan_room) hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  else hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, false>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+}
 template <typename T, int D>
 static void launch_attend(const PagedGeom& g, hipStream_t s) {
-  if (g.tiles > 1) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, s, g);
+  if (g.plan_room) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, s, g);
   if (g.tile_rows == kChunkRows) launch_paged_chunk(g, s);
-  else if (g.tile_rows <= 16) hipLaunchKernelGGL((paged_attend_kernel<T, D, 1>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
-  else hipLaunchKernelGGL((paged_attend_kernel<T, D, 2>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  else if (g.tile_rows <= 16) launch_split<T, D, 1>(g, s);
+  else launch_split<T, D, 2>(g, s);
 }
 void launch_paged_attention(const PagedGeom& g, hipStream_t s) {
   if (g.dtype == TKPHI_BF16) {

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_score_kernel(PagedGeom g,
   if (have <= g.kept) return;                                      // it sees all of them
   const int lo = max(g.first, (int)blockIdx.x * blocks_per_wg), hi = min(have - g.last, ((int)blockIdx.x + 1) * blocks_per_wg);
   if (lo >= hi) return;
-  const int part = tid % kScoreLanes, per = g.page / g.block;
+  const int part = tid % kScoreLanes, per = g.by_page.d / g.block;
   uint64_t* keys = g.keys + ((int64_t)local * g.Hkv + h) * g.max_blocks;
   bool staged = false;
   for (int b0 = lo; b0 < hi; b0 += kScoreBlocks) {
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(kSelThreads) void block_select_kernel(PagedGeom g) 
     if (tid == 0) g.list_head[at] = make_int4(0, 0, 0, 0);
     return;
   }
-  const int pos = f.s.cached + token - f.s.row, have = pos / g.block + 1, per = g.page / g.block;
+  const int pos = f.s.cached + token - f.s.row, have = pos / g.block + 1, per = g.by_page.d / g.block;
   const int lo = g.first, hi = have - g.last, n = hi - lo;         // blocks [lo, hi) compete
   const bool all = have <= g.kept;
   const uint64_t* keys = g.keys + at * g.max_blocks + lo;

@@ -82,10 +82,10 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
   }
 
   const int w = share_number(blockIdx.x, gridDim.x);
-  const Share sh = share_of(g, w, 4);
+  const Share<true> sh = share_of<true>(g, w, 4);
   int hint = -1;
   for (int64_t x = sh.begin; x < sh.end;) {
-    const Piece p = piece_at(g, sh, x, &hint);
+    const Piece<true> p = piece_at<true>(g, sh, x, &hint);
     const PagedSeq s = p.s;
     const ItemRange it = p.it;
     const int t0 = it.begin + p.u0 * kChunkTokens, t1 = min(it.begin + p.u1 * kChunkTokens, it.end);
@@ -113,11 +113,11 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
 
     const char* const Kh = g.K + p.h * g.st_head;
     const char* const Vh = g.V + p.h * g.st_head;
-    const int seen_first = s.cached + p.tile * g.tile_rows / g.G;  // limit of the workgroup's first row
+    const int seen_first = s.cached + g.by_group(p.tile * g.tile_rows);  // limit of the workgroup's first row
     const int low_last = g.window > 0 ? it.end - g.window : 0;     // first token that its last row sees
 
     // Stretches of the piece whose part of the page table fits LDS
-    const int stretch = (int)min((int64_t)16384, (int64_t)(kPageCache - 2) * g.page / kChunkTokens * kChunkTokens);
+    const int stretch = (int)min((int64_t)16384, (int64_t)(kPageCache - 2) * g.by_page.d / kChunkTokens * kChunkTokens);
     for (int ts = t0; ts < t1; ts += stretch) {
     const int te = min(ts + stretch, t1), n = (te - ts + kTileTokens - 1) / kTileTokens;
     const int page0 = page_of(g, ts), page_lo = page_of(g, max(ts, it.low)), page_hi = page_of(g, te - 1);
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         const int pt = page_of(g, tw);
         const int id = present ? __builtin_amdgcn_readfirstlane(sh_page[pt - page0]) : -1;
         if (id < 0) present = 0;
-        const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(tw - pt * g.page) * g.st_tok;
+        const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(tw - pt * g.by_page.d) * g.st_tok;
 #pragma unroll
         for (int k = 0; k < Tile::LOADS; ++k) load_to_lds16(Kh + at, kat[k], kdst + k * 1024);
 #pragma unroll
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         for (int k = 0; k < Tile::LOADS; ++k) {
           const int r = k * Tile::ROWS + lrow, t = tw + r, pt = page_of(g, t);
           const int id = (present >> r) & 1 ? sh_page[pt - page0] : -1;
-          const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.page) * g.st_tok;
+          const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
           load_to_lds16(Kh + at + kat[k], kdst + k * 1024);
           load_to_lds16(Vh + at + vat[k], vdst + k * 1024);
           const uint64_t there = __ballot(id >= 0);
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
           const float weight = __uint_as_float(slot & 1 ? word & 0xffff0000u : word << 16);
           if (!((present >> slot) & 1)) continue;
           const int pt = page_of(g, t), id = max(page_id(g, p.seq, pt), 0);
-          const uint16_t* v = (const uint16_t*)(g.V + (int64_t)id * g.st_page + p.h * g.st_head + (int64_t)(t - pt * g.page) * g.st_tok);
+          const uint16_t* v = (const uint16_t*)(g.V + (int64_t)id * g.st_page + p.h * g.st_head + (int64_t)(t - pt * g.by_page.d) * g.st_tok);
           const bool sees = t <= lim && t >= low;
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
             v[1] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)y[2], (__bf16)y[3]});
             *(__attribute__((address_space(1))) pc_u32x2*)(dst + (32 * ct + 8 * a + 4 * hi) * 2) = v;
           }
-        if (hi == 0 && g.lse) g.lse[(int64_t)token * g.Hq + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        if (hi == 0 && g.lse) g.lse[(int64_t)token * g.Hq + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
       } else {
         float* slot = partial_slot(g, w, x == sh.begin);
 #pragma unroll
@@ -348,13 +348,13 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         if (hi == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     }
-    if (!whole) finish_item<uint16_t, D, kChunkThreads>(g, sh, p, lds, &sh_last);
+    if (!whole) finish_item<uint16_t, D, kChunkThreads, true>(g, sh, p, lds, &sh_last);
     x = min(sh.end, p.item1);
   }
 }
 
 void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
-  const bool uniform = g.page % kWaveTokens == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
+  const bool uniform = g.by_page.d % kWaveTokens == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
   if (g.d == 64) {
     if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<64, true>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
     else hipLaunchKernelGGL((paged_chunk_kernel<64, false>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);

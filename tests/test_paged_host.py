@@ -39,7 +39,7 @@ EVERY = [
     ("ESHAPE", dict(cfg__block=8)), ("ESHAPE", dict(cfg__block=64)), ("EINVAL", dict(cfg__first_blocks=-1)), ("EINVAL", dict(cfg__top_blocks=2000)),
     ("EINVAL", dict(cfg__workgroups=5000)), ("EINVAL", dict(step__n_seqs=-1)), ("ESHAPE", dict(step__n_seqs=70000)), ("EINVAL", dict(step__rows=-1)),
     ("EINVAL", dict(step__reserved=1)), ("ESHAPE", dict(step__n_seqs=60000, step__max_len=1 << 30)), ("EINVAL", dict(step__seqs=0)), ("EALIGN", dict(step__seqs=4100)),
-    ("EINVAL", dict(step__pages=0)), ("EALIGN", dict(step__pages=4098)), ("EINVAL", dict(pool__K=0)), ("EALIGN", dict(pool__V=8200)),
+    ("EINVAL", dict(step__pages=0)), ("EINVAL", dict(step__max_pages=0)), ("EALIGN", dict(step__pages=4098)), ("EINVAL", dict(pool__K=0)), ("EALIGN", dict(pool__V=8200)),
     ("EINVAL", dict(pool__n_pages=0)), ("EINVAL", dict(pool__n_pages=-3)), ("EINVAL", dict(pool__reserved=1)),
 ]
 
