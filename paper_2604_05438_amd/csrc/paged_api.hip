@@ -54,6 +54,7 @@ tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, Pag
     return TKPHI_EINVAL;
   }
   if (c->workgroups < 0 || c->workgroups > kMaxSplit) { set_error("workgroups=%d outside [0, %d]", c->workgroups, kMaxSplit); return TKPHI_EINVAL; }
+  if (c->block > 0 && c->stride_tok * es >= (1ll << 28)) { set_error("stride_tok=%lld too large for blocks", (long long)c->stride_tok); return TKPHI_ESHAPE; }
   for (const int32_t r : c->reserved)
     if (r != 0) { set_error("reserved words of the config must be 0"); return TKPHI_EINVAL; }
   if (st->n_seqs < 0 || st->rows < 0 || st->max_new < 0 || st->max_len < 0 || st->max_pages < 0 || st->reserved != 0) {

@@ -9,7 +9,7 @@ namespace tkphi {
 
 constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
-constexpr int join_lds(int threads, int rows) { return (kJoinPairs + threads + rows) * 8; }
+constexpr int join_lds(int threads, int rows) { return (kJoinPairs + rows) * 8 > threads * 16 ? (kJoinPairs + rows) * 8 : threads * 16; }
 
 template <typename T>
 __device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float2 o, float m, float l) {
@@ -36,23 +36,67 @@ static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
 // of one row took 30 us, and one of 2 pieces of 256 rows as much.
 template <typename T, int D, int NT, typename Slot, typename RowOf>
 __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
-  constexpr int HALF = D / 2, BATCH = 8, WIDE = 16;
-  float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
-  float2* part = ml + kJoinPairs;                                  // [threads]
-  float2* sums = part + NT;                                        // [rows]: m, l of the whole
+  constexpr int HALF = D / 2, BATCH = 8;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const auto finish = [&](int r, int c, float2 o, float m, float l) {          // channels c, c + 1 of row r
+    int token, head;
+    row_of(r, &token, &head);
+    store_out<T>(g, token, head, c, o, m, l);
+  };
+  // Few elements (pairs of channels): several threads share the pieces of one; each of them gets along with one round of loads, (m, l) among them
+  if (rows * HALF <= NT) {
+    constexpr int WIDE = 16;
+    const int items = rows * HALF, share = NT / items, x = tid % items, mine = tid / items, r = x / HALF, c = x % HALF * 2;
+    float4* part = (float4*)lds;
+    __syncthreads();
+    float m = -INFINITY, l = 0.f;
+    float2 o = make_float2(0.f, 0.f);
+    if (mine < share)
+      for (int p0 = mine; p0 < pieces; p0 += share * WIDE) {
+        float2 v[WIDE], ml[WIDE];
+#pragma unroll
+        for (int k = 0; k < WIDE; ++k) {
+          const float* at = slot(min(p0 + k * share, pieces - 1));
+          v[k] = load_pair(at + r * D + c);
+          ml[k] = load_pair(at + stride * D + r * 2);
+        }
+        float mb = m;
+#pragma unroll
+        for (int k = 0; k < WIDE; ++k) mb = fmaxf(mb, ml[k].x);      // (the last one again past the end)
+        const float ref = mb == -INFINITY ? 0.f : mb, fix = __builtin_amdgcn_exp2f(m - ref);
+        m = mb;
+        l *= fix; o.x *= fix; o.y *= fix;
+#pragma unroll
+        for (int k = 0; k < WIDE; ++k) {
+          const bool in = p0 + k * share < pieces;
+          const float f = __builtin_amdgcn_exp2f(ml[k].x - ref);
+          l = fmaf(in ? ml[k].y : 0.f, f, l);
+          o.x = fmaf(in ? v[k].x : 0.f, f, o.x);
+          o.y = fmaf(in ? v[k].y : 0.f, f, o.y);
+        }
+      }
+    part[tid] = make_float4(m, l, o.x, o.y);
+    __syncthreads();
+    if (mine == 0) {
+      for (int k = 1; k < share; ++k) {
+        const float4 other = part[k * items + x];
+        const float mb = fmaxf(m, other.x), ref = mb == -INFINITY ? 0.f : mb;
+        const float f = __builtin_amdgcn_exp2f(m - ref), h = __builtin_amdgcn_exp2f(other.x - ref);
+        m = mb;
+        l = fmaf(other.y, h, l * f);
+        o.x = fmaf(other.z, h, o.x * f);
+        o.y = fmaf(other.w, h, o.y * f);
+      }
+      finish(r, c, o, m, l);
+    }
+    return;
+  }
+  float2* ml = (float2*)lds;                                       // [rows][pieces]: (m, l), then (weight, -)
+  float2* sums = ml + kJoinPairs;                                  // [rows]: m, l of the whole
   const int group = min(rows, kJoinPairs / pieces);
   for (int r0 = 0; r0 < rows; r0 += group) {
     const int n = min(group, rows - r0);
     const int items = n * HALF;
-    // few elements: the pieces are shared by several threads, and the first loads go out at once
-    const int share = max(1, NT / items), first = tid / items;
-    const bool few = items <= NT && first < share;
-    float2 fv[WIDE];
-    if (few) {
-#pragma unroll
-      for (int k = 0; k < WIDE; ++k) fv[k] = load_pair(slot(min(first + k * share, pieces - 1)) + r0 * D + tid % items * 2);
-    }
     __syncthreads();
     for (int x = tid; x < n * pieces; x += NT) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
     __syncthreads();
@@ -86,39 +130,7 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
       }
     }
     __syncthreads();
-    const auto finish = [&](int x, float2 o) {                     // element x: a row and a pair of its channels
-      const int r = x / HALF, c = x % HALF;
-      int token, head;
-      row_of(r0 + r, &token, &head);
-      store_out<T>(g, token, head, 2 * c, o, sums[r].x, sums[r].y);
-    };
-    if (items <= NT) {
-      const int x = tid % items, r = x / HALF;
-      float2 o = make_float2(0.f, 0.f);
-      if (few)
-        for (int p0 = first;;) {
-#pragma unroll
-          for (int k = 0; k < WIDE; ++k) {
-            const bool in = p0 + k * share < pieces;
-            const float f = ml[r * pieces + min(p0 + k * share, pieces - 1)].x;
-            o.x = fmaf(in ? fv[k].x : 0.f, f, o.x);
-            o.y = fmaf(in ? fv[k].y : 0.f, f, o.y);
-          }
-          p0 += share * WIDE;
-          if (p0 >= pieces) break;
-#pragma unroll
-          for (int k = 0; k < WIDE; ++k) fv[k] = load_pair(slot(min(p0 + k * share, pieces - 1)) + r0 * D + x * 2);
-        }
-      part[tid] = o;
-      __syncthreads();
-      if (first == 0) {
-        for (int k = 1; k < share; ++k) {
-          o.x += part[k * items + x].x;
-          o.y += part[k * items + x].y;
-        }
-        finish(x, o);
-      }
-    } else {                                                       // many: several elements of two pieces at a time
+    // several elements of two pieces at a time
       for (int x0 = tid; x0 < items; x0 += NT * BATCH) {
         float2 o[BATCH];
 #pragma unroll
@@ -145,9 +157,11 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
         }
 #pragma unroll
         for (int k = 0; k < BATCH; ++k)
-          if (x0 + k * NT < items) finish(x0 + k * NT, o[k]);
+          if (x0 + k * NT < items) {
+            const int x = x0 + k * NT, r = x / HALF;
+            finish(r0 + r, x % HALF * 2, o[k], sums[r].x, sums[r].y);
+          }
       }
-    }
   }
 }
 

@@ -26,8 +26,11 @@ __device__ __forceinline__ pa_u32x2 lds_read_transposed(const char* p) {
 }
 
 // One wavefront's share of an item piece.
-// T, D: storage, head dimension; RT: tiles of 16 query rows
-template <typename T, int D, int RT>
+// T, D: storage, head dimension; RT: tiles of 16 query rows; STREAM: the cache is read once (non-temporal loads)
+// A load instruction covers 8 rows x 128 bytes, whole cache lines: lane (r, kg) takes 16 bytes of row r mod 8, in the first half of its line for
+// r < 8, in the second for r >= 8.  Keys of 16 rows then change places between two registers to make plain operands; values go to LDS anyway.
+// (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of LINES_TBS.)
+template <typename T, int D, int RT, bool STREAM>
 struct WaveAttend {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int RB = D * (int)sizeof(T);                   // bytes of a row
@@ -53,19 +56,40 @@ struct WaveAttend {
     }
   }
 
-  // The cached rows that a lane loads of a tile (slots lane & 15, + 16): byte offset, and the token's position; a position < 0 is seen by
-  // nobody (its offset is readable all the same).
-  struct Rows {
-    int64_t off[SUB];
-    int pos[SUB];
-  };
+  static constexpr int GR = TOK / 8;                              // groups of 8 tokens per tile
 
-  __device__ __forceinline__ void load(const char* base, const Rows& r, PagedFrag (&f)[SUB][NF]) {
-    const int kg = (threadIdx.x >> 4) & 3;
+  // The cached rows of a tile: byte offset of the lane's row of each group of 8, the position of the group's first token, and which of
+  // its tokens anyone may see (the rows of the others are readable all the same).
+  struct Rows {
+    int64_t off[GR];
+    int pos[GR], mask[GR];
+  };
+  static __device__ __forceinline__ int lane_offset() { return ((threadIdx.x >> 3) & 1) * 64 + ((threadIdx.x >> 4) & 3) * 16; }
+
+  // `at`: what the lane adds to the groups' offsets
+  __device__ __forceinline__ void load(const char* base, uint32_t at, const Rows& r, PagedFrag (&f)[SUB][NF]) {
 #pragma unroll
     for (int s = 0; s < SUB; ++s)
 #pragma unroll
-      for (int j = 0; j < NF; ++j) f[s][j].u = gload128(base + r.off[s] + kg * 16 + j * 64);
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int j = 0; j < NF / 2; ++j) {
+          const char* p = base + r.off[2 * s + u] + at + j * 128;
+          f[s][2 * j + u].u = STREAM ? gload128_stream(p) : gload128(p);
+        }
+  }
+
+  // the operands of 16 rows out of what two groups loaded: lanes 8 .. 15 of each row of 16 of the one <-> lanes 0 .. 7 of the other
+  static __device__ __forceinline__ void to_operands(PagedFrag (&f)[NF]) {
+#pragma unroll
+    for (int j = 0; j < NF; j += 2) {
+      const PagedFrag a = f[j], b = f[j + 1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        f[j].u[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)a.u[e], (int)b.u[e], 0x128, 0xf, 0xc, false);
+        f[j + 1].u[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)b.u[e], (int)a.u[e], 0x128, 0xf, 0x3, false);
+      }
+    }
   }
 
   __device__ __forceinline__ pa_floatx4 score(const PagedFrag (&k)[NF], const PagedFrag (&qq)[NF]) {
@@ -105,13 +129,15 @@ struct WaveAttend {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         for (int k = 0; k < 4; ++k) {
-          const int slot = 4 * k + e, pos = __shfl(rows.pos[u], slot);
+          const int slot = 4 * k + e, in = slot & 7;
+          const int pos = (k >> 1 ? rows.pos[2 * u + 1] : rows.pos[2 * u]) + in;
+          const bool there = ((k >> 1 ? rows.mask[2 * u + 1] : rows.mask[2 * u]) >> in) & 1;
           const char* v = vlds + (u * 16 + slot) * VROW;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
             const uint32_t word = __shfl(p[rt][0].u[BF ? 2 * u + e / 2 : e], 16 * k + r);
             const float weight = __uint_as_float(!BF ? word : e & 1 ? word & 0xffff0000u : word << 16);
-            if (pos < low[rt] || pos > lim[rt]) continue;
+            if (!there || pos < low[rt] || pos > lim[rt]) continue;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -120,17 +146,18 @@ struct WaveAttend {
         }
   }
 
-  // rows_of(i): the lane's rows (slots lane & 15, + 16) of its tile i; tiles 0 .. n - 1.  clean(i): every row sees every token of tile i.
+  // rows_of(i): the rows of its tile i; tiles 0 .. n - 1.  clean(i): every row sees every token of tile i.  at: see load().
   template <typename RowsOf, typename Clean>
-  __device__ __forceinline__ void run(const PagedGeom& g, int h, char* vlds, int n, RowsOf&& rows_of, Clean&& clean) {
+  __device__ __forceinline__ void run(const PagedGeom& g, int h, char* vlds, int n, uint32_t lane_at, RowsOf&& rows_of, Clean&& clean) {
     if (n <= 0) return;
-    const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
+    const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, r7 = lane & 7;
     const char* Kb = g.K + h * g.st_head;
     const char* Vb = g.V + h * g.st_head;
+    char* const vw = vlds + r7 * VROW + lane_offset();
     PagedFrag kf[SUB][NF], vf[SUB][NF];
     Rows cur = rows_of(0);
-    load(Kb, cur, kf);
-    load(Vb, cur, vf);
+    load(Kb, lane_at, cur, kf);
+    load(Vb, lane_at, cur, vf);
     Rows nxt = rows_of(min(1, n - 1));
     for (int i = 0; i < n; ++i) {
       const Rows here = cur;
@@ -138,25 +165,28 @@ struct WaveAttend {
       // ---- scores
       pa_floatx4 s[SUB][RT];
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
+      for (int u = 0; u < SUB; ++u) {
+        to_operands(kf[u]);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[u][rt] = score(kf[u], q[rt]);
-      if (i + 1 < n) load(Kb, cur, kf);
+      }
+      if (i + 1 < n) load(Kb, lane_at, cur, kf);
       nxt = rows_of(min(i + 2, n - 1));
       // ---- what nobody may see
       bool all = clean(i);
 #pragma unroll
-      for (int u = 0; u < SUB; ++u) all = all && __ballot(here.pos[u] < 0) == 0ull;
+      for (int u = 0; u < GR; ++u) all = all && here.mask[u] == 0xff;
       if (!all) {
 #pragma unroll
-        for (int u = 0; u < SUB; ++u)
+        for (int u = 0; u < SUB; ++u) {
+          const int pos0 = (kg < 2 ? here.pos[2 * u] : here.pos[2 * u + 1]) + 4 * (kg & 1);
+          const int bits = (kg < 2 ? here.mask[2 * u] : here.mask[2 * u + 1]) >> (4 * (kg & 1));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int pos = __shfl(here.pos[u], 4 * kg + e);
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt)
-              if (pos < low[rt] || pos > lim[rt]) s[u][rt][e] = -INFINITY;
-          }
+              if (!((bits >> e) & 1) || pos0 + e < low[rt] || pos0 + e > lim[rt]) s[u][rt][e] = -INFINITY;
+        }
       }
       // ---- running maximum and sum
       PagedFrag p[RT][(SUB + 1) / 2];
@@ -198,17 +228,17 @@ struct WaveAttend {
       // ---- V through LDS; rows that nobody sees as zeros, whatever they hold
       bool odd = false;                                            // a value that is no number, or infinite, which some rows may not see
 #pragma unroll
-      for (int u = 0; u < SUB; ++u)
+      for (int u = 0; u < GR; ++u)
 #pragma unroll
-        for (int j = 0; j < NF; ++j) {
-          u32x4 w = vf[u][j].u;
+        for (int j = 0; j < NF / 2; ++j) {
+          u32x4 w = vf[u / 2][2 * j + u % 2].u;
           if (!all) {
-            if (here.pos[u] < 0) w = (u32x4){0u, 0u, 0u, 0u};
+            if (!((here.mask[u] >> r7) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
             odd = odd || not_finite(w);
           }
-          *(u32x4*)(vlds + (u * 16 + r) * VROW + kg * 16 + j * 64) = w;
+          *(u32x4*)(vw + u * 8 * VROW + j * 128) = w;
         }
-      if (i + 1 < n) load(Vb, cur, vf);
+      if (i + 1 < n) load(Vb, lane_at, cur, vf);
       if (!all && __ballot(odd)) {                                 // (0 times such a value is not 0: row by row, without what they do not see)
         add_seen(p, here, vlds);
         continue;
@@ -238,12 +268,12 @@ struct WaveAttend {
 };
 
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
-template <typename T, int D, int RT>
-constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
+template <typename T, int D, int RT, bool STREAM>
+constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT, STREAM>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
 
 // Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
-template <typename T, int D, int RT, typename Emit>
-__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT>& w, char* lds, int rows, Emit&& emit) {
+template <typename T, int D, int RT, bool STREAM, typename Emit>
+__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM>& w, char* lds, int rows, Emit&& emit) {
   constexpr int W = kPagedThreads / 64, R = 16 * RT, STR = D + 2;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = threadIdx.x >> 6;
   float* mine = (float*)lds + (size_t)wave * R * STR;
@@ -346,11 +376,13 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
   if (tid == 0) *g.plan_count = items;
 }
 
-template <typename T, int D, int RT, bool PLAN>
+// UNIFORM: 8 tokens always lie in one page
+template <typename T, int D, int RT, bool PLAN, bool UNIFORM>
 __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
-  using Wave = WaveAttend<T, D, RT>;
+  constexpr bool STREAM = !PLAN;                                   // (several items of a sequence read the same rows)
+  using Wave = WaveAttend<T, D, RT, STREAM>;
   constexpr int WAVES = kPagedThreads / 64;
-  __shared__ __align__(16) char lds[attend_lds<T, D, RT>()];
+  __shared__ __align__(16) char lds[attend_lds<T, D, RT, STREAM>()];
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
@@ -387,15 +419,31 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     at.reset();
     const int tiles = (t1 - t0 + Wave::TOK - 1) / Wave::TOK, mine = (tiles - wave + WAVES - 1) / WAVES;
     const auto tile0 = [&](int i) { return t0 + (wave + i * WAVES) * Wave::TOK; };
-    at.run(g, h, lds + wave * Wave::LDS, mine,
+    const uint32_t lane_at = Wave::lane_offset() + (UNIFORM ? (uint32_t)(lane & 7) * (uint32_t)g.st_tok : 0u);
+    at.run(g, h, lds + wave * Wave::LDS, mine, lane_at,
            [&](int i) {
              typename Wave::Rows rows;
+             const int tb = tile0(i);
+             if constexpr (UNIFORM) {                              // lane u < GR looks up the page of group u
+               const int t = tb + min(lane, Wave::GR - 1) * 8, pt = page_of(g, t);
+               const int id = t + 7 >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
 #pragma unroll
-             for (int u = 0; u < Wave::SUB; ++u) {
-               const int t = tile0(i) + u * 16 + r, pt = page_of(g, t);
-               const int id = t >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
-               rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
-               rows.pos[u] = id >= 0 ? t : -1;
+               for (int u = 0; u < Wave::GR; ++u) {
+                 const int tu = tb + u * 8, gid = __builtin_amdgcn_readlane(id, u), gp = __builtin_amdgcn_readlane(pt, u);
+                 const int from = max(it.low - tu, 0), to = min(t1 - tu, 8);                    // tokens [from, to) of the group
+                 rows.off[u] = (int64_t)max(gid, 0) * g.st_page + (int64_t)(tu - gp * g.by_page.d) * g.st_tok;
+                 rows.pos[u] = tu;
+                 rows.mask[u] = gid < 0 || from >= to ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
+               }
+             } else {
+#pragma unroll
+               for (int u = 0; u < Wave::GR; ++u) {
+                 const int t = tb + u * 8 + (lane & 7), pt = page_of(g, t);
+                 const int id = t >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
+                 rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
+                 rows.pos[u] = tb + u * 8;
+                 rows.mask[u] = (int)(__ballot(id >= 0) & 0xff);
+               }
              }
              return rows;
            },
@@ -404,7 +452,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     // ---- out, or a partial
     const bool whole = p.whole();
     float* slot = partial_slot(g, w, x == sh.begin);
-    join_waves<T, D, RT>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
+    join_waves<T, D, RT, STREAM>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
       if (whole) {
         int token, head;
         p.place(g, row, &token, &head);
@@ -424,9 +472,9 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
 // ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g) {
-  using Wave = WaveAttend<T, D, 1>;
+  using Wave = WaveAttend<T, D, 1, true>;
   constexpr int WAVES = kPagedThreads / 64;
-  __shared__ __align__(16) char lds[attend_lds<T, D, 1>()];
+  __shared__ __align__(16) char lds[attend_lds<T, D, 1, true>()];
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int h = blockIdx.y, local = blockIdx.z, token = g.row0 + local, split = blockIdx.x;
@@ -434,8 +482,8 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   const int4 head = g.list_head[at_list];                          // entries, position of the query, its sequence; 0 entries: a row of no sequence
   if (head.x <= 0) return;
   const int2* list = g.list + at_list * g.kept;
-  const int n = head.x * g.block;                                  // slots: listed blocks times tokens
-  const int tiles = (n + Wave::TOK - 1) / Wave::TOK;
+  const int slots = head.x * g.block;                              // listed blocks times tokens
+  const int tiles = (slots + Wave::TOK - 1) / Wave::TOK;
   const int a = (int)((int64_t)tiles * split / g.splits), b = (int)((int64_t)tiles * (split + 1) / g.splits);
 
   Wave at;
@@ -448,19 +496,21 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
     if (r < g.G) at.q[0][f].u = gload128(src + f * 64 + kg * 16);
   }
   at.reset();
-  const int per = g.by_page.d / g.block;
+  const int per = g.by_page.d / g.block, shift = 31 - __builtin_clz(g.block);          // (a power of two of at least 16 tokens, in one page)
   const auto tile_slot = [&](int i) { return (a + wave + i * WAVES) * Wave::TOK; };
-  at.run(g, h, lds + wave * Wave::LDS, (b - a - wave + WAVES - 1) / WAVES,
+  at.run(g, h, lds + wave * Wave::LDS, (b - a - wave + WAVES - 1) / WAVES, Wave::lane_offset() + (uint32_t)(lane & 7) * (uint32_t)g.st_tok,
          [&](int i) {
            typename Wave::Rows rows;
+           const int t0 = tile_slot(i), e = (t0 + min(lane, Wave::GR - 1) * 8) >> shift;
+           const int2 blk = list[min(e, head.x - 1)];              // lane u < GR: the block of group u
+           const int first = blk.y % per << shift;
 #pragma unroll
-           for (int u = 0; u < Wave::SUB; ++u) {
-             const int t = tile_slot(i) + u * 16 + r, e = t / g.block;
-             const int2 blk = e < head.x ? list[e] : make_int2(-1, 0);
-             const int in = t - e * g.block;                       // token of the block
-             rows.off[u] = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)(blk.y % per * g.block + in) * g.st_tok;
-             const int pos = blk.y * g.block + in;
-             rows.pos[u] = blk.x >= 0 && pos <= head.y ? pos : -1;
+           for (int u = 0; u < Wave::GR; ++u) {
+             const int in = (t0 + u * 8) & (g.block - 1), id = __builtin_amdgcn_readlane(blk.x, u);
+             const int pos = (__builtin_amdgcn_readlane(blk.y, u) << shift) + in, n = head.y + 1 - pos;         // tokens up to the query's own
+             rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(__builtin_amdgcn_readlane(first, u) + in) * g.st_tok;
+             rows.pos[u] = pos;
+             rows.mask[u] = id < 0 || n <= 0 || t0 + u * 8 >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
            }
            return rows;
          },
@@ -472,7 +522,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   if (a == b) return;
   const int piece = tiles < g.splits ? a : split;
   float* slot = part + (int64_t)piece * 16 * (D + 2);
-  join_waves<T, D, 1>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
+  join_waves<T, D, 1, true>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
       store_out<T>(g, token, h * g.G + row, c, o, m, l);
     } else {
@@ -487,8 +537,10 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
 
 template <typename T, int D, int RT>
 static void launch_split(const PagedGeom& g, hipStream_t s) {
-  if (g.plan_room) hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
-  else hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, false>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+  const bool uniform = g.by_page.d % 8 == 0 && g.st_tok < (1ll << 28);           // (offsets of 32 bits within 8 tokens)
+  const auto kernel = g.plan_room ? uniform ? paged_attend_kernel<T, D, RT, true, true> : paged_attend_kernel<T, D, RT, true, false>
+                                  : uniform ? paged_attend_kernel<T, D, RT, false, true> : paged_attend_kernel<T, D, RT, false, false>;
+  hipLaunchKernelGGL(kernel, dim3(g.splits), dim3(kPagedThreads), 0, s, g);
 }
 template <typename T, int D>
 static void launch_attend(const PagedGeom& g, hipStream_t s) {
