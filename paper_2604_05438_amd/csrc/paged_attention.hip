@@ -29,7 +29,7 @@ __device__ __forceinline__ pa_u32x2 lds_read_transposed(const char* p) {
 // T, D: storage, head dimension; RT: tiles of 16 query rows; STREAM: the cache is read once (non-temporal loads)
 // A load instruction covers 8 rows x 128 bytes, whole cache lines: lane (r, kg) takes 16 bytes of row r mod 8, in the first half of its line for
 // r < 8, in the second for r >= 8.  Keys of 16 rows then change places between two registers to make plain operands; values go to LDS anyway.
-// (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of LINES_TBS.)
+// (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of 6.5.)
 template <typename T, int D, int RT, bool STREAM>
 struct WaveAttend {
   static constexpr bool BF = sizeof(T) == 2;

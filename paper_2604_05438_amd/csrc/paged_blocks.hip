@@ -110,52 +110,42 @@ struct Edge {
   int ties;
 };
 
-// Up to kHeld keys per thread, thread t's k-th being number t + k kSelThreads: scores in 2048 bins of equal width between the lowest and the highest one
-// (a histogram of a leading digit would put nearly all of them into a few bins), then the exact order within the bin of the edge.
-// false: that bin holds more than fits, or there is no spread (the caller sorts digit by digit).
-constexpr int kHeld = 8, kBins2 = 2048;
+// Up to kHeld keys per thread, thread t's k-th being number t + k kSelThreads: a histogram over 32 octaves of the score by sign and five
+// bits each (of a leading digit nearly all would share a few bins), then the exact order within the bin of the edge.
+// false: that bin holds more than fits (the caller sorts digit by digit).
+constexpr int kHeld = 8, kScoreBins = 2048;
 struct HeldScratch {
-  uint32_t hist[kBins2];
+  uint32_t hist[kScoreBins];
   uint64_t cand[kSelThreads];
   int cand_at[kSelThreads];
   int scan[16];
-  float lo[16], hi[16];
   int bin, need, n_cand;
   Edge edge;
 };
-__device__ __forceinline__ float key_value(uint64_t key) {         // the score in 32 bits (rounding keeps the order), finite
-  const uint64_t b = key >> 63 ? key & 0x7fffffffffffffffull : ~key;
-  const float x = (float)__builtin_bit_cast(double, b);
-  return fminf(fmaxf(x, -1e38f), 1e38f);
+__device__ __forceinline__ int score_bin(uint64_t key) {           // monotone in the key
+  const bool pos = key >> 63;
+  const uint64_t mag = (pos ? key : ~key) & 0x7fffffffffffffffull;
+  const int e = (int)(mag >> 52) - (1023 - 16), m = (int)(mag >> 47) & 31;
+  const int b = e < 0 ? 0 : e > 31 ? 1023 : e * 32 + m;
+  return pos ? 1024 + b : 1023 - b;
 }
-__device__ __forceinline__ bool find_edge(const uint64_t (&key)[kHeld], int want, HeldScratch& sh, Edge* edge) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float lo = INFINITY, hi = -INFINITY, val[kHeld];
+// rounds: how many of the kHeld are in use
+__device__ __forceinline__ bool find_edge(const uint64_t (&key)[kHeld], int rounds, int want, HeldScratch& sh, Edge* edge) {
+  const int tid = threadIdx.x;
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
-    val[k] = key_value(key[k]);
-    if (key[k]) { lo = fminf(lo, val[k]); hi = fmaxf(hi, val[k]); }
-  }
-  lo = -wave_max(-lo);
-  hi = wave_max(hi);
-  if (lane == 0) { sh.lo[wave] = lo; sh.hi[wave] = hi; }
-#pragma unroll
-  for (int k = 0; k < kBins2 / kSelThreads; ++k) sh.hist[tid + k * kSelThreads] = 0;
+  for (int k = 0; k < kScoreBins / kSelThreads; ++k) sh.hist[tid + k * kSelThreads] = 0;
   if (tid == 0) sh.n_cand = 0;
   lds_barrier();
-  lo = -wave_max(lane < 16 ? -sh.lo[lane] : -INFINITY);
-  hi = wave_max(lane < 16 ? sh.hi[lane] : -INFINITY);
-  const float width = hi - lo, scale = (kBins2 - 1) / width;
-  if (!(width > 0.f) || !(scale < 1e38f)) return false;
   int bin[kHeld];
 #pragma unroll
   for (int k = 0; k < kHeld; ++k) {
-    bin[k] = min((int)((val[k] - lo) * scale), kBins2 - 1);        // (monotone in the score)
+    if (k >= rounds) break;
+    bin[k] = score_bin(key[k]);
     if (key[k]) atomicAdd(&sh.hist[bin[k]], 1u);
   }
   lds_barrier();
   // thread t looks at the two bins from the top: number of keys in the bins above
-  const int b1 = kBins2 - 1 - 2 * tid;
+  const int b1 = kScoreBins - 1 - 2 * tid;
   const int c1 = (int)sh.hist[b1], c0 = (int)sh.hist[b1 - 1];
   const int incl = sel_scan_incl(c0 + c1, sh.scan), above = incl - c0 - c1;
   if (above < want && want <= incl) {
@@ -163,16 +153,21 @@ __device__ __forceinline__ bool find_edge(const uint64_t (&key)[kHeld], int want
     sh.bin = first ? b1 : b1 - 1;
     sh.need = want - above - (first ? 0 : c1);
   }
+  if (tid == kSelThreads - 1 && incl <= want) sh.bin = -1;         // all of them
   lds_barrier();
-  const int edge_bin = sh.bin, need = sh.need, count = (int)sh.hist[edge_bin];
+  const int edge_bin = sh.bin, need = sh.need;
+  if (edge_bin < 0) return true;
+  const int count = (int)sh.hist[edge_bin];
   if (count > kSelThreads) return false;
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
+  for (int k = 0; k < kHeld; ++k) {
+    if (k >= rounds) break;
     if (key[k] && bin[k] == edge_bin) {
       const int at = atomicAdd(&sh.n_cand, 1);
       sh.cand[at] = key[k];
       sh.cand_at[at] = tid + k * kSelThreads;
     }
+  }
   lds_barrier();
   if (tid < count) {                                               // the need-th of the bin, equal keys by number
     const uint64_t mine = sh.cand[tid];
@@ -193,7 +188,7 @@ __device__ __forceinline__ bool find_edge(const uint64_t (&key)[kHeld], int want
 // One workgroup per query token and KV head: the blocks it sees, ascending
 __global__ __launch_bounds__(kSelThreads) void block_select_kernel(PagedGeom g) {
   __shared__ HeldScratch sh;
-  __shared__ int want_sh, counted[kHeld * 16 + 1];
+  __shared__ int want_sh, counted[kHeld * 16];
   __shared__ uint64_t prefix;
   const int h = blockIdx.x, local = blockIdx.y, token = g.row0 + local, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t at = (int64_t)local * g.Hkv + h;
@@ -207,32 +202,35 @@ __global__ __launch_bounds__(kSelThreads) void block_select_kernel(PagedGeom g) 
   const bool all = have <= g.kept;
   const uint64_t* keys = g.keys + at * g.max_blocks + lo;
   int2* list = g.list + at * g.kept;
-  Edge edge{1ull, 0x7fffffff};
+  Edge edge{1ull, 0x7fffffff};                                     // (all that are eligible)
   uint64_t key[kHeld];
+  int page[kHeld];
   const bool held = n <= kHeld * kSelThreads;
+  const int rounds = held ? (n + kSelThreads - 1) / kSelThreads : kHeld;
   if (!all) {
-    int eligible = 0;
     if (held) {
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
+        if (k >= rounds) break;
         const int j = tid + k * kSelThreads;
         key[k] = j < n && g.top > 0 ? keys[j] : 0ull;
+        page[k] = j < n ? page_id(g, f.index, (lo + j) / per) : -1;
       }
-#pragma unroll
-      for (int k = 0; k < kHeld; ++k) eligible += key[k] != 0ull;
-    } else if (g.top > 0) {
-      for (int j = tid; j < n; j += kSelThreads) eligible += keys[j] != 0ull;
     }
-    eligible = wave_sum(eligible);
-    if (lane == 0) counted[wave] = eligible;
-    lds_barrier();
-    eligible = wave_sum(lane < 16 ? counted[lane] : 0);
-    lds_barrier();
     if (g.top == 0) {
       edge = Edge{~0ull, 0};
-    } else if (eligible > g.top && !(held && find_edge(key, g.top, sh, &edge))) {
-      edge.key = radix_select_desc(n, g.top, [&](int j, uint64_t* v) { *v = keys[j]; return *v != 0ull; }, sh.hist, sh.scan, &prefix, &want_sh);
-      edge.ties = want_sh;
+    } else if (!(held && find_edge(key, rounds, g.top, sh, &edge))) {
+      int eligible = 0;
+      for (int j = tid; j < n; j += kSelThreads) eligible += keys[j] != 0ull;
+      eligible = wave_sum(eligible);
+      if (lane == 0) counted[wave] = eligible;
+      lds_barrier();
+      eligible = wave_sum(lane < 16 ? counted[lane] : 0);
+      lds_barrier();
+      if (eligible > g.top) {
+        edge.key = radix_select_desc(n, g.top, [&](int j, uint64_t* v) { *v = keys[j]; return *v != 0ull; }, sh.hist, sh.scan, &prefix, &want_sh);
+        edge.ties = want_sh;
+      }
     }
   }
   // Ascending list: first blocks, taken ones of [lo, hi), last blocks.  All blocks in order where it sees all.
@@ -246,22 +244,26 @@ __global__ __launch_bounds__(kSelThreads) void block_select_kernel(PagedGeom g) 
         for (int k = 0; k < kHeld; ++k) {
           const int j = j0 + tid + k * kSelThreads;
           key[k] = j < n ? keys[j] : 0ull;
+          page[k] = j < n ? page_id(g, f.index, (lo + j) / per) : -1;
         }
       }
       // how many wavefront w takes of its 64 k-th keys, and how many ties there are ahead
       uint64_t over[kHeld], tie[kHeld];
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
+        if (k >= rounds) break;
         over[k] = __ballot(key[k] > edge.key);
         tie[k] = __ballot(key[k] == edge.key && key[k] != 0ull);
         if (lane == 0) counted[k * 16 + wave] = __builtin_popcountll(over[k]) | __builtin_popcountll(tie[k]) << 16;
       }
       lds_barrier();
-      // prefix sums over the 128 counts (k, wavefront), two per lane; the ties' limit applies in order
-      const int a = counted[2 * lane], b = counted[2 * lane + 1];
+      // prefix sums over the counts (k, wavefront), two per lane; the ties' limit applies in order
+      const bool used = 2 * lane < 16 * rounds;
+      const int a = used ? counted[2 * lane] : 0, b = used ? counted[2 * lane + 1] : 0;
       const int o_incl = wave_scan_incl((a & 0xffff) + (b & 0xffff)), t_incl = wave_scan_incl((a >> 16) + (b >> 16));
 #pragma unroll
       for (int k = 0; k < kHeld; ++k) {
+        if (k >= rounds) break;
         const int c = k * 16 + wave, from = c >> 1;                // counts before c: of the lanes before, and of this lane's first
         const int pa = __builtin_amdgcn_readlane(a, from), pb = __builtin_amdgcn_readlane(b, from);
         const int o_before = __builtin_amdgcn_readlane(o_incl, from) - (pa & 0xffff) - (pb & 0xffff) + (c & 1 ? pa & 0xffff : 0);
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(kSelThreads) void block_select_kernel(PagedGeom g) 
         // taken ties ahead of this key: min(ties ahead, limit) less those before this sweep, which `count` has
         const int place = count + o_before + __builtin_popcountll(over[k] & below) + min(my_t, edge.ties) - min(equal, edge.ties);
         const int blk = lo + j0 + tid + k * kSelThreads;
-        if (take) list[place] = make_int2(page_id(g, f.index, blk / per), blk);
+        if (take) list[place] = make_int2(page[k], blk);
       }
       const int o_all = __builtin_amdgcn_readlane(o_incl, 63), t_all = __builtin_amdgcn_readlane(t_incl, 63);
       count += o_all + min(equal + t_all, edge.ties) - min(equal, edge.ties);
