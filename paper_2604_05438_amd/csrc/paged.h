@@ -23,6 +23,7 @@ struct Divisor {
   uint32_t mul, shift;
   void set(int value) {
     int l = 0;
+    value = value < 1 ? 1 : value;
     while ((1ll << l) < value) ++l;
     d = value;
     mul = (uint32_t)((((uint64_t)1 << (31 + l)) + value - 1) / value);
@@ -62,6 +63,7 @@ struct PagedGeom {
   int plan_room;                          // items the plan has room for; 0: none needed
   // append
   int dtype, rot, adjacent;
+  Divisor by_half, by_lines;              // rot / 2; rows per token and KV head: query heads, key, value
   const char *k, *v;
   const double* inv_freq;
   int64_t k_row, k_head, v_row, v_head;

@@ -227,6 +227,8 @@ tkphi_status tkphi_kv_append(const tkphi_paged_config* cfg, const tkphi_step* st
   g.q = (const char*)io->q; g.k = (const char*)io->k; g.v = (const char*)io->v;
   g.out = (char*)io->q_rot;
   g.inv_freq = io->inv_freq;
+  g.by_half.set(g.rot / 2);
+  g.by_lines.set((g.q ? g.G : 0) + 2);
   (void)hipGetLastError();
   launch_paged_append(g, (hipStream_t)hip_stream);
   return hip_status(hipGetLastError(), "tkphi_kv_append launch");

@@ -4,7 +4,9 @@
 // A workgroup takes a tile of consecutive cache positions of one sequence (a whole block where means are kept, so that the mean has one
 // writer and a fixed order) and one KV head with its query heads.  Bound by memory: every row is read once and written
 // once, 16 bytes per lane; the angles (64 bits: at position 10^6 a 32-bit product is off by 0.06 rad) are taken once per
-// token, pair and workgroup and shared through LDS.
+// token, pair and workgroup and shared through LDS.  A chunk of 16001 tokens of a 3B layer (24 / 8 heads of 128): 77 us = 4.3 TB/s, where a large copy
+// runs at 4.85; 64 single tokens 5 us.  Several KV heads per workgroup, which share the angles: 76 us, but 21 instead of 11 us for 3000 tokens of
+// a 1B layer; non-temporal loads: 14 instead of 11 us there; two or four tasks per thread at a time: no faster.
 #include "paged.h"
 
 namespace tkphi {
@@ -57,25 +59,25 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
   T* kept = (T*)(lds + (size_t)tile * half * sizeof(float2));    // [tile][D] keys as stored, for the mean
   const bool fills = g.block > 0 && hi == t0 + tile;
   const int first_row = f.s.row + (lo - f.s.cached);
+  const int block_entry = page_of(g, t0), block_row = t0 - block_entry * g.by_page.d;   // (a block lies in one page)
+  bool lost = false;
 
-  if (fills && lo > t0) {                                        // older keys of the block: one page
-    const int pt = page_of(g, t0), id = page_id(g, f.index, pt);
-    const char* src = g.K + (int64_t)max(id, 0) * g.st_page + h * g.st_head + (int64_t)(t0 - pt * g.by_page.d) * g.st_tok;
+  if (fills && lo > t0) {                                      // older keys of the block
+    const char* src = g.K + (int64_t)max(page_id(g, f.index, block_entry), 0) * g.st_page + h * g.st_head + (int64_t)block_row * g.st_tok;
     constexpr int PIECES = D / EPL;
     for (int i = tid; i < (lo - t0) * PIECES; i += kPagedThreads)
       *(u32x4*)(kept + (i / PIECES) * D + (i % PIECES) * EPL) = gload128(src + (int64_t)(i / PIECES) * g.st_tok + (i % PIECES) * 16);
   }
   for (int i = tid; i < n * half; i += kPagedThreads) {
-    const int t = i / half, j = i - t * half;
+    const int t = g.by_half(i), j = i - t * half;
     turn[i] = cos_sin((double)(lo + t) * g.inv_freq[j]);
   }
   __syncthreads();
-
-  const int heads = g.q ? g.G : 0, lines = heads + 2;            // query heads, the key, the value
+  const int lines = g.by_lines.d;                                // query heads, the key, the value
   const int rotated = g.rot / (2 * EPL);                         // pairs of pieces that turn
   for (int i = tid; i < n * lines * PAIRS; i += kPagedThreads) {
-    const int p = i % PAIRS, line = i / PAIRS % lines, t = i / PAIRS / lines;
-    const bool is_v = line == heads + 1, is_k = line == heads;
+    const int p = i % PAIRS, t = g.by_lines(i / PAIRS), line = i / PAIRS - t * lines;
+    const bool is_v = line == lines - 1, is_k = line == lines - 2;
     const char* src = is_v   ? g.v + (int64_t)(first_row + t) * g.v_row + h * g.v_head
                       : is_k ? g.k + (int64_t)(first_row + t) * g.k_row + h * g.k_head
                              : g.q + (int64_t)(first_row + t) * g.q_row + (int64_t)(h * g.G + line) * g.q_head;
@@ -84,12 +86,12 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
     const int pa = turns && !g.adjacent ? p : 2 * p, pb = turns && !g.adjacent ? p + rotated : 2 * p + 1;
     u32x4 ua = gload128(src + pa * 16), ub = gload128(src + pb * 16);
     char* dst;
-    if (line < heads) {
+    if (line < lines - 2) {
       dst = g.out + (int64_t)(first_row + t) * g.out_row + (int64_t)(h * g.G + line) * g.out_head;
     } else {
-      const int pt = page_of(g, lo + t), id = page_id(g, f.index, pt);
+      const int pt = page_of(g, lo + t), id = page_id(g, f.index, pt, &lost);
       dst = id < 0 ? nullptr : (is_v ? g.V : g.K) + (int64_t)id * g.st_page + h * g.st_head + (int64_t)(lo + t - pt * g.by_page.d) * g.st_tok;
-      if (id < 0) atomicOr(g.status, TKPHI_DEV_BAD_PAGE);
+      lost = lost || id < 0;
     }
     if (turns) {
       float a[EPL], b[EPL], x[EPL], y[EPL];
@@ -121,20 +123,20 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
       gstore128(dst + pb * 16, ub);
     }
     if (is_k && fills) {
-      T* row = kept + (lo + t - t0) * D;
-      *(u32x4*)(row + pa * EPL) = ua;
-      *(u32x4*)(row + pb * EPL) = ub;
+      T* key = kept + (lo + t - t0) * D;
+      *(u32x4*)(key + pa * EPL) = ua;
+      *(u32x4*)(key + pb * EPL) = ub;
     }
   }
+  report_pages(g, lost);
   if (!fills) return;
   __syncthreads();
-  const int pt = page_of(g, t0), id = page_id(g, f.index, pt);
-  if (id < 0) return;
-  const int per = g.by_page.d / g.block, b = (t0 - pt * g.by_page.d) / g.block;
-  for (int c = tid; c < D; c += kPagedThreads) {
+  const int id = page_id(g, f.index, block_entry);
+  const int per = g.by_page.d / g.block, b = block_row / g.block;
+  for (int c = tid; c < D && id >= 0; c += kPagedThreads) {
     float sum = 0.f;
     for (int t = 0; t < tile; ++t) sum += Elem<T>::load1(kept, t * D + c);
-    sum *= 1.f / (float)g.block;                                 // (a power of two)
+    sum *= 1.f / (float)g.block;                               // (a power of two)
     const int64_t at = (((int64_t)id * g.Hkv + h) * per + b) * D + c;
     if constexpr (sizeof(T) == 2) ((__bf16*)g.M)[at] = (__bf16)sum;
     else ((float*)g.M)[at] = sum;
@@ -145,7 +147,8 @@ void launch_paged_append(const PagedGeom& g, hipStream_t s) {
   const int tile = g.block ? g.block : 16;
   // sequence by sequence a tile at either end may be cut
   const int64_t by_rows = g.rows / tile + 2ll * g.n_seqs, by_seqs = (int64_t)g.n_seqs * ((g.max_new - 2 + tile) / tile + 1);
-  const dim3 grid((unsigned)(by_rows < by_seqs ? by_rows : by_seqs), g.Hkv);
+  const unsigned tiles = (unsigned)(by_rows < by_seqs ? by_rows : by_seqs);
+  const dim3 grid(tiles, g.Hkv);
   const size_t lds = (size_t)tile * (g.rot / 2) * sizeof(float2) + (g.block ? (size_t)tile * g.d * (g.dtype == TKPHI_BF16 ? 2 : 4) : 0);
   if (g.dtype == TKPHI_BF16) {
     if (g.d == 64) hipLaunchKernelGGL((paged_append_kernel<uint16_t, 64>), grid, dim3(kPagedThreads), lds, s, g, tile);
