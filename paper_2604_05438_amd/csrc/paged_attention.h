@@ -197,6 +197,12 @@ __device__ __forceinline__ int item_units(const PagedGeom& g, const ItemRange& i
 // Workgroup b of n -> its share's number: consecutive shares, which pass over the same KV head, on one XCD (workgroup b runs on XCD b % 8)
 __device__ __forceinline__ int share_number(int b, int n) { return n % 8 == 0 ? b % 8 * (n / 8) + b / 8 : b; }
 
+// A value that is the same in every lane, in scalar registers (what is loaded arrives in vector registers, and would stay there)
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x) | (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32;
+}
+
 // The work of a call in order: KV heads outermost, then items, then units of an item, in W equal shares (the first ones one unit longer).
 // PLAN: the items have been listed by paged_plan_kernel.  Otherwise there are at most 64 sequences of one item per KV head, a lane holds each,
 // and the numbers fit 32 bits: a launch over short contexts lasts as long as its longest chain of instructions and loads, and 64-bit divisions, searches
@@ -230,8 +236,8 @@ __device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w, int l
   r.s = PagedSeq{0, 0, 0};
   r.units = r.units_incl = 0;
   if constexpr (PLAN) {
-    r.count = *g.plan_count;
-    r.per_head = r.count > 0 ? g.plan_end[r.count - 1] : 0;
+    r.count = uniform(*g.plan_count);
+    r.per_head = r.count > 0 ? uniform(g.plan_end[r.count - 1]) : 0;
   } else {
     const int lane = threadIdx.x & 63;
     if (lane < g.n_seqs) {
@@ -246,7 +252,7 @@ __device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w, int l
   r.begin = r.end = r.each = 0;
   r.rest = 0;
   if (w < r.W) {
-    r.each = Share<PLAN>::quotient(r.all, r.W);
+    r.each = uniform(Share<PLAN>::quotient(r.all, r.W));
     r.rest = (int)(r.all - r.each * r.W);
     r.begin = r.first_of(w);
     r.end = r.first_of(w + 1);
@@ -279,7 +285,7 @@ __device__ __forceinline__ Piece<PLAN> piece_at(const PagedGeom& g, const Share<
   const Int y = x - p.h * sh.per_head;
   Int before;
   if constexpr (PLAN) {
-    int a = y == 0 ? 0 : *hint + 1;        // the next one; to begin with, 64 ends at a time, the first item whose end is past y
+    int a = uniform(y == 0 ? 0 : *hint + 1);        // the next one; to begin with, 64 ends at a time, the first item whose end is past y
     if (*hint < 0 && y > 0) {
       int n = sh.count, step = 1;          // among items [a, a + n)
       a = 0;
@@ -287,17 +293,18 @@ __device__ __forceinline__ Piece<PLAN> piece_at(const PagedGeom& g, const Share<
         step = (n + 63) / 64;
         const int at = a + min(((int)(threadIdx.x & 63) + 1) * step, n) - 1;
         const uint64_t past = __ballot(g.plan_end[at] > y);
-        const int k = __builtin_ctzll(past);
+        const int k = uniform(__builtin_ctzll(past));
         n = min(step, n - k * step);
         a += k * step;
       }
     }
     *hint = a;
     const int2 it = g.plan_item[a];
-    p.seq = __builtin_amdgcn_readfirstlane(it.x);
-    p.tile = __builtin_amdgcn_readfirstlane(it.y);
-    before = a > 0 ? g.plan_end[a - 1] : 0;
+    p.seq = uniform(it.x);
+    p.tile = uniform(it.y);
+    before = a > 0 ? uniform(g.plan_end[a - 1]) : 0;
     p.s = check_seq(g, g.seqs[p.seq]);
+    p.s = PagedSeq{uniform(p.s.cached), uniform(p.s.fresh), uniform(p.s.row)};
   } else {
     p.seq = __builtin_ctzll(__ballot(sh.units_incl > y));
     p.tile = 0;

@@ -41,6 +41,7 @@ struct ChunkTile {
   static constexpr int LOADS = kWaveTokens / ROWS;                 // loads per wavefront of K, and of V
 };
 static_assert(join_lds(kChunkThreads, kChunkRows) <= 65536, "");
+static_assert(ChunkTile<128>::LOADS == 4 && ChunkTile<64>::LOADS == 2, "");
 static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 16, "");
 
 // UNIFORM: 16 tokens always lie in one page
@@ -49,7 +50,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
   using Tile = ChunkTile<D>;
   constexpr int RB = Tile::RB, NF = D / 16, CT = D / 32, BUFS = Tile::BUFS;
   // tiles of K and V each; later the join's scratch
-  __shared__ __align__(1024) char lds[BUFS * 2 * Tile::BYTES];
+  __shared__ __align__(8192) char lds[BUFS * 2 * Tile::BYTES];
   __shared__ int sh_page[kPageCache];
   __shared__ __align__(8) uint16_t sh_present[BUFS][kChunkWaves];  // which tokens of the tile anyone may see, 16 per wavefront
   __shared__ int sh_last, sh_odd[4];
@@ -58,28 +59,18 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
   const uint32_t lds0 = (uint32_t)(size_t)(lds_ptr)lds;
   if (tid < 4) sh_odd[tid] = 0;
 
-  // where this lane reads: keys of row col, channels 16 f + 8 hi ..; values of 4 rows, transposed by the read (lane i of 16 points at
-  // row i / 4, channels 4 (i % 4) .. and gets channel i of the four)
-  int ka[NF], va[CT][2];
-#pragma unroll
-  for (int f = 0; f < NF; ++f) ka[f] = col * RB + ((2 * f + hi) ^ key_swap<D>(col)) * 16;
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int r = 8 * x + 4 * hi + (i16 >> 2), c = 4 * ct + 2 * grp + ((i16 & 3) >> 1);
-      va[ct][x] = r * RB + (c ^ value_swap<D>(r)) * 16 + (i16 & 1) * 8;
-    }
-  // and what it loads: places lane % PIECES of rows 16 wave + ROWS k + lane / PIECES of the tile
+  // Where this lane reads: keys of row col, channels 16 f + 8 hi .., at kbase ^ 32 f; values of row 4 hi + i16 / 4 (and + 8), transposed
+  // by the read (lane i of 16 points at row i / 4, channels 4 (i % 4) .. and gets channel i of the four), channels 32 ct + 16 grp .., at
+  // vbase ^ (64 ct + 32 x) and x times 8 rows on.  (The swaps are exclusive ors, so are the steps; registers are what this kernel is short of.)
+  const int kbase = col * RB + (hi ^ key_swap<D>(col)) * 16;
+  const int vrow = 4 * hi + (i16 >> 2), vbase = vrow * RB + ((2 * grp + ((i16 & 3) >> 1)) ^ value_swap<D>(vrow)) * 16 + (i16 & 1) * 8;
+  // And what it loads: places lane % PIECES of rows 16 wave + ROWS k + lane / PIECES of the tile
   const int lrow = lane / Tile::PIECES, lplace = lane % Tile::PIECES;
-  uint32_t kat[Tile::LOADS], vat[Tile::LOADS];                     // byte offsets from the row, where rows adjoin from the wavefront's first
-#pragma unroll
-  for (int k = 0; k < Tile::LOADS; ++k) {
-    const int r = k * Tile::ROWS + lrow, rt = wave * kWaveTokens + r;
-    const uint32_t row = UNIFORM ? (uint32_t)(r * (int)g.st_tok) : 0u;
-    kat[k] = row + (lplace ^ key_swap<D>(rt)) * 16;
-    vat[k] = row + (lplace ^ value_swap<D>(rt)) * 16;
-  }
+  const uint32_t kplace = (lplace ^ key_swap<D>(lrow)) * 16, vplace = (lplace ^ value_swap<D>(lrow)) * 16;        // of k = 0
+  const uint32_t lrow_at = UNIFORM ? (uint32_t)(lrow * (int)g.st_tok) : 0u;
+  const auto kat = [&](int k) { return lrow_at + (kplace ^ (D == 128 ? 64u * k : 0u)); };
+  const auto vat = [&](int k) { return lrow_at + (vplace ^ (D == 128 ? 16u * k : 32u * k)); };
+  const int64_t step = UNIFORM ? Tile::ROWS * g.st_tok : 0;        // from the rows of load k to those of k + 1
 
   const int w = share_number(blockIdx.x, gridDim.x);
   const Share<true> sh = share_of<true>(g, w, 4);
@@ -125,7 +116,11 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
     for (int e = page_lo + tid; e <= page_hi; e += kChunkThreads) sh_page[e - page0] = page_id(g, p.seq, e);
     __syncthreads();
 
-    const auto request = [&](int i) {
+    // UNIFORM: where the tile that is being loaded comes from, and goes to; its loads are spread over the work on the tile before the last
+    // (all at once right after the barrier they kept every wavefront from its products for 1900 of a tile's 11600 cycles)
+    int64_t coming = 0;
+    uint32_t coming_lds = 0;
+    const auto request = [&](int i, bool at_once) {
       const int buf = i % BUFS, tw = ts + i * kTileTokens + wave * kWaveTokens;
       const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * kWaveTokens * RB, vdst = kdst + Tile::BYTES;
       const int a = max(it.low - tw, 0), z = min(te - tw, kWaveTokens);          // tokens [a, z) of the 16
@@ -134,11 +129,15 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         const int pt = page_of(g, tw);
         const int id = present ? __builtin_amdgcn_readfirstlane(sh_page[pt - page0]) : -1;
         if (id < 0) present = 0;
-        const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(tw - pt * g.by_page.d) * g.st_tok;
+        coming = (int64_t)max(id, 0) * g.st_page + (int64_t)(tw - pt * g.by_page.d) * g.st_tok;
+        coming_lds = kdst;
+        if (at_once) {
 #pragma unroll
-        for (int k = 0; k < Tile::LOADS; ++k) load_to_lds16(Kh + at, kat[k], kdst + k * 1024);
-#pragma unroll
-        for (int k = 0; k < Tile::LOADS; ++k) load_to_lds16(Vh + at, vat[k], vdst + k * 1024);
+          for (int k = 0; k < Tile::LOADS; ++k) {
+            load_to_lds16(Kh + coming + k * step, kat(k), kdst + k * 1024);
+            load_to_lds16(Vh + coming + k * step, vat(k), vdst + k * 1024);
+          }
+        }
       } else {
         uint32_t here = 0;
 #pragma unroll
@@ -146,8 +145,8 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
           const int r = k * Tile::ROWS + lrow, t = tw + r, pt = page_of(g, t);
           const int id = (present >> r) & 1 ? sh_page[pt - page0] : -1;
           const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
-          load_to_lds16(Kh + at + kat[k], kdst + k * 1024);
-          load_to_lds16(Vh + at + vat[k], vdst + k * 1024);
+          load_to_lds16(Kh + at + kat(k), kdst + k * 1024);
+          load_to_lds16(Vh + at + vat(k), vdst + k * 1024);
           const uint64_t there = __ballot(id >= 0);
 #pragma unroll
           for (int y = 0; y < Tile::ROWS; ++y) here |= (uint32_t)((there >> (y * Tile::PIECES)) & 1) << (k * Tile::ROWS + y);
@@ -159,7 +158,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
 
 #pragma unroll
     for (int i = 0; i < BUFS - 1; ++i)
-      if (i < n) request(i);
+      if (i < n) request(i, true);
     for (int i = 0; i < n; ++i) {
       // tile i is there (loads come back in order), tile i - 1 is done with
       const int ahead = min(n - 1 - i, BUFS - 2);
@@ -169,17 +168,25 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
       lds_barrier();
       if (tid < 2) sh_odd[2 * (1 - (i & 1)) + tid] = 0;
       const int buf = i % BUFS;
-      if (i + BUFS - 1 < n) request(i + BUFS - 1);
+      const bool more = i + BUFS - 1 < n;
+      if (more) request(i + BUFS - 1, false);
+      // load number k of K in the first half, of V in the second
+      const auto spread = [&](int half, int k) {
+        if constexpr (UNIFORM) {
+          if (more) load_to_lds16((half ? Vh : Kh) + coming + k * step, half ? vat(k) : kat(k), coming_lds + (half ? Tile::BYTES : 0) + k * 1024);
+        }
+      };
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
       const int tb = ts + i * kTileTokens + half * kChunkTokens;
-      if (tb >= te) break;
+      if (tb < te) {
       const bool skip = idle || tb > lim_hi || tb + kChunkTokens <= low_lo;        // (nothing here for this wavefront)
-      char* const kt = lds + buf * 2 * Tile::BYTES + half * kChunkTokens * RB;
-      char* const vt = kt + Tile::BYTES;
+      const int half_at = buf * 2 * Tile::BYTES + half * kChunkTokens * RB;        // a multiple of 8 KB
+      char* const vt = lds + half_at + Tile::BYTES;
       const uint64_t in_lds = *(const uint64_t*)(sh_present[buf] + half * 4);
 
       // ---- S^T: token 32 u + 8 a + 4 hi + b in element 4 a + b of sc[u]
+      spread(half, 0);
       pc_floatx16 sc[2];
       if (!skip) {
 #pragma unroll
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           ChunkFrag k;
-          k.u = *(const u32x4*)(kt + ka[f] + u * 32 * RB);
+          k.u = *(const u32x4*)(lds + (((half_at + kbase) ^ (32 * f)) + u * 32 * RB));
           sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, q[f].v, sc[u], 0, 0, 0);
         }
       // the LDS reads run four ahead of the products that take them
@@ -200,6 +207,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         if (k < 2 * NF - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       }
+      if constexpr (Tile::LOADS > 2) spread(half, 1);
       const uint64_t present = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)in_lds) |
                                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(in_lds >> 32)) << 32;
 
@@ -231,7 +239,9 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         lds_barrier();
         odd = __builtin_amdgcn_readfirstlane(sh_odd[2 * (i & 1) + half]) != 0;
       }
-      if (skip) continue;
+      spread(half, Tile::LOADS / 2);
+      if constexpr (Tile::LOADS > 2) spread(half, 3);
+      if (!skip) {
 
       if (present != ~0ull || tb + kChunkTokens - 1 > lim_lo || tb < low_hi) {
         const uint64_t mine = present >> (4 * hi);
@@ -278,7 +288,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
           ChunkFrag v;
 #pragma unroll
           for (int y = 0; y < 2; ++y)
-            v.h[y] = __builtin_bit_cast(pc_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pc_s16x4*)(vt + va[ct][y] + k * 16 * RB)));
+            v.h[y] = __builtin_bit_cast(pc_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pc_s16x4*)(lds + (((half_at + vbase) ^ (64 * ct + 32 * y)) + Tile::BYTES + (8 * y + 16 * k) * RB))));
           o[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, pr[k].v, o[ct], 0, 0, 0);
         }
         if (k < 3) weigh(k + 1);
@@ -315,6 +325,8 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
               if (sees && (bits & 0x7f80) == 0x7f80) o[ct][e] = fmaf(weight, bf16_bits_to_float(bits), o[ct][e]);
             }
         }
+      }
+      }
       }
       }
     }
