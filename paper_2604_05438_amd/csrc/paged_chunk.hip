@@ -244,13 +244,17 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
       if (!skip) {
 
       if (present != ~0ull || tb + kChunkTokens - 1 > lim_lo || tb < low_hi) {
-        const uint64_t mine = present >> (4 * hi);
+        // which of the 64 tokens the row sees, those 4 hi on at the bottom; a bit widened to a word picks the score or -inf
+        const int last = lim - tb, first = max(low - tb, 0);
+        uint64_t sees = last < 0 ? 0ull : last > 62 ? ~0ull : (2ull << last) - 1ull;
+        sees &= first > 63 ? 0ull : ~0ull << first;
+        sees = (sees & present) >> (4 * hi);
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int slot = 32 * u + 8 * (e / 4) + e % 4, t = tb + slot + 4 * hi;
-            if (!((mine >> slot) & 1) || t > lim || t < low) sc[u][e] = -INFINITY;
+            const int pick = __builtin_amdgcn_sbfe((int)(uint32_t)(sees >> (32 * u)), 8 * (e / 4) + e % 4, 1);
+            sc[u][e] = __uint_as_float((__float_as_uint(sc[u][e]) & (uint32_t)pick) | (0xff800000u & ~(uint32_t)pick));
           }
       }
       // ---- running maximum and sum
@@ -280,6 +284,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         for (int y = 0; y < 4; ++y) pr[k].u[y] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)e[2 * y], (__bf16)e[2 * y + 1]});
         sum[k] = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       };
+      __builtin_amdgcn_s_setprio(1);                               // (the wavefront next door, between its products, yields: 1 to 3 %)
       weigh(0);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -293,6 +298,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         }
         if (k < 3) weigh(k + 1);
       }
+      __builtin_amdgcn_s_setprio(0);
       l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       // the next step's weights between this one's products
       __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
