@@ -61,6 +61,7 @@ struct PagedGeom {
   int2* plan_item;                        // (sequence, tile)
   int* plan_count;
   int plan_room;                          // items the plan has room for; 0: none needed
+  int least;                              // units that a workgroup gets at least, with a plan
   // append
   int dtype, rot, adjacent;
   Divisor by_half, by_lines;              // rot / 2; rows per token and KV head: query heads, key, value

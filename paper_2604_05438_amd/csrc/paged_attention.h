@@ -24,23 +24,26 @@ __device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int
 __device__ __forceinline__ void store_pair(float* p, float a, float b) {
   store_agent((uint64_t*)p, (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a));
 }
+// SAME: within the launch that stored it (GPU-coherent); otherwise after a kernel boundary
+template <bool SAME>
 __device__ __forceinline__ float2 load_pair(const float* p) {
-  const uint64_t v = load_agent((const uint64_t*)p);
+  uint64_t v;
+  if constexpr (SAME) v = load_agent((const uint64_t*)p);
+  else v = *(const __attribute__((address_space(1))) uint64_t*)p;
   return make_float2(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 
 static_assert(kJoinPairs >= kMaxSplit, "one row of the most pieces has to fit");
 
-// Joins `pieces` partials of `rows` x D of an item, piece p at slot(p) with (m, l) behind `stride` rows; called by the last workgroup to
-// arrive.  What a thread needs is requested before it waits: one load after another, each to memory and back, a join of 64 pieces
-// of one row took 30 us, and one of 2 pieces of 256 rows as much.
-template <typename T, int D, int NT, typename Slot, typename RowOf>
-__device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
-  constexpr int HALF = D / 2, BATCH = 8;
+// Joins `pieces` partials of the rows [row0, row0 + rows) of an item, piece p at slot(p) with (m, l) behind `stride` rows.  What a thread needs
+// is requested before it waits: one load after another, each to memory and back, a join of 64 pieces of one row took 30 us.
+template <typename T, int D, int NT, bool SAME, typename Slot, typename RowOf>
+__device__ void join_pieces(const PagedGeom& g, int pieces, int row0, int rows, int stride, char* lds, Slot&& slot, RowOf&& row_of) {
+  constexpr int HALF = D / 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const auto finish = [&](int r, int c, float2 o, float m, float l) {          // channels c, c + 1 of row r
+  const auto finish = [&](int r, int c, float2 o, float m, float l) {          // channels c, c + 1 of row row0 + r
     int token, head;
-    row_of(r, &token, &head);
+    row_of(row0 + r, &token, &head);
     store_out<T>(g, token, head, c, o, m, l);
   };
   // Few elements (pairs of channels): several threads share the pieces of one; each of them gets along with one round of loads, (m, l) among them
@@ -57,8 +60,8 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
 #pragma unroll
         for (int k = 0; k < WIDE; ++k) {
           const float* at = slot(min(p0 + k * share, pieces - 1));
-          v[k] = load_pair(at + r * D + c);
-          ml[k] = load_pair(at + stride * D + r * 2);
+          v[k] = load_pair<SAME>(at + (row0 + r) * D + c);
+          ml[k] = load_pair<SAME>(at + stride * D + (row0 + r) * 2);
         }
         float mb = m;
 #pragma unroll
@@ -98,7 +101,7 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
     const int n = min(group, rows - r0);
     const int items = n * HALF;
     __syncthreads();
-    for (int x = tid; x < n * pieces; x += NT) ml[x] = load_pair(slot(x % pieces) + stride * D + (r0 + x / pieces) * 2);
+    for (int x = tid; x < n * pieces; x += NT) ml[x] = load_pair<SAME>(slot(x % pieces) + stride * D + (row0 + r0 + x / pieces) * 2);
     __syncthreads();
     if (pieces <= 8) {
       for (int r = tid; r < n; r += NT) {
@@ -130,38 +133,43 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int rows, int stride
       }
     }
     __syncthreads();
-    // several elements of two pieces at a time
-      for (int x0 = tid; x0 < items; x0 += NT * BATCH) {
-        float2 o[BATCH];
+    // E elements of 16 / E pieces at a time
+    const auto sum_up = [&](auto elements) {
+      constexpr int E = decltype(elements)::value, P = 16 / E;
+      for (int x0 = tid; x0 < items; x0 += NT * E) {
+        float2 o[E];
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k) o[k] = make_float2(0.f, 0.f);
-        for (int p = 0; p < pieces; p += 2) {
-          const int p1 = min(p + 1, pieces - 1);
-          float2 a[BATCH], b[BATCH];
+        for (int k = 0; k < E; ++k) o[k] = make_float2(0.f, 0.f);
+        for (int p0 = 0; p0 < pieces; p0 += P) {
+          float2 v[P][E];
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
-            const int x = min(x0 + k * NT, items - 1);
-            a[k] = load_pair(slot(p) + r0 * D + x * 2);
-            b[k] = load_pair(slot(p1) + r0 * D + x * 2);
+          for (int y = 0; y < P; ++y) {
+            const float* at = slot(min(p0 + y, pieces - 1)) + (row0 + r0) * D;
+#pragma unroll
+            for (int k = 0; k < E; ++k) v[y][k] = load_pair<SAME>(at + min(x0 + k * NT, items - 1) * 2);
           }
 #pragma unroll
-          for (int k = 0; k < BATCH; ++k) {
-            const int r = min(x0 + k * NT, items - 1) / HALF;
-            const float f = ml[r * pieces + p].x, h = ml[r * pieces + p1].x;
-            o[k].x = fmaf(a[k].x, f, o[k].x);
-            o[k].y = fmaf(a[k].y, f, o[k].y);
-            if (p1 == p) continue;
-            o[k].x = fmaf(b[k].x, h, o[k].x);
-            o[k].y = fmaf(b[k].y, h, o[k].y);
+          for (int k = 0; k < E; ++k) {
+            const float2* f = ml + min(x0 + k * NT, items - 1) / HALF * pieces;
+#pragma unroll
+            for (int y = 0; y < P; ++y) {
+              const bool in = p0 + y < pieces;
+              const float weight = f[min(p0 + y, pieces - 1)].x;
+              o[k].x = fmaf(in ? v[y][k].x : 0.f, weight, o[k].x);
+              o[k].y = fmaf(in ? v[y][k].y : 0.f, weight, o[k].y);
+            }
           }
         }
 #pragma unroll
-        for (int k = 0; k < BATCH; ++k)
+        for (int k = 0; k < E; ++k)
           if (x0 + k * NT < items) {
             const int x = x0 + k * NT, r = x / HALF;
             finish(r0 + r, x % HALF * 2, o[k], sums[r].x, sums[r].y);
           }
       }
+    };
+    if (items <= 2 * NT) sum_up(std::integral_constant<int, 2>());
+    else sum_up(std::integral_constant<int, 4>());
   }
 }
 
@@ -227,9 +235,8 @@ struct Share {
     return __builtin_amdgcn_readfirstlane((int)(unit < longer ? quotient(unit, each + 1) : rest + quotient(unit - longer, each)));
   }
 };
-// least: units that a workgroup gets at least where there are more workgroups than that
 template <bool PLAN>
-__device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w, int least) {
+__device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w) {
   using Int = typename Share<PLAN>::Int;
   Share<PLAN> r;
   r.count = 0;
@@ -248,7 +255,7 @@ __device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w, int l
     r.per_head = __builtin_amdgcn_readlane(r.units_incl, 63);
   }
   r.all = r.per_head * g.Hkv;
-  r.W = (int)min((Int)g.splits, least == 1 ? r.all : (r.all + least - 1) / least);
+  r.W = (int)min((Int)g.splits, PLAN ? (r.all + g.least - 1) / g.least : r.all);
   r.begin = r.end = r.each = 0;
   r.rest = 0;
   if (w < r.W) {
@@ -325,14 +332,15 @@ __device__ __forceinline__ Piece<PLAN> piece_at(const PagedGeom& g, const Share<
 __device__ __forceinline__ float* partial_slot(const PagedGeom& g, int w, bool first) {
   return g.partial + ((int64_t)w * 2 + (first ? 0 : 1)) * g.tile_rows * (g.d + 2);
 }
-// After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.
-template <typename T, int D, int NT, bool PLAN>
-__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share<PLAN>& sh, const Piece<PLAN>& p, char* lds, int* sh_last) {
+// After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.  (With a plan a
+// kernel of its own does, in which many workgroups share the rows of an item: paged_join_kernel.)
+template <typename T, int D, int NT>
+__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share<false>& sh, const Piece<false>& p, char* lds, int* sh_last) {
   const int w0 = sh.owner(p.item0), w1 = sh.owner(p.item1 - 1);
   if (!last_to_arrive(g.arrived + w0, w1 - w0 + 1, sh_last)) return;
   const bool first = sh.first_of(w0) == p.item0;          // the first workgroup's share starts with this item
-  join_pieces<T, D, NT>(g, w1 - w0 + 1, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
-                    [&](int row, int* token, int* head) { p.place(g, row, token, head); });
+  join_pieces<T, D, NT, true>(g, w1 - w0 + 1, 0, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
+                              [&](int row, int* token, int* head) { p.place(g, row, token, head); });
 }
 
 }  // namespace tkphi

@@ -387,7 +387,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
   const int w = blockIdx.x;
-  const auto sh = share_of<PLAN>(g, w, 1);
+  const auto sh = share_of<PLAN>(g, w);
   Wave at;
   int hint = -1;
   for (auto x = sh.begin; x < sh.end;) {
@@ -457,16 +457,41 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
         int token, head;
         p.place(g, row, &token, &head);
         store_out<T>(g, token, head, c, o, m, l);
+      } else if constexpr (PLAN) {
+        *(float2*)(slot + row * D + c) = o;
+        if (c == 0) *(float2*)(slot + g.tile_rows * D + row * 2) = make_float2(m, l);
       } else {
         store_pair(slot + row * D + c, o.x, o.y);
         if (c == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
       }
     });
     report_pages(g, bad);
-    if (!whole) finish_item<T, D, kPagedThreads, PLAN>(g, sh, p, lds, &sh_last);
+    if constexpr (!PLAN) {
+      if (!whole) finish_item<T, D, kPagedThreads>(g, sh, p, lds, &sh_last);
+    }
     __syncthreads();
     x = min(sh.end, p.item1);
   }
+}
+
+// After the kernels with a plan: share w joins the item that starts in it and ends in another, 8 rows per workgroup at a time (one workgroup for
+// a whole item: 250 us for 64 rows in 125 pieces)
+constexpr int kJoinRows = 8, kJoinGroups = 8;
+template <typename T, int D>
+__global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedGeom g) {
+  __shared__ __align__(16) char lds[join_lds(kPagedThreads, kJoinRows)];
+  const int w = blockIdx.x;
+  const Share<true> sh = share_of<true>(g, w);
+  if (sh.begin >= sh.end) return;
+  int hint = -1;
+  const Piece<true> p = piece_at<true>(g, sh, sh.end - 1, &hint);
+  if (p.item0 < sh.begin || p.item1 <= sh.end) return;
+  const int pieces = sh.owner(p.item1 - 1) - w + 1;
+  const bool first = p.item0 == sh.begin;
+  for (int r0 = blockIdx.y * kJoinRows; r0 < p.it.rows; r0 += kJoinRows * kJoinGroups)
+    join_pieces<T, D, kPagedThreads, false>(g, pieces, r0, min(kJoinRows, p.it.rows - r0), g.tile_rows, lds,
+                                            [&](int k) { return partial_slot(g, w + k, k > 0 || first); },
+                                            [&](int row, int* token, int* head) { p.place(g, row, token, head); });
 }
 
 // ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens
@@ -531,7 +556,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
     }
   });
   if (!whole && last_to_arrive(g.arrived + at_list, pieces, &sh_last))
-    join_pieces<T, D, kPagedThreads>(g, pieces, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
+    join_pieces<T, D, kPagedThreads, true>(g, pieces, 0, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
                       [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
 }
 
@@ -548,6 +573,7 @@ static void launch_attend(const PagedGeom& g, hipStream_t s) {
   if (g.tile_rows == kChunkRows) launch_paged_chunk(g, s);
   else if (g.tile_rows <= 16) launch_split<T, D, 1>(g, s);
   else launch_split<T, D, 2>(g, s);
+  if (g.plan_room) hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(g.splits, kJoinGroups), dim3(kPagedThreads), 0, s, g);
 }
 void launch_paged_attention(const PagedGeom& g, hipStream_t s) {
   if (g.dtype == TKPHI_BF16) {

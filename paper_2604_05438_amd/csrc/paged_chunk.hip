@@ -40,7 +40,6 @@ struct ChunkTile {
   static constexpr int ROWS = 1024 / RB;                           // rows that one load of a wavefront covers
   static constexpr int LOADS = kWaveTokens / ROWS;                 // loads per wavefront of K, and of V
 };
-static_assert(join_lds(kChunkThreads, kChunkRows) <= 65536, "");
 static_assert(ChunkTile<128>::LOADS == 4 && ChunkTile<64>::LOADS == 2, "");
 static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 16, "");
 
@@ -49,11 +48,11 @@ template <int D, bool UNIFORM>
 __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g) {
   using Tile = ChunkTile<D>;
   constexpr int RB = Tile::RB, NF = D / 16, CT = D / 32, BUFS = Tile::BUFS;
-  // tiles of K and V each; later the join's scratch
+  // tiles of K and V each
   __shared__ __align__(8192) char lds[BUFS * 2 * Tile::BYTES];
   __shared__ int sh_page[kPageCache];
   __shared__ __align__(8) uint16_t sh_present[BUFS][kChunkWaves];  // which tokens of the tile anyone may see, 16 per wavefront
-  __shared__ int sh_last, sh_odd[4];
+  __shared__ int sh_odd[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
   const uint32_t lds0 = (uint32_t)(size_t)(lds_ptr)lds;
@@ -73,7 +72,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
   const int64_t step = UNIFORM ? Tile::ROWS * g.st_tok : 0;        // from the rows of load k to those of k + 1
 
   const int w = share_number(blockIdx.x, gridDim.x);
-  const Share<true> sh = share_of<true>(g, w, 4);
+  const Share<true> sh = share_of<true>(g, w);
   int hint = -1;
   for (int64_t x = sh.begin; x < sh.end;) {
     const Piece<true> p = piece_at<true>(g, sh, x, &hint);
@@ -112,7 +111,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
     for (int ts = t0; ts < t1; ts += stretch) {
     const int te = min(ts + stretch, t1), n = (te - ts + kTileTokens - 1) / kTileTokens;
     const int page0 = page_of(g, ts), page_lo = page_of(g, max(ts, it.low)), page_hi = page_of(g, te - 1);
-    __syncthreads();                                               // (the stretch before, or the join of the item before, is done with LDS)
+    __syncthreads();                                               // (the stretch, or the item, before is done with LDS)
     for (int e = page_lo + tid; e <= page_hi; e += kChunkThreads) sh_page[e - page0] = page_id(g, p.seq, e);
     __syncthreads();
 
@@ -362,11 +361,12 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int e = 0; e < 16; e += 2) store_pair(slot + row * D + 32 * ct + 8 * (e / 4) + 4 * hi + e % 4, o[ct][e], o[ct][e + 1]);
-        if (hi == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
+          for (int a = 0; a < 4; ++a)
+            *(__attribute__((address_space(1))) u32x4*)(slot + row * D + 32 * ct + 8 * a + 4 * hi) =
+                (u32x4){__float_as_uint(o[ct][4 * a]), __float_as_uint(o[ct][4 * a + 1]), __float_as_uint(o[ct][4 * a + 2]), __float_as_uint(o[ct][4 * a + 3])};
+        if (hi == 0) *(float2*)(slot + g.tile_rows * D + row * 2) = make_float2(m, l);
       }
     }
-    if (!whole) finish_item<uint16_t, D, kChunkThreads, true>(g, sh, p, lds, &sh_last);
     x = min(sh.end, p.item1);
   }
 }
