@@ -6,4 +6,4 @@ ctypes binding with the same entry-point names (`binding`), the build helper
 loaded at import time; the binding loads the shared library on first use and
 raises if it has not been built.
 """
-__all__ = ["binding", "inputs", "build"]
+__all__ = ["binding", "inputs", "build", "paged"]

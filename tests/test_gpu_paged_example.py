@@ -1,0 +1,34 @@
+"""The serving example: prompts in chunks, dense steps, block steps on one cache, every output against the oracle; and the cache's bookkeeping."""
+import os
+import sys
+
+import pytest
+
+sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_serving_loop(dtype):
+    import paged_serving
+    assert paged_serving.check(dtype) <= 1.0
+
+
+def test_pages_are_taken_and_given_back():
+    from paper_2604_05438_amd.paged import PagedCache
+    c = PagedCache(4, 2, 64, 5, 16, 3, 40, 64, block=16, last_blocks=1, device="cpu")
+    st = c.begin_step({"a": 17, "b": 3})
+    assert (st.n_seqs, st.rows, st.max_new, st.max_len, st.max_pages) == (2, 20, 17, 17, 2)
+    assert c._seqs.tolist() == [[0, 17, 0, 0], [0, 3, 17, 0]] and c._table.tolist() == [[0, 1], [2, -1]]
+    c.end_step()
+    c.begin_step({"b": 1, "a": 1})
+    assert c._seqs.tolist() == [[3, 1, 0, 0], [17, 1, 1, 0]] and len(c.free) == 2
+    c.end_step()
+    with pytest.raises(MemoryError):
+        c.begin_step({"a": 31, "d": 9})
+    with pytest.raises(ValueError):
+        c.begin_step({"a": 3, "d": 38})
+    c.release("a")
+    assert sorted(c.free) == [0, 1, 3, 4] and "a" not in c.length
+    c.begin_step({"c": 40})
+    assert len(c.pages["c"]) == 3
