@@ -87,14 +87,14 @@ tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, Pag
 void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   const int64_t rows = (int64_t)g->max_new * g->G;
   const bool chunk = g->dtype == TKPHI_BF16 && rows > kPagedRows;
-  g->tile_rows = chunk ? kChunkRows : rows <= 16 ? 16 : kPagedRows;
+  g->tile_rows = chunk ? chunk_rows(g->d) : rows <= 16 ? 16 : kPagedRows;
   const int64_t tiles = std::max<int64_t>(1, up(rows, g->tile_rows));
   g->unit_shift = g->dtype == TKPHI_BF16 && !chunk ? 7 : 6;
   const int64_t units = (int64_t)g->n_seqs * tiles * g->Hkv * up(std::max(g->max_len, 1), 1 << g->unit_shift);      // at most
   g->least = 2;      // (1 or 4: 16 and 29 instead of 20 us for 16 tokens of a 3B layer alone, 51 and 47 instead of 43 for four chunks of up to 100)
   if (chunk || tiles > 1 || g->n_seqs > 64 || units >= (1ll << 31))
     g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * tiles);
-  g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? kChunkSplit : 256 * attend_per_cu(g->d, g->tile_rows / 16)));
+  g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? 256 * chunk_per_simd(g->d) / (chunk_rows(g->d) / 128) : 256 * attend_per_cu(g->d, g->tile_rows / 16)));
 }
 
 void plan_blocks(const tkphi_paged_config* c, PagedGeom* g) {
@@ -122,7 +122,7 @@ PagedSpace space_of(const tkphi_paged_config* c, const PagedGeom& g0) {
   if (g.block) block_slots = heads * (c->workgroups ? std::min(c->workgroups, 64) : 1) + (c->workgroups ? 0 : 2 * 512 + g.Hkv * 64);
   s.arrived = 256;
   s.partial = s.arrived + padded(std::max<size_t>(kMaxSplit, heads) * sizeof(uint32_t));
-  s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, (c->workgroups ? c->workgroups : kChunkSplit) * kChunkRows) * 2, (size_t)block_slots * 16) * row_bytes);
+  s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, c->workgroups ? c->workgroups * chunk_rows(128) : kChunkSplitRows) * 2, (size_t)block_slots * 16) * row_bytes);
   s.plan_item = s.plan_end + padded((size_t)items * sizeof(int64_t));
   s.keys = s.plan_item + padded((size_t)items * sizeof(int2) + 256);
   s.list = s.keys + padded(g.block ? (size_t)heads * g.max_blocks * sizeof(uint64_t) : 0);

@@ -570,7 +570,7 @@ static void launch_split(const PagedGeom& g, hipStream_t s) {
 template <typename T, int D>
 static void launch_attend(const PagedGeom& g, hipStream_t s) {
   if (g.plan_room) hipLaunchKernelGGL(paged_plan_kernel, dim3(1), dim3(1024), 0, s, g);
-  if (g.tile_rows == kChunkRows) launch_paged_chunk(g, s);
+  if (g.tile_rows > kPagedRows) launch_paged_chunk(g, s);
   else if (g.tile_rows <= 16) launch_split<T, D, 1>(g, s);
   else launch_split<T, D, 2>(g, s);
   if (g.plan_room) hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(g.splits, kJoinGroups), dim3(kPagedThreads), 0, s, g);

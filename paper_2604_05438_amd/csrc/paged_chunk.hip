@@ -20,10 +20,7 @@ union ChunkFrag {
 };
 
 constexpr int kChunkTokens = 64;                                   // that a wavefront takes at a time
-constexpr int kTileTokens = 128;                                   // that go to LDS at a time
-constexpr int kChunkThreads = 512, kChunkWaves = kChunkThreads / 64;
-constexpr int kWaveTokens = kTileTokens / kChunkWaves;            // rows of a tile that a wavefront loads
-constexpr int kPageCache = 4096;                                   // entries of the page table in LDS
+constexpr int kPageCache = 2048;                                   // entries of the page table in LDS
 constexpr float kSlack = 8.f;             // the reference of the exponentials is raised when a score passes it by 2^8 (sums stay far from overflow)
 
 // LDS of one tile: rows of D bf16 in 16-byte pieces, piece c of row r at place c ^ key_swap(r) or c ^ value_swap(r).  Keys are read as 16 bytes of 32
@@ -35,23 +32,26 @@ template <int D> __device__ __forceinline__ int value_swap(int r) {
 
 template <int D>
 struct ChunkTile {
-  static constexpr int RB = D * 2, PIECES = RB / 16, BYTES = kTileTokens * RB;
-  static constexpr int BUFS = 65536 / BYTES;                       // tiles in LDS: one that is worked on, the others on their way
+  static constexpr int RB = D * 2, PIECES = RB / 16;
+  static constexpr int TOKENS = D == 64 ? 64 : 128, HALVES = TOKENS / kChunkTokens;      // that go to LDS at a time
+  static constexpr int BYTES = TOKENS * RB;
+  static constexpr int BUFS = 2;                                   // tiles in LDS: one that is worked on, the others on their way
   static constexpr int ROWS = 1024 / RB;                           // rows that one load of a wavefront covers
-  static constexpr int LOADS = kWaveTokens / ROWS;                 // loads per wavefront of K, and of V
+  static constexpr int WAVES = chunk_rows(D) / 32, THREADS = 64 * WAVES;
+  static constexpr int WAVE_TOKENS = TOKENS / WAVES, GROUPS = WAVE_TOKENS / 16;     // rows of a tile that a wavefront loads, 16 at a time
+  static constexpr int LOADS = WAVE_TOKENS / ROWS, EACH = LOADS / GROUPS;                // loads per wavefront of K, and of V; and per 16 rows
 };
-static_assert(ChunkTile<128>::LOADS == 4 && ChunkTile<64>::LOADS == 2, "");
-static_assert(kChunkRows == 32 * kChunkWaves && kWaveTokens == 16, "");
+static_assert(ChunkTile<128>::LOADS == 2 * ChunkTile<128>::HALVES && ChunkTile<64>::LOADS == 2 * ChunkTile<64>::HALVES, "");
 
 // UNIFORM: 16 tokens always lie in one page
 template <int D, bool UNIFORM>
-__global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g) {
+__global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_per_eu(chunk_per_simd(D), chunk_per_simd(D)))) void paged_chunk_kernel(PagedGeom g) {
   using Tile = ChunkTile<D>;
-  constexpr int RB = Tile::RB, NF = D / 16, CT = D / 32, BUFS = Tile::BUFS;
+  constexpr int THREADS = Tile::THREADS, RB = Tile::RB, NF = D / 16, CT = D / 32, BUFS = Tile::BUFS;
   // tiles of K and V each
   __shared__ __align__(8192) char lds[BUFS * 2 * Tile::BYTES];
   __shared__ int sh_page[kPageCache];
-  __shared__ __align__(8) uint16_t sh_present[BUFS][kChunkWaves];  // which tokens of the tile anyone may see, 16 per wavefront
+  __shared__ __align__(8) uint16_t sh_present[BUFS][Tile::TOKENS / 16];      // which tokens of the tile anyone may see
   __shared__ int sh_odd[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
@@ -63,12 +63,12 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
   // vbase ^ (64 ct + 32 x) and x times 8 rows on.  (The swaps are exclusive ors, so are the steps; registers are what this kernel is short of.)
   const int kbase = col * RB + (hi ^ key_swap<D>(col)) * 16;
   const int vrow = 4 * hi + (i16 >> 2), vbase = vrow * RB + ((2 * grp + ((i16 & 3) >> 1)) ^ value_swap<D>(vrow)) * 16 + (i16 & 1) * 8;
-  // And what it loads: places lane % PIECES of rows 16 wave + ROWS k + lane / PIECES of the tile
+  // And what it loads: places lane % PIECES of rows WAVE_TOKENS wave + ROWS k + lane / PIECES of the tile
   const int lrow = lane / Tile::PIECES, lplace = lane % Tile::PIECES;
   const uint32_t kplace = (lplace ^ key_swap<D>(lrow)) * 16, vplace = (lplace ^ value_swap<D>(lrow)) * 16;        // of k = 0
   const uint32_t lrow_at = UNIFORM ? (uint32_t)(lrow * (int)g.st_tok) : 0u;
   const auto kat = [&](int k) { return lrow_at + (kplace ^ (D == 128 ? 64u * k : 0u)); };
-  const auto vat = [&](int k) { return lrow_at + (vplace ^ (D == 128 ? 16u * k : 32u * k)); };
+  const auto vat = [&](int k) { return lrow_at + (vplace ^ (D == 128 ? 16u * k : 32u * (k & 1))); };
   const int64_t step = UNIFORM ? Tile::ROWS * g.st_tok : 0;        // from the rows of load k to those of k + 1
 
   const int w = share_number(blockIdx.x, gridDim.x);
@@ -109,75 +109,76 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
     // Stretches of the piece whose part of the page table fits LDS
     const int stretch = (int)min((int64_t)16384, (int64_t)(kPageCache - 2) * g.by_page.d / kChunkTokens * kChunkTokens);
     for (int ts = t0; ts < t1; ts += stretch) {
-    const int te = min(ts + stretch, t1), n = (te - ts + kTileTokens - 1) / kTileTokens;
+    const int te = min(ts + stretch, t1), n = (te - ts + Tile::TOKENS - 1) / Tile::TOKENS;
     const int page0 = page_of(g, ts), page_lo = page_of(g, max(ts, it.low)), page_hi = page_of(g, te - 1);
     __syncthreads();                                               // (the stretch, or the item, before is done with LDS)
-    for (int e = page_lo + tid; e <= page_hi; e += kChunkThreads) sh_page[e - page0] = page_id(g, p.seq, e);
+    for (int e = page_lo + tid; e <= page_hi; e += THREADS) sh_page[e - page0] = page_id(g, p.seq, e);
     __syncthreads();
 
     // UNIFORM: where the tile that is being loaded comes from, and goes to; its loads are spread over the work on the tile before the last
     // (all at once right after the barrier they kept every wavefront from its products for 1900 of a tile's 11600 cycles)
-    int64_t coming = 0;
+    int64_t coming[Tile::GROUPS] = {};
     uint32_t coming_lds = 0;
     const auto request = [&](int i, bool at_once) {
-      const int buf = i % BUFS, tw = ts + i * kTileTokens + wave * kWaveTokens;
-      const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * kWaveTokens * RB, vdst = kdst + Tile::BYTES;
-      const int a = max(it.low - tw, 0), z = min(te - tw, kWaveTokens);          // tokens [a, z) of the 16
-      uint32_t present = a >= z ? 0u : ((1u << z) - 1u) & ~((1u << a) - 1u);
+      const int buf = i % BUFS, tw = ts + i * Tile::TOKENS + wave * Tile::WAVE_TOKENS;
+      const uint32_t kdst = lds0 + buf * 2 * Tile::BYTES + wave * Tile::WAVE_TOKENS * RB, vdst = kdst + Tile::BYTES;
       if constexpr (UNIFORM) {
-        const int pt = page_of(g, tw);
-        const int id = present ? __builtin_amdgcn_readfirstlane(sh_page[pt - page0]) : -1;
-        if (id < 0) present = 0;
-        coming = (int64_t)max(id, 0) * g.st_page + (int64_t)(tw - pt * g.by_page.d) * g.st_tok;
+        uint32_t present = 0;
+#pragma unroll
+        for (int y = 0; y < Tile::GROUPS; ++y) {
+          const int t = tw + 16 * y, pt = page_of(g, t), a = max(it.low - t, 0), z = min(te - t, 16);        // tokens [a, z) of the 16
+          const int id = a < z ? __builtin_amdgcn_readfirstlane(sh_page[pt - page0]) : -1;
+          if (id >= 0) present |= (((1u << z) - 1u) & ~((1u << a) - 1u)) << (16 * y);
+          coming[y] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
+        }
         coming_lds = kdst;
         if (at_once) {
 #pragma unroll
           for (int k = 0; k < Tile::LOADS; ++k) {
-            load_to_lds16(Kh + coming + k * step, kat(k), kdst + k * 1024);
-            load_to_lds16(Vh + coming + k * step, vat(k), vdst + k * 1024);
+            const int64_t at = coming[k / Tile::EACH] + k % Tile::EACH * step;
+            load_to_lds16(Kh + at, kat(k), kdst + k * 1024);
+            load_to_lds16(Vh + at, vat(k), vdst + k * 1024);
           }
         }
+        if (lane < Tile::GROUPS) sh_present[buf][wave * Tile::GROUPS + lane] = (uint16_t)(present >> (16 * lane));
       } else {
-        uint32_t here = 0;
+        uint32_t present = 0;
 #pragma unroll
         for (int k = 0; k < Tile::LOADS; ++k) {
           const int r = k * Tile::ROWS + lrow, t = tw + r, pt = page_of(g, t);
-          const int id = (present >> r) & 1 ? sh_page[pt - page0] : -1;
+          const int id = t >= it.low && t < te ? sh_page[pt - page0] : -1;
           const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
           load_to_lds16(Kh + at + kat(k), kdst + k * 1024);
           load_to_lds16(Vh + at + vat(k), vdst + k * 1024);
           const uint64_t there = __ballot(id >= 0);
 #pragma unroll
-          for (int y = 0; y < Tile::ROWS; ++y) here |= (uint32_t)((there >> (y * Tile::PIECES)) & 1) << (k * Tile::ROWS + y);
+          for (int y = 0; y < Tile::ROWS; ++y) present |= (uint32_t)((there >> (y * Tile::PIECES)) & 1) << (k * Tile::ROWS + y);
         }
-        present = here;
+        if (lane < Tile::GROUPS) sh_present[buf][wave * Tile::GROUPS + lane] = (uint16_t)(present >> (16 * lane));
       }
-      if (lane == 0) sh_present[buf][wave] = (uint16_t)present;
     };
 
-#pragma unroll
-    for (int i = 0; i < BUFS - 1; ++i)
-      if (i < n) request(i, true);
+    request(0, true);
     for (int i = 0; i < n; ++i) {
-      // tile i is there (loads come back in order), tile i - 1 is done with
-      const int ahead = min(n - 1 - i, BUFS - 2);
-      if (ahead == 0) wait_vm_loads<0>();
-      else if (ahead == 1) wait_vm_loads<2 * Tile::LOADS>();
-      else wait_vm_loads<4 * Tile::LOADS>();
+      // tile i is there, tile i - 1 is done with
+      wait_vm_loads<0>();
       lds_barrier();
       if (tid < 2) sh_odd[2 * (1 - (i & 1)) + tid] = 0;
       const int buf = i % BUFS;
-      const bool more = i + BUFS - 1 < n;
-      if (more) request(i + BUFS - 1, false);
-      // load number k of K in the first half, of V in the second
-      const auto spread = [&](int half, int k) {
+      const bool more = i + 1 < n;
+      if (more) request(i + 1, false);
+      // one load at each of four places per 64 tokens: first those of K, then those of V
+      const auto spread = [&](int half, int y) {
         if constexpr (UNIFORM) {
-          if (more) load_to_lds16((half ? Vh : Kh) + coming + k * step, half ? vat(k) : kat(k), coming_lds + (half ? Tile::BYTES : 0) + k * 1024);
+          if (!more) return;
+          const bool v = Tile::HALVES == 2 ? half == 1 : y >= Tile::LOADS;
+          const int k = y % Tile::LOADS;
+          load_to_lds16((v ? Vh : Kh) + coming[k / Tile::EACH] + k % Tile::EACH * step, v ? vat(k) : kat(k), coming_lds + (v ? Tile::BYTES : 0) + k * 1024);
         }
       };
 #pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-      const int tb = ts + i * kTileTokens + half * kChunkTokens;
+      for (int half = 0; half < Tile::HALVES; ++half) {
+      const int tb = ts + i * Tile::TOKENS + half * kChunkTokens;
       if (tb < te) {
       const bool skip = idle || tb > lim_hi || tb + kChunkTokens <= low_lo;        // (nothing here for this wavefront)
       const int half_at = buf * 2 * Tile::BYTES + half * kChunkTokens * RB;        // a multiple of 8 KB
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         if (k < 2 * NF - 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
       }
-      if constexpr (Tile::LOADS > 2) spread(half, 1);
+      spread(half, 1);
       const uint64_t present = (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)in_lds) |
                                (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(in_lds >> 32)) << 32;
 
@@ -215,7 +216,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
       bool odd = false;
       if (present != ~0ull || tb + kChunkTokens - 1 > seen_first || tb < low_last) {
         bool mine = false;
-        for (int k = tid; k < kChunkTokens * Tile::PIECES; k += kChunkThreads) {
+        for (int k = tid; k < kChunkTokens * Tile::PIECES; k += THREADS) {
           const int r = k / Tile::PIECES;
           u32x4* at = (u32x4*)(vt + k * 16);
           if (!((present >> r) & 1)) {
@@ -238,8 +239,8 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
         lds_barrier();
         odd = __builtin_amdgcn_readfirstlane(sh_odd[2 * (i & 1) + half]) != 0;
       }
-      spread(half, Tile::LOADS / 2);
-      if constexpr (Tile::LOADS > 2) spread(half, 3);
+      spread(half, 2);
+      spread(half, 3);
       if (!skip) {
 
       if (present != ~0ull || tb + kChunkTokens - 1 > lim_lo || tb < low_hi) {
@@ -372,14 +373,9 @@ __global__ __launch_bounds__(kChunkThreads) void paged_chunk_kernel(PagedGeom g)
 }
 
 void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
-  const bool uniform = g.by_page.d % kWaveTokens == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
-  if (g.d == 64) {
-    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<64, true>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
-    else hipLaunchKernelGGL((paged_chunk_kernel<64, false>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
-  } else {
-    if (uniform) hipLaunchKernelGGL((paged_chunk_kernel<128, true>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
-    else hipLaunchKernelGGL((paged_chunk_kernel<128, false>), dim3(g.splits), dim3(kChunkThreads), 0, s, g);
-  }
+  const bool uniform = g.by_page.d % 16 == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
+  if (g.d == 64) hipLaunchKernelGGL((uniform ? paged_chunk_kernel<64, true> : paged_chunk_kernel<64, false>), dim3(g.splits), dim3(ChunkTile<64>::THREADS), 0, s, g);
+  else hipLaunchKernelGGL((uniform ? paged_chunk_kernel<128, true> : paged_chunk_kernel<128, false>), dim3(g.splits), dim3(ChunkTile<128>::THREADS), 0, s, g);
 }
 
 }  // namespace tkphi
