@@ -211,3 +211,28 @@ def test_pool_beyond_32_bits():
     st.dev["K"], st.dev["V"] = K, V
     out, lse = st.call(B.tkphi_paged_attention, st.config())
     P.check(st, out, lse, want)
+
+
+@pytest.mark.parametrize("model", ["mha", "five"])
+def test_long_pieces(model):
+    """One workgroup passes over more tokens, and more pages, than it holds the page table of."""
+    run("bf16", model, [(40000, 20)], 16, workgroups=1)
+    run("bf16", model, [(40000, 20)], 16, workgroups=1, window=33000)
+    run("bf16", model, [(5000, 20)], 1, workgroups=1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_many_sequences_of_several_tokens(dtype):
+    r = np.random.default_rng(6)
+    run(dtype, "five", [(int(r.integers(0, 90)), int(r.integers(0, 12))) for _ in range(90)], 16, slack_rows=1)
+    run(dtype, "wide", [(int(r.integers(0, 90)), int(r.integers(0, 2))) for _ in range(90)], 16, workgroups=50)
+
+
+def test_sequences_that_share_rows_do_no_harm():
+    """More items than the rows allow for: what fits is done, the rest is left out and reported; memory stays whole."""
+    st = P.Step("bf16", 14, 2, 64, [(0, 40)] * 30, 16, seed=1)
+    st.seqs[:, 2] = 0
+    st.rows, st.q = 40, st.q[:40]
+    st.upload()
+    out, lse = st.call(B.tkphi_paged_attention, st.config(), check_status=B.TKPHI_DEV_BAD_LENGTH)
+    assert np.isfinite(out).all()
