@@ -65,6 +65,7 @@ struct PagedGeom {
   int64_t* plan_end;                      // [items]: units up to and with this item
   int2* plan_item;                        // (sequence, tile)
   int* plan_count;
+  int4* joins;                            // [splits][2] what paged_join_kernel has to know of the item that starts in a share and ends in another
   int plan_room;                          // items the plan has room for; 0: none needed
   int least;                              // units that a workgroup gets at least, with a plan
   // append

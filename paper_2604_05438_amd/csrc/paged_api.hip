@@ -10,7 +10,7 @@ namespace {
 
 // Bytes of the workspace's parts, in order
 struct PagedSpace {
-  size_t arrived, partial, plan_end, plan_item, keys, list, list_head, total;
+  size_t arrived, joins, partial, plan_end, plan_item, keys, list, list_head, total;
 };
 
 size_t padded(size_t x) { return (x + 255) / 256 * 256; }
@@ -121,7 +121,8 @@ PagedSpace space_of(const tkphi_paged_config* c, const PagedGeom& g0) {
   plan_blocks(c, &g);
   if (g.block) block_slots = heads * (c->workgroups ? std::min(c->workgroups, 64) : 1) + (c->workgroups ? 0 : 2 * 512 + g.Hkv * 64);
   s.arrived = 256;
-  s.partial = s.arrived + padded(std::max<size_t>(kMaxSplit, heads) * sizeof(uint32_t));
+  s.joins = s.arrived + padded(std::max<size_t>(kMaxSplit, heads) * sizeof(uint32_t));
+  s.partial = s.joins + padded(kMaxSplit * 2 * sizeof(int4));
   s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, c->workgroups ? c->workgroups * chunk_rows(128) : kChunkSplitRows) * 2, (size_t)block_slots * 16) * row_bytes);
   s.plan_item = s.plan_end + padded((size_t)items * sizeof(int64_t));
   s.keys = s.plan_item + padded((size_t)items * sizeof(int2) + 256);
@@ -177,6 +178,7 @@ tkphi_status check_call(const tkphi_paged_config* c, const tkphi_step* st, const
   g->status = (uint32_t*)w;
   g->plan_count = (int*)(w + s.keys - 256);
   g->arrived = (uint32_t*)(w + s.arrived);
+  g->joins = (int4*)(w + s.joins);
   g->partial = (float*)(w + s.partial);
   g->plan_end = (int64_t*)(w + s.plan_end);
   g->plan_item = (int2*)(w + s.plan_item);

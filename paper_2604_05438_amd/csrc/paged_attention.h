@@ -332,6 +332,19 @@ __device__ __forceinline__ Piece<PLAN> piece_at(const PagedGeom& g, const Share<
 __device__ __forceinline__ float* partial_slot(const PagedGeom& g, int w, bool first) {
   return g.partial + ((int64_t)w * 2 + (first ? 0 : 1)) * g.tile_rows * (g.d + 2);
 }
+// With a plan: which item, if any, paged_join_kernel joins for share w, the one that starts in it and ends in another
+struct JoinRecord {
+  int4 a{0, 0, 0, 0}, b{0, 0, 0, 0};       // pieces (0: none), rows, KV head, first row among the sequence's; first row of q and out, whether the share starts with it
+  __device__ __forceinline__ void note(const PagedGeom& g, const Share<true>& sh, const Piece<true>& p, int w, bool first) {
+    if (p.u0 > 0 || p.item1 <= sh.end) return;
+    a = make_int4(sh.owner(p.item1 - 1) - w + 1, p.it.rows, p.h, p.tile * g.tile_rows);
+    b = make_int4(p.s.row, first, 0, 0);
+  }
+  __device__ __forceinline__ void store(const PagedGeom& g, int w) const {       // by every workgroup of the launch
+    if (threadIdx.x == 0) { g.joins[2 * w] = a; g.joins[2 * w + 1] = b; }
+  }
+};
+
 // After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.  (With a plan a
 // kernel of its own does, in which many workgroups share the rows of an item: paged_join_kernel.)
 template <typename T, int D, int NT>

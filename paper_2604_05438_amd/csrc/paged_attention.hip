@@ -390,6 +390,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   const auto sh = share_of<PLAN>(g, w);
   Wave at;
   int hint = -1;
+  JoinRecord join;
   for (auto x = sh.begin; x < sh.end;) {
     const auto p = piece_at<PLAN>(g, sh, x, &hint);
     const PagedSeq s = p.s;
@@ -469,29 +470,31 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     if constexpr (!PLAN) {
       if (!whole) finish_item<T, D, kPagedThreads>(g, sh, p, lds, &sh_last);
     }
+    if constexpr (PLAN) join.note(g, sh, p, w, x == sh.begin);
     __syncthreads();
     x = min(sh.end, p.item1);
   }
+  if constexpr (PLAN) join.store(g, w);
 }
 
-// After the kernels with a plan: share w joins the item that starts in it and ends in another, 8 rows per workgroup at a time (one workgroup for
+// After the kernels with a plan: the item that starts in share w and ends in another is joined, 8 rows per workgroup at a time (one workgroup for
 // a whole item: 250 us for 64 rows in 125 pieces)
 constexpr int kJoinRows = 8, kJoinGroups = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedGeom g) {
   __shared__ __align__(16) char lds[join_lds(kPagedThreads, kJoinRows)];
   const int w = blockIdx.x;
-  const Share<true> sh = share_of<true>(g, w);
-  if (sh.begin >= sh.end) return;
-  int hint = -1;
-  const Piece<true> p = piece_at<true>(g, sh, sh.end - 1, &hint);
-  if (p.item0 < sh.begin || p.item1 <= sh.end) return;
-  const int pieces = sh.owner(p.item1 - 1) - w + 1;
-  const bool first = p.item0 == sh.begin;
-  for (int r0 = blockIdx.y * kJoinRows; r0 < p.it.rows; r0 += kJoinRows * kJoinGroups)
-    join_pieces<T, D, kPagedThreads, false>(g, pieces, r0, min(kJoinRows, p.it.rows - r0), g.tile_rows, lds,
+  const int4 a = g.joins[2 * w], b = g.joins[2 * w + 1];
+  const int pieces = uniform(a.x), rows = uniform(a.y), h = uniform(a.z), row0 = uniform(a.w), q0 = uniform(b.x), first = uniform(b.y);
+  if (pieces == 0) return;
+  for (int r0 = blockIdx.y * kJoinRows; r0 < rows; r0 += kJoinRows * kJoinGroups)
+    join_pieces<T, D, kPagedThreads, false>(g, pieces, r0, min(kJoinRows, rows - r0), g.tile_rows, lds,
                                             [&](int k) { return partial_slot(g, w + k, k > 0 || first); },
-                                            [&](int row, int* token, int* head) { p.place(g, row, token, head); });
+                                            [&](int row, int* token, int* head) {
+                                              const int r = row0 + row, i = g.by_group(r);
+                                              *token = q0 + i;
+                                              *head = h * g.G + r - i * g.G;
+                                            });
 }
 
 // ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens

@@ -74,6 +74,7 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
   const int w = share_number(blockIdx.x, gridDim.x);
   const Share<true> sh = share_of<true>(g, w);
   int hint = -1;
+  JoinRecord join;
   for (int64_t x = sh.begin; x < sh.end;) {
     const Piece<true> p = piece_at<true>(g, sh, x, &hint);
     const PagedSeq s = p.s;
@@ -368,8 +369,10 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
         if (hi == 0) *(float2*)(slot + g.tile_rows * D + row * 2) = make_float2(m, l);
       }
     }
+    join.note(g, sh, p, w, x == sh.begin);
     x = min(sh.end, p.item1);
   }
+  join.store(g, w);
 }
 
 void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
