@@ -46,8 +46,8 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int row0, int rows, 
     row_of(row0 + r, &token, &head);
     store_out<T>(g, token, head, c, o, m, l);
   };
-  // Few elements (pairs of channels): several threads share the pieces of one; each of them gets along with one round of loads, (m, l) among them
-  if (rows * HALF <= NT) {
+  // Few elements (pairs of channels) of many pieces: several threads share the pieces of one; each of them gets along with one round of loads, (m, l) among them
+  if (rows * HALF <= NT && pieces > 4) {
     constexpr int WIDE = 16;
     const int items = rows * HALF, share = NT / items, x = tid % items, mine = tid / items, r = x / HALF, c = x % HALF * 2;
     float4* part = (float4*)lds;
@@ -168,7 +168,8 @@ __device__ void join_pieces(const PagedGeom& g, int pieces, int row0, int rows, 
           }
       }
     };
-    if (items <= 2 * NT) sum_up(std::integral_constant<int, 2>());
+    if (pieces <= 2) sum_up(std::integral_constant<int, 8>());
+    else if (pieces > 4 && items <= 2 * NT) sum_up(std::integral_constant<int, 2>());
     else sum_up(std::integral_constant<int, 4>());
   }
 }

@@ -477,9 +477,9 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   if constexpr (PLAN) join.store(g, w);
 }
 
-// After the kernels with a plan: the item that starts in share w and ends in another is joined, 8 rows per workgroup at a time (one workgroup for
+// After the kernels with a plan: the item that starts in share w and ends in another is joined, 32 rows per workgroup at a time, 8 of many pieces (one workgroup for
 // a whole item: 250 us for 64 rows in 125 pieces)
-constexpr int kJoinRows = 8, kJoinGroups = 8;
+constexpr int kJoinRows = 32, kJoinGroups = 8;
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedGeom g) {
   __shared__ __align__(16) char lds[join_lds(kPagedThreads, kJoinRows)];
@@ -487,8 +487,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedGeom g) 
   const int4 a = g.joins[2 * w], b = g.joins[2 * w + 1];
   const int pieces = uniform(a.x), rows = uniform(a.y), h = uniform(a.z), row0 = uniform(a.w), q0 = uniform(b.x), first = uniform(b.y);
   if (pieces == 0) return;
-  for (int r0 = blockIdx.y * kJoinRows; r0 < rows; r0 += kJoinRows * kJoinGroups)
-    join_pieces<T, D, kPagedThreads, false>(g, pieces, r0, min(kJoinRows, rows - r0), g.tile_rows, lds,
+  const int step = pieces <= 4 ? kJoinRows : 8;
+  for (int r0 = blockIdx.y * step; r0 < rows; r0 += step * kJoinGroups)
+    join_pieces<T, D, kPagedThreads, false>(g, pieces, r0, min(step, rows - r0), g.tile_rows, lds,
                                             [&](int k) { return partial_slot(g, w + k, k > 0 || first); },
                                             [&](int row, int* token, int* head) {
                                               const int r = row0 + row, i = g.by_group(r);
