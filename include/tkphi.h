@@ -368,8 +368,8 @@ int32_t tkphi_budget_mid(int64_t L, int32_t r_bp, int32_t n_sink, int32_t n_tail
  *   tkphi_block_attention  new tokens over the first and last blocks of their sequence and those whose
  *                          mean keys score highest against them
  * Token t of a sequence is row t % page_tokens of page pages[seq][t / page_tokens].  A step brings
- * new_tokens more tokens per sequence behind the `cached` that are there; the tokens of all sequences
- * stand one behind another in the rows of q, k, v and out.  tkphi_kv_append comes first: the attention
+ * new_tokens more tokens per sequence behind the `cached` that are there; the tokens of a sequence
+ * stand one behind another in the rows of q, k, v and out, and no two sequences share a row.  tkphi_kv_append comes first: the attention
  * calls read the new tokens' keys and values from their pages, like all others.
  *
  * All structs below are HOST structs, read at call time; the pointers inside are DEVICE pointers.
@@ -379,8 +379,8 @@ int32_t tkphi_budget_mid(int64_t L, int32_t r_bp, int32_t n_sink, int32_t n_tail
  *
  * What the host cannot see is checked by the kernels and recorded in the workspace's status word
  * (tkphi_read_device_status): a sequence with cached or new_tokens negative, new_tokens > max_new,
- * cached + new_tokens > max_len, rows outside [0, rows) is skipped (TKPHI_DEV_BAD_LENGTH; its outputs
- * are left alone); a page id outside [-1, n_pages), or -1 (absent) where tkphi_kv_append has to write,
+ * cached + new_tokens > max_len, rows outside [0, rows) is skipped (TKPHI_DEV_BAD_LENGTH, also set where shared rows
+ * make more work than there is room for; outputs are left alone); a page id outside [-1, n_pages), or -1 (absent) where tkphi_kv_append has to write,
  * counts as absent (TKPHI_DEV_BAD_PAGE).  Tokens of absent pages are seen by nobody; a query that sees
  * nothing gets the output 0 and lse -inf.  What a query does not see does not touch its output,
  * whatever the memory holds there.

@@ -2,6 +2,8 @@
 //
 // score(b) = max over the KV head's query heads of q . M_b.  Which blocks a query sees is a yes or no, so the scores are sums in 64 bits (products of two
 // bf16 are exact there, of two fp32 too), compared as order-preserving 64-bit keys, equal ones by the lower block.
+#include <type_traits>
+
 #include "paged.h"
 #include "select_utils.h"
 
@@ -14,19 +16,19 @@ __device__ __forceinline__ uint64_t score_key64(double x) {
   return b >> 63 ? ~b : b | 0x8000000000000000ull;
 }
 
-__device__ __forceinline__ double eighth_sum(double x) {           // over 8 neighbouring lanes, in every one
+__device__ __forceinline__ double quad_sum(double x) {             // over 4 neighbouring lanes, in every one
   const auto move = [](double y, auto ctrl) {
     const uint64_t b = __builtin_bit_cast(uint64_t, y);
     return __builtin_bit_cast(double, (uint64_t)dpp_move<decltype(ctrl)::value>((uint32_t)b) | (uint64_t)dpp_move<decltype(ctrl)::value>((uint32_t)(b >> 32)) << 32);
   };
   x += move(x, std::integral_constant<int, 0xB1>());               // quad_perm [1, 0, 3, 2]
-  x += move(x, std::integral_constant<int, 0x4E>());               // quad_perm [2, 3, 0, 1]
-  return x + move(x, std::integral_constant<int, 0x141>());        // row_half_mirror
+  return x + move(x, std::integral_constant<int, 0x4E>());         // quad_perm [2, 3, 0, 1]
 }
 
-// A lane takes an eighth of the channels of four blocks: the queries, 64-bit numbers in LDS, are read once for the four (with a quarter
-// of one block per lane the kernel was bound by those reads).
-constexpr int kScoreLanes = 8, kScoreEach = 4;
+// A lane takes a quarter of the channels of two blocks; the queries, 64-bit numbers in LDS, are read once for both.  Bound by the 64-bit
+// arithmetic, the sums over lanes among it (an eighth of the channels of four blocks per lane: 15 us for the 16 sequences of a 1B layer, over 38000 blocks;
+// a quarter of two: 11), and by the means' rows of 128 bytes.
+constexpr int kScoreLanes = 4, kScoreEach = 2;
 constexpr int kScoreBlocks = kPagedThreads / kScoreLanes * kScoreEach;         // per pass of a workgroup
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void block_score_kernel(PagedGeom g, int blocks_per_wg) {
@@ -43,7 +45,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_score_kernel(PagedGeom g,
   uint64_t* keys = g.keys + ((int64_t)local * g.Hkv + h) * g.max_blocks;
   bool staged = false;
   for (int b0 = lo; b0 < hi; b0 += kScoreBlocks) {
-    // blocks b0 + tid / 8 + 32 k
+    // blocks b0 + tid / 4 + 64 k
     int id[kScoreEach];
     u32x4 u[kScoreEach][C / EPL];
 #pragma unroll
@@ -91,7 +93,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_score_kernel(PagedGeom g,
       }
 #pragma unroll
       for (int k = 0; k < kScoreEach; ++k) {
-        const double s = eighth_sum(sum[k]);
+        const double s = quad_sum(sum[k]);
         nan[k] = nan[k] || s != s;
         best[k] = s > best[k] ? s : best[k];
       }
