@@ -124,10 +124,10 @@ __device__ __forceinline__ int page_id(const PagedGeom& g, int i, int p) {
 }
 
 // The sequence that owns unit x when sequence i has count(seq) units and they are numbered in order; wave-uniform, every wavefront by
-// itself.  index: -1 if x is past the end; before: units of the sequences ahead of it; total: of all (only if x is past the end).
+// itself.  index: -1 if x is past the end; before: units of the sequences ahead of it.
 struct FoundSeq {
   PagedSeq s;
-  int index, before, total;
+  int index, before;
 };
 template <typename Count>
 __device__ __forceinline__ FoundSeq find_seq(const PagedGeom& g, int x, Count&& count) {
@@ -151,12 +151,11 @@ __device__ __forceinline__ FoundSeq find_seq(const PagedGeom& g, int x, Count&& 
       f.s.fresh = __builtin_amdgcn_readlane(s.fresh, at);
       f.s.row = __builtin_amdgcn_readlane(s.row, at);
       f.before = base + __builtin_amdgcn_readlane(incl - c, at);
-      f.total = 0;
       return f;
     }
     base += total;
   }
-  f.before = f.total = base;
+  f.before = base;
   f.s = PagedSeq{0, 0, 0};
   return f;
 }
@@ -165,7 +164,7 @@ __device__ __forceinline__ FoundSeq find_row(const PagedGeom& g, int x) {
   const int lane = threadIdx.x & 63;
   FoundSeq f;
   f.index = -1;
-  f.before = f.total = 0;
+  f.before = 0;
   f.s = PagedSeq{0, 0, 0};
   for (int i0 = 0; i0 < g.n_seqs; i0 += 64) {
     PagedSeq s{0, 0, 0};
