@@ -52,7 +52,7 @@ struct PagedGeom {
   float* lse;
   // attention: the work of all items (sequence x tile of query rows x KV head) in units of a fixed number of tokens is
   // cut into `splits` equal shares, one per workgroup
-  uint32_t* arrived;                      // [splits] or [row group][Hkv]: pieces of a split item that are done; zero between calls
+  uint32_t* arrived;                      // [kMaxSplit], of which [splits] or [row group][Hkv] are used: pieces of a split item that are done; zero between calls
   float* partial;                         // [splits][2][tile_rows][d + 2]
   int n_pages, n_seqs, max_pages, rows, max_new, max_len;
   int Hkv, G, Hq, d;

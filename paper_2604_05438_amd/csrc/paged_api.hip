@@ -97,13 +97,19 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   g->splits = c->workgroups ? c->workgroups : (int)std::max<int64_t>(1, std::min<int64_t>(units, chunk ? 256 * chunk_per_simd(g->d) / (chunk_rows(g->d) / 128) : 256 * attend_per_cu(g->d, g->tile_rows / 16)));
 }
 
+// Query tokens whose scores and pieces the workspace holds at once: where several workgroups share a KV head of one of them it has a
+// counter, and there are kMaxSplit of those at the same place whatever the step (they are zero between calls, and what follows them is not)
+constexpr int kBlockSplitHeads = 512;     // without config.workgroups: KV heads of query tokens from which on each has one workgroup
+static_assert(kBlockSplitHeads <= kMaxSplit, "the heads that several workgroups share have a counter each");
+int block_row_group(const tkphi_paged_config* c) { return c->workgroups > 1 ? std::min(kBlockRowGroup, kMaxSplit / c->n_kv_heads) : kBlockRowGroup; }
+
 void plan_blocks(const tkphi_paged_config* c, PagedGeom* g) {
   if (!g->block) return;
   g->max_blocks = (int)up(g->max_len, g->block);
   g->kept = std::max(1, std::min(g->first + g->last + g->top, std::max(g->max_blocks, 1)));
   const int64_t tiles = up((int64_t)g->kept * g->block, kPagedThreads / 64 * (g->dtype == TKPHI_BF16 ? 32 : 16));
   const int64_t heads = std::max<int64_t>(1, (int64_t)g->Hkv * g->row_group);
-  g->splits = c->workgroups ? std::min(c->workgroups, 64) : (int)std::max<int64_t>(1, std::min(tiles, up(512, heads)));
+  g->splits = c->workgroups ? std::min(c->workgroups, 64) : (int)std::max<int64_t>(1, std::min(tiles, up(kBlockSplitHeads, heads)));
 }
 
 // The largest need of any step within these bounds: every part grows with every bound, but for the block attention's partials, whose number of
@@ -112,16 +118,16 @@ PagedSpace space_of(const tkphi_paged_config* c, const PagedGeom& g0) {
   PagedGeom g = g0;
   PagedSpace s;
   const size_t row_bytes = (size_t)(g.d + 2) * sizeof(float);
-  const int rg = std::min(g.rows, kBlockRowGroup);
+  const int rg = std::min(g.rows, block_row_group(c));
   const int64_t heads = (int64_t)rg * g.Hkv;
   plan_attention(c, &g);
   const int64_t items = (int64_t)g.rows * g.G / 16 + g.n_seqs;        // (a plan is at most that long, whichever kernel runs)
   int64_t block_slots = 0;
   g.row_group = rg;
   plan_blocks(c, &g);
-  if (g.block) block_slots = heads * (c->workgroups ? std::min(c->workgroups, 64) : 1) + (c->workgroups ? 0 : 2 * 512 + g.Hkv * 64);
+  if (g.block) block_slots = heads * (c->workgroups ? std::min(c->workgroups, 64) : 1) + (c->workgroups ? 0 : 2 * kBlockSplitHeads + g.Hkv * 64);
   s.arrived = 256;
-  s.joins = s.arrived + padded(std::max<size_t>(kMaxSplit, heads) * sizeof(uint32_t));
+  s.joins = s.arrived + padded(kMaxSplit * sizeof(uint32_t));
   s.partial = s.joins + padded(kMaxSplit * 2 * sizeof(int4));
   s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, c->workgroups ? c->workgroups * chunk_rows(128) : kChunkSplitRows) * 2, (size_t)block_slots * 16) * row_bytes);
   s.plan_item = s.plan_end + padded((size_t)items * sizeof(int64_t));
@@ -264,8 +270,9 @@ tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_st
   if ((st = check_pointer(g.M, "M", 16)) != TKPHI_OK) return st;
   g.lse = nullptr;
   (void)hipGetLastError();
-  for (g.row0 = 0; g.row0 < g.rows; g.row0 += kBlockRowGroup) {      // (the scores of so many query tokens fit the workspace)
-    g.row_group = std::min(kBlockRowGroup, g.rows - g.row0);
+  const int group = block_row_group(cfg);
+  for (g.row0 = 0; g.row0 < g.rows; g.row0 += group) {
+    g.row_group = std::min(group, g.rows - g.row0);
     plan_blocks(cfg, &g);
     launch_block_select(g, (hipStream_t)hip_stream);
     launch_block_attention(g, (hipStream_t)hip_stream);
