@@ -11,6 +11,12 @@ constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kJoinPairs = 2048;          // (m, l) of pieces x rows in LDS at once
 constexpr int join_lds(int threads, int rows) { return (kJoinPairs + rows) * 8 > threads * 16 ? (kJoinPairs + rows) * 8 : threads * 16; }
 
+// The weights of bf16 values are rounded to bf16 for the product O = P V, and O is divided by the sum of the weights as rounded: what a weight's rounding
+// adds to the product it adds to the divisor, the output is a mean of the values it sees, off by at most 2^-8 sum p |v - y| / sum p.  (Divided by
+// the sum of the weights themselves, which lse takes, a peak whose weight is no round number had its half step of 2^-8 in the output.)  A partial's O is
+// multiplied by l over that sum, and goes with l from there on.
+__device__ __forceinline__ float to_sum(float l, float l_rounded) { return l == 0.f ? 0.f : l * __builtin_amdgcn_rcpf(l_rounded); }
+
 template <typename T>
 __device__ __forceinline__ void store_out(const PagedGeom& g, int token_row, int head, int c, float2 o, float m, float l) {
   const float inv = l == 0.f ? 0.f : 1.f / l;                      // (l = 0: the row sees nothing, and o is 0)

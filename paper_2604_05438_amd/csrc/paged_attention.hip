@@ -48,6 +48,7 @@ struct WaveAttend {
   PagedFrag q[RT][NF];
   pa_floatx4 o[RT][CT];                                           // O^T: channels 16 ct + 4 kg + i of query row (lane & 15)
   float m[RT], l[RT];                                             // running maximum (of the row) and sum (of this lane's tokens), base 2
+  pa_floatx4 lr[RT];                                              // bf16: sum of the row's weights as rounded, as one more channel of 1 (in every element)
   int lim[RT], low[RT];                                           // tokens [low, lim] are seen by this lane's row
 
   __device__ __forceinline__ void reset() {
@@ -55,6 +56,7 @@ struct WaveAttend {
     for (int rt = 0; rt < RT; ++rt) {
       m[rt] = -INFINITY;
       l[rt] = 0.f;
+      lr[rt] = (pa_floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) o[rt][ct] = (pa_floatx4){0.f, 0.f, 0.f, 0.f};
     }
@@ -218,7 +220,8 @@ struct WaveAttend {
         l[rt] = fmaf(l[rt], fix, sum);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) o[rt][ct] *= fix;
-        if constexpr (BF) {                                        // (the weights enter the product in the cache's own type; their sum does not)
+        if constexpr (BF) {                                        // (the weights enter the product in the cache's own type)
+          lr[rt] *= fix;
 #pragma unroll
           for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -243,6 +246,12 @@ struct WaveAttend {
           *(u32x4*)(vw + u * 8 * VROW + j * 128) = w;
         }
       if (i + 1 < n) load(Vb, lane_at, cur, vf);
+      if constexpr (BF) {
+        PagedFrag ones;
+        ones.u = (u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) lr[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones.v, p[rt][0].v, lr[rt], 0, 0, 0);
+      }
       if (!all && __ballot(odd)) {                                 // (0 times such a value is not 0: row by row, without what they do not see)
         add_seen(p, here, vlds);
         continue;
@@ -285,11 +294,13 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM>& w, char
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float l = across_32(across_16(w.l[rt], AddOp()), AddOp());
+    float f = 1.f;
+    if constexpr (sizeof(T) == 2) f = to_sum(l, w.lr[rt][0]);
     float* row = mine + (rt * 16 + r) * STR;
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) row[ct * 16 + kg * 4 + i] = w.o[rt][ct][i];
+      for (int i = 0; i < 4; ++i) row[ct * 16 + kg * 4 + i] = w.o[rt][ct][i] * f;
     if (kg == 0) { row[D] = w.m[rt]; row[D + 1] = l; }
   }
   __syncthreads();

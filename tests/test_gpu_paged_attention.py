@@ -236,3 +236,39 @@ def test_sequences_that_share_rows_do_no_harm():
     st.upload()
     out, lse = st.call(B.tkphi_paged_attention, st.config(), check_status=B.TKPHI_DEV_BAD_LENGTH)
     assert np.isfinite(out).all()
+
+
+@pytest.mark.parametrize("model", ["odd", "five"])
+@pytest.mark.parametrize("lens,workgroups", [([(1000, 64), (5, 40)], 0), ([(1000, 64), (5, 40)], 1), ([(3000, 1), (70, 2)], 0), ([(3000, 1), (70, 2)], 1)])
+@pytest.mark.parametrize("scale", [1.0, 0.125, 0.02])
+def test_a_mean_of_equal_values_is_that_value(model, lens, workgroups, scale):
+    """Where all values are 1 the output is 1 whatever the weights: what their rounding takes from the product it takes from the divisor.  Sums in
+    32 bits are off by far less than the 2^-9 at which the output would round to the number below 1."""
+    hq, hkv, d = HEADS[model]
+    st = P.Step("bf16", hq, hkv, d, lens, 16, seed=11)
+    st.V[:] = 1.0
+    st.upload()
+    out, lse = st.call(B.tkphi_paged_attention, st.config(scale=scale, workgroups=workgroups))
+    P.check(st, out, lse, P.attention_oracle(st, scale=scale))
+    assert (out == 1.0).all(), (out != 1.0).mean()
+
+
+@pytest.mark.parametrize("model", ["odd", "five"])
+@pytest.mark.parametrize("fresh", [1, 40])
+def test_equal_weights_below_a_peak(model, fresh):
+    """One token with the highest score and many with the same lower one, whose weight lies between two numbers of 8 bits: every one of them is rounded
+    the same way."""
+    hq, hkv, d = HEADS[model]
+    for lag in (0.3, 0.51, 5.3, -float(np.log2(0.5 + 0.9 * 2.0 ** -9)), -float(np.log2(0.5 + 1.1 * 2.0 ** -9))):      # (0.9: half a step down, all but)
+        st = P.Step("bf16", hq, hkv, d, [(300, fresh)], 16, seed=12)
+        st.K[:] = 0
+        st.K[..., 0] = 4.0
+        st.K[st.table[0, 12], :, 5, 0] = 6.0              # token 197
+        st.q[:] = 0
+        st.q[..., 0] = 1.0
+        st.V[:] = 1.0
+        scale = lag * 0.6931471805599453 / 2              # exponents of 2 between the two scores
+        st.upload()
+        out, lse = st.call(B.tkphi_paged_attention, st.config(scale=scale))
+        P.check(st, out, lse, P.attention_oracle(st, scale=scale))
+        assert (out == 1.0).all(), (lag, (out != 1.0).mean())
