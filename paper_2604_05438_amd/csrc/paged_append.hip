@@ -52,6 +52,10 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
   const int h = blockIdx.y, tid = threadIdx.x;
   const FoundSeq f = find_seq(g, blockIdx.x, [&](const PagedSeq& s) { return (s.cached + s.fresh - 1) / tile - s.cached / tile + 1; });
   if (f.index < 0) return;
+  if (blockIdx.x == gridDim.x - 1) {                             // past what the rows allow for: sequences share some (tiles from here on are left out)
+    if (h == 0 && tid == 0) atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
+    return;
+  }
   const int t0 = (f.s.cached / tile + ((int)blockIdx.x - f.before)) * tile;
   const int lo = max(t0, f.s.cached), hi = min(t0 + tile, f.s.cached + f.s.fresh);      // new tokens of this tile
   const int n = hi - lo, half = g.rot / 2;
@@ -148,7 +152,7 @@ void launch_paged_append(const PagedGeom& g, hipStream_t s) {
   // sequence by sequence a tile at either end may be cut
   const int64_t by_rows = g.rows / tile + 2ll * g.n_seqs, by_seqs = (int64_t)g.n_seqs * ((g.max_new - 2 + tile) / tile + 1);
   const unsigned tiles = (unsigned)(by_rows < by_seqs ? by_rows : by_seqs);
-  const dim3 grid(tiles, g.Hkv);
+  const dim3 grid(tiles + 1, g.Hkv);                             // (the last one has a tile only where sequences share rows)
   const size_t lds = (size_t)tile * (g.rot / 2) * sizeof(float2) + (g.block ? (size_t)tile * g.d * (g.dtype == TKPHI_BF16 ? 2 : 4) : 0);
   if (g.dtype == TKPHI_BF16) {
     if (g.d == 64) hipLaunchKernelGGL((paged_append_kernel<uint16_t, 64>), grid, dim3(kPagedThreads), lds, s, g, tile);

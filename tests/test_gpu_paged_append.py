@@ -125,3 +125,31 @@ def test_bad_descriptions_and_pages():
         st = P.Step("bf16", 4, 2, 64, lens, 16, block=16)
         st.table[2, 0] = value
         check_append(st, 64, False, status=B.TKPHI_DEV_BAD_PAGE)
+
+
+@pytest.mark.parametrize("block", [0, 16])
+def test_sequences_that_share_rows_do_no_harm(block):
+    """More tiles than the rows allow for: what fits is written, the rest is left out and reported; nothing else moves."""
+    st = P.Step("bf16", 4, 2, 64, [(0, 40)] * 30, 16, block=block, seed=1)
+    st.seqs[:, 2] = 0
+    st.rows = 40
+    st.upload()
+    qkv = torch.randn(40, 8, 64, generator=torch.Generator().manual_seed(5)).bfloat16().cuda()
+    q_rot = torch.zeros(40, 4, 64, device="cuda", dtype=torch.bfloat16)
+    cfg, step, t = st.config(rot_dim=0), st.step(), st.dev
+    ws = B.alloc_paged_workspace(B.tkphi_paged_workspace_bytes(cfg, step))
+    B.tkphi_kv_append(cfg, step, B.make_pool(t["K"], t["V"], t["M"]), B.make_new_rows(qkv[:, :4], qkv[:, 4:6], qkv[:, 6:], q_rot), ws.data_ptr(), ws.numel(),
+                      B.current_stream_ptr())
+    assert B.tkphi_read_device_status(ws.data_ptr(), B.current_stream_ptr()) == B.TKPHI_DEV_BAD_LENGTH
+    assert torch.equal(q_rot, qkv[:, :4])
+    for now, before, new in ((t["K"], st.K, qkv[:, 4:6]), (t["V"], st.V, qkv[:, 6:])):
+        want = before.clone()
+        done = 0
+        for pages in st.table:
+            for k in range(40):
+                at = pages[k // 16], slice(None), k % 16
+                got = now[at].cpu()
+                if torch.equal(got, new[k].cpu()):
+                    want[at] = got
+                    done += 1
+        assert torch.equal(now.cpu(), want) and 40 <= done < 30 * 40
