@@ -326,7 +326,8 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM>& w, char
 // The items in order with the running sum of their units, by one workgroup.  (Items past the plan's room, as there are if sequences share
 // rows, are left out.)
 __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
-  __shared__ int first[1025], sums[16];
+  __shared__ int first[1025];
+  __shared__ uint32_t sums[16];
   __shared__ int64_t sums64[16];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int items = 0;
@@ -336,22 +337,23 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
       const PagedSeq s = check_seq(g, g.seqs[i0 + tid]);
       tiles = s.fresh > 0 ? (s.fresh * g.G + g.tile_rows - 1) / g.tile_rows : 0;
     }
-    const int x = wave_scan_incl(tiles);
+    // (up to 2^27 rows, 8 heads and 32 rows per item: 2^31 items of 64 sequences that share rows)
+    const uint32_t x = (uint32_t)wave_scan_incl(tiles);
     if (lane == 63) sums[wave] = x;
     __syncthreads();
-    int ahead = 0, all = 0;
+    int64_t ahead = 0, all = 0;
     for (int k = 0; k < 16; ++k) {
       if (k < wave) ahead += sums[k];
       all += sums[k];
     }
-    first[tid + 1] = min(ahead + x, g.plan_room - items);
+    first[tid + 1] = (int)min(ahead + (int64_t)x, (int64_t)(g.plan_room - items));
     if (tid == 0) first[0] = 0;
     __syncthreads();
     if (items + all > g.plan_room) {
       if (tid == 0) atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
       all = g.plan_room - items;
     }
-    for (int j = tid; j < all; j += 1024) {
+    for (int j = tid; j < (int)all; j += 1024) {
       int a = 0, b = min(1024, g.n_seqs - i0) - 1;                 // last sequence that starts at or before j (and has items)
       while (a < b) {
         const int c = (a + b + 1) / 2;
@@ -360,7 +362,7 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
       }
       g.plan_item[items + j] = make_int2(i0 + a, j - first[a]);
     }
-    items += all;
+    items += (int)all;
     __syncthreads();
   }
   __threadfence_block();

@@ -272,3 +272,24 @@ def test_equal_weights_below_a_peak(model, fresh):
         out, lse = st.call(B.tkphi_paged_attention, st.config(scale=scale))
         P.check(st, out, lse, P.attention_oracle(st, scale=scale))
         assert (out == 1.0).all(), (lag, (out != 1.0).mean())
+
+
+def test_more_items_than_32_bits_of_sequences_that_share_rows():
+    """1024 sequences of 2^23 new tokens on the same rows, 2^31 items among them, and some of one token behind them: what fits is done, the rest is
+    left out and reported.  No page is there, so all outputs are 0 (rows and heads of q and of out overlap in memory, to be small)."""
+    n, rows, hq, d = 1100, 1 << 23, 8, 64
+    seqs = torch.zeros(n, 4, dtype=torch.int32)
+    seqs[:1024, 1] = rows
+    seqs[1024:, 1] = 1
+    seqs, pages = seqs.cuda(), torch.full((n, 1), -1, dtype=torch.int32, device="cuda")
+    K = torch.zeros(2, 1, 16, d, device="cuda")
+    q = torch.ones((rows + hq - 1) * d, device="cuda").as_strided((rows, hq, d), (d, d, 1))
+    flat = torch.full(((rows + hq - 1) * d,), 7.0, device="cuda")
+    out = flat.as_strided((rows, hq, d), (d, d, 1))
+    cfg = B.make_paged_config(hq, 1, d, "f32", 0.125, K, K, window=1)
+    step = B.make_step(seqs, pages, rows, rows, rows)
+    ws = B.alloc_paged_workspace(B.tkphi_paged_workspace_bytes(cfg, step))
+    assert ws.numel() > 256, B.tkphi_last_error()
+    B.tkphi_paged_attention(cfg, step, B.make_pool(K, K), B.make_attention_rows(q, out), ws.data_ptr(), ws.numel(), B.current_stream_ptr())
+    assert B.tkphi_read_device_status(ws.data_ptr(), B.current_stream_ptr()) == B.TKPHI_DEV_BAD_LENGTH
+    assert (flat == 0).all()
