@@ -155,7 +155,7 @@ __device__ __forceinline__ bool find_edge(const uint64_t (&key)[kHeld], int roun
     sh.bin = first ? b1 : b1 - 1;
     sh.need = want - above - (first ? 0 : c1);
   }
-  if (tid == kSelThreads - 1 && incl <= want) sh.bin = -1;         // all of them
+  if (tid == kSelThreads - 1 && incl < want) sh.bin = -1;          // all of them (where exactly `want` compete, the edge is the last of them)
   lds_barrier();
   const int edge_bin = sh.bin, need = sh.need;
   if (edge_bin < 0) return true;

@@ -123,3 +123,20 @@ def test_same_in_a_graph():
         call()
         torch.cuda.synchronize()
         assert np.array_equal(t["out"].double().cpu().numpy(), out)
+
+
+def leave(st, keep):
+    """No block's mean but those of `keep` (numbers of the first sequence) is a number."""
+    per = st.page // st.block
+    old = st.M.clone()
+    st.M[:] = float("nan")
+    for b in keep:
+        st.M[st.table[0, b // per], :, b % per] = old[st.table[0, b // per], :, b % per]
+
+
+@pytest.mark.parametrize("count", [0, 1, 11, 12, 13])
+def test_about_as_many_candidates_as_are_retrieved(count):
+    """Twelve are: fewer, exactly as many (the edge is the last of them), one more; in one step of the selection and in several."""
+    r = np.random.default_rng(count)
+    run("bf16", (4, 2, 64), [(5000, 1)], 64, 16, 1, 1, 12, change=lambda st: leave(st, r.choice(np.arange(2, 300), count, replace=False)))
+    run("bf16", (2, 1, 64), [(135000, 1)], 64, 16, 1, 1, 12, change=lambda st: leave(st, r.choice(np.arange(2, 8400), count, replace=False)))
