@@ -140,3 +140,19 @@ def test_about_as_many_candidates_as_are_retrieved(count):
     r = np.random.default_rng(count)
     run("bf16", (4, 2, 64), [(5000, 1)], 64, 16, 1, 1, 12, change=lambda st: leave(st, r.choice(np.arange(2, 300), count, replace=False)))
     run("bf16", (2, 1, 64), [(135000, 1)], 64, 16, 1, 1, 12, change=lambda st: leave(st, r.choice(np.arange(2, 8400), count, replace=False)))
+
+
+@pytest.mark.parametrize("tokens", [30000, 140000])
+@pytest.mark.parametrize("kind", ["any", "same", "few", "close"])
+def test_long_lists_and_full_bins(tokens, kind):
+    """1875 blocks, which the threads hold, and 8750, which they do not; scores anywhere, and more than 1024 of them in one bin of the histogram."""
+    def change(st):
+        if kind == "same":
+            st.M[:] = st.M[0, 0, 0]
+        elif kind == "few":
+            st.M[:] = st.M[:2].repeat(st.n_pages // 2 + 1, 1, 1, 1)[:st.n_pages]
+        elif kind == "close":
+            r = torch.Generator().manual_seed(2)
+            st.M[:] = st.M[0, 0, 0] * (1 + torch.randint(-900, 900, st.M.shape, generator=r) * 2.0 ** -23)
+    run("f32" if kind == "close" else "bf16", (2, 1, 64), [(tokens, 1)], 64, 16, 1, 2, 64, change=change, seed=9)
+    run("f32", (1, 1, 64), [(tokens, 2)], 64, 16, 0, 1, 1000, change=change, seed=10)
