@@ -244,18 +244,46 @@ def tkphi_paged_workspace_bytes(cfg: tkphi_paged_config, step: tkphi_step) -> in
     return lib().tkphi_paged_workspace_bytes(C.byref(cfg), C.byref(step))
 
 
+def _fits(cfg, step, pool, io, heads) -> None:
+    """The tensors that cfg, step, pool and io were made from (make_step and so on) against each other: the kernels go by the config's types, heads and
+    strides and by the step's rows.  heads: the note of the config that the rows' heads have to match.  (A struct filled by hand has
+    no notes: nothing is compared then.  0.3 us where all is well.)"""
+    try:
+        (rows, form, device), want, has, geometry, on, at = io.form, getattr(cfg, heads), pool.form, cfg.pool, pool.device, step.device
+    except AttributeError:
+        return
+    if rows >= step.rows and form == want and has == geometry and on == device == at >= 0 and (pool.blocks == cfg.blocks or not (pool.blocks and cfg.blocks)):
+        return
+    if rows < step.rows:
+        raise ValueError(f"{rows} rows for a step of {step.rows}")
+    if form != want:
+        raise ValueError(f"rows of (storage type, channels, heads) {form} for a config of {want}")
+    if not on == device == at >= 0:
+        raise ValueError(f"rows, pool and step on GPUs {device}, {on}, {at} (-1: not on a GPU)")
+    if pool.blocks != cfg.blocks and pool.blocks and cfg.blocks:
+        raise ValueError(f"M has {pool.blocks} blocks per page, the config {cfg.blocks}")
+    for name, a, b in zip(("storage type", "channels", "KV heads", "tokens per page", "stride of pages", "stride of heads", "stride of tokens"), has, geometry):
+        if a != b and a is not None and b is not None:
+            raise ValueError(f"pool: {name} {a}, in the config {b}")
+
+
 def tkphi_kv_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_new_rows, workspace_ptr: int,
                     workspace_bytes: int, stream: int) -> None:
+    _fits(cfg, step, pool, io, "kv_q_heads" if io.q else "kv_heads")
+    if 2 * getattr(io, "angles", 1 << 30) < cfg.rot_dim:
+        raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
     _check(lib().tkphi_kv_append(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
 
 
 def tkphi_paged_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_attention_rows, workspace_ptr: int,
                           workspace_bytes: int, stream: int) -> None:
+    _fits(cfg, step, pool, io, "q_heads")
     _check(lib().tkphi_paged_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
 
 
 def tkphi_block_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_attention_rows, workspace_ptr: int,
                           workspace_bytes: int, stream: int) -> None:
+    _fits(cfg, step, pool, io, "q_heads")
     _check(lib().tkphi_block_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
 
 
@@ -314,7 +342,7 @@ def alloc_workspace(nbytes: int, device="cuda"):
 
 
 # ---- the paged cache -----------------------------------------------------------------------
-# The structs hold addresses only: the caller keeps the tensors.
+# The structs hold addresses only: the caller keeps the tensors.  What the calls compare with the config (_fits) is noted beside the fields.
 def _tensor(name, t, dims, dtype=None, adjoin=True):
     if t.dim() != dims or (adjoin and t.shape[-1] > 1 and t.stride(-1) != 1) or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}, {t.dtype}; needs {dims} dimensions"
@@ -327,6 +355,26 @@ def _storage_type(kv_dtype):
     return {TKPHI_BF16: torch.bfloat16, TKPHI_F32: torch.float32}[kv_dtype]
 
 
+def _kv_dtype(t):
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{t.dtype} is no storage type (torch.bfloat16 or torch.float32)")
+    return TKPHI_BF16 if t.dtype == torch.bfloat16 else TKPHI_F32
+
+
+def _pool_form(K):
+    """Storage type, channels, heads, tokens and strides; a stride over one element does not matter (None)."""
+    return (_kv_dtype(K), K.shape[3], K.shape[1], K.shape[2], *(K.stride(i) if K.shape[i] > 1 else None for i in range(3)))
+
+
+def _one_device(**tensors):
+    """The GPU that all of them are on, -1 for the CPU"""
+    devices = {n: t.get_device() for n, t in tensors.items() if t is not None}
+    if len(set(devices.values())) > 1:
+        raise ValueError(f"tensors on several GPUs (-1: not on one): {devices}")
+    return next(iter(devices.values()))
+
+
 def make_paged_config(n_q_heads, n_kv_heads, d_head, dtype, score_scale, K, V, window=0, rot_dim=0, rot_adjacent=False, block=0,
                       first_blocks=0, last_blocks=0, top_blocks=0, workgroups=0) -> tkphi_paged_config:
     """K, V: the pool's tensors as [pages][KV heads][tokens per page][channels], in any memory order with adjoining channels and
@@ -336,9 +384,12 @@ def make_paged_config(n_q_heads, n_kv_heads, d_head, dtype, score_scale, K, V, w
         _tensor(name, t, 4, _storage_type(kv))
         if t.shape != K.shape or t.stride() != K.stride() or t.shape[1] != n_kv_heads or t.shape[3] != d_head:
             raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()} do not fit K and the heads")
-    return tkphi_paged_config(int(n_q_heads), int(n_kv_heads), int(d_head), kv, float(score_scale), K.shape[2], K.stride(0), K.stride(1),
-                              K.stride(2), int(window), int(rot_dim), int(bool(rot_adjacent)), int(block), int(first_blocks), int(last_blocks),
-                              int(top_blocks), int(workgroups))
+    cfg = tkphi_paged_config(int(n_q_heads), int(n_kv_heads), int(d_head), kv, float(score_scale), K.shape[2], K.stride(0), K.stride(1),
+                             K.stride(2), int(window), int(rot_dim), int(bool(rot_adjacent)), int(block), int(first_blocks), int(last_blocks),
+                             int(top_blocks), int(workgroups))
+    cfg.pool, cfg.blocks = _pool_form(K), K.shape[2] // cfg.block if cfg.block > 0 else 0
+    cfg.q_heads, cfg.kv_heads, cfg.kv_q_heads = (kv, cfg.d_head, cfg.n_q_heads), (kv, cfg.d_head, cfg.n_kv_heads), (kv, cfg.d_head, cfg.n_kv_heads, cfg.n_q_heads)
+    return cfg
 
 
 def make_step(seqs, pages, rows: int, max_new: int, max_len: int) -> tkphi_step:
@@ -350,16 +401,24 @@ def make_step(seqs, pages, rows: int, max_new: int, max_len: int) -> tkphi_step:
             raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()}; one contiguous row per sequence")
     if seqs.shape[1] != 4:
         raise ValueError("seqs: four words per sequence")
-    return tkphi_step(_ptr(seqs), _ptr(pages), seqs.shape[0], pages.shape[1], int(rows), int(max_new), int(max_len), 0)
+    step = tkphi_step(_ptr(seqs), _ptr(pages), seqs.shape[0], pages.shape[1], int(rows), int(max_new), int(max_len), 0)
+    step.device = _one_device(seqs=seqs, pages=pages)
+    return step
 
 
 def make_pool(K, V, M=None) -> tkphi_kv_pool:
-    """M: mean keys [pages][KV heads][blocks per page][channels], contiguous, or None."""
+    """K, V as for make_paged_config; M: mean keys [pages][KV heads][blocks per page][channels], contiguous, or None."""
+    for name, t in (("K", K), ("V", V)):
+        _tensor(name, t, 4, K.dtype)
+        if t.shape != K.shape or t.stride() != K.stride():
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()} are not those of K")
     if M is not None:
         _tensor("M", M, 4, K.dtype)
         if not M.is_contiguous() or M.shape[:2] != K.shape[:2] or M.shape[3] != K.shape[3]:
             raise ValueError(f"M: shape {tuple(M.shape)}, strides {M.stride()} do not fit K")
-    return tkphi_kv_pool(_ptr(K), _ptr(V), _ptr(M), K.shape[0], 0)
+    pool = tkphi_kv_pool(_ptr(K), _ptr(V), _ptr(M), K.shape[0], 0)
+    pool.form, pool.blocks, pool.device = _pool_form(K), 0 if M is None else M.shape[2], _one_device(K=K, V=V, M=M)
+    return pool
 
 
 def make_new_rows(q, k, v, q_rot, inv_freq=None) -> tkphi_new_rows:
@@ -376,7 +435,11 @@ def make_new_rows(q, k, v, q_rot, inv_freq=None) -> tkphi_new_rows:
         st += [t.stride(0), t.stride(1)]
     if inv_freq is not None:
         _tensor("inv_freq", inv_freq, 1, torch.float64)
-    return tkphi_new_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(q_rot), _ptr(inv_freq), *st)
+    io = tkphi_new_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(q_rot), _ptr(inv_freq), *st)
+    io.form = (k.shape[0], (_kv_dtype(k), k.shape[2], k.shape[1]) + (() if q is None else (q.shape[1],)), _one_device(k=k, v=v, q=q, q_rot=q_rot, inv_freq=inv_freq))
+    if inv_freq is not None:
+        io.angles = inv_freq.shape[0]
+    return io
 
 
 def make_attention_rows(q, out, lse=None) -> tkphi_attention_rows:
@@ -390,7 +453,9 @@ def make_attention_rows(q, out, lse=None) -> tkphi_attention_rows:
         _tensor("lse", lse, 2, torch.float32)
         if not lse.is_contiguous() or lse.shape != q.shape[:2]:
             raise ValueError(f"lse: shape {tuple(lse.shape)}, strides {lse.stride()} do not fit q")
-    return tkphi_attention_rows(_ptr(q), _ptr(out), _ptr(lse), q.stride(0), q.stride(1), out.stride(0), out.stride(1))
+    io = tkphi_attention_rows(_ptr(q), _ptr(out), _ptr(lse), q.stride(0), q.stride(1), out.stride(0), out.stride(1))
+    io.form = (q.shape[0], (_kv_dtype(q), q.shape[2], q.shape[1]), _one_device(q=q, out=out, lse=lse))
+    return io
 
 
 def alloc_paged_workspace(nbytes: int, device="cuda"):

@@ -131,3 +131,63 @@ def test_oracle_on_a_case_by_hand():
     M = np.array([[[1.0], [3.0]], [[3.0], [2.0]], [[0.0], [0.0]]])
     assert O.pick_blocks(np.array([[1.0]]), M, [0, 1, 2], 2, 4, 11, 0, 1, 1) == [1, 5]
     assert O.pick_blocks(np.array([[-1.0], [0.5]]), M, [0, 1, 2], 2, 4, 11, 1, 1, 2) == [0, 1, 2, 5]
+
+
+def test_calls_refuse_tensors_that_do_not_fit_config_and_step(monkeypatch):
+    """Rows, heads, channels, type, pool and device are compared before anything is launched.  (On the CPU what fits ends at the device.)"""
+    from paper_2604_05438_amd.paged import PagedCache
+    monkeypatch.setattr(B, "current_stream_ptr", lambda: 0)
+    c = PagedCache(4, 2, 64, 5, 16, 3, 40, 64, block=16, last_blocks=1, device="cpu")
+    c.begin_step({"a": 5, "b": 2})
+
+    def rows(n=7, heads=4, d=64, dtype=torch.bfloat16):
+        return torch.zeros(n, heads, d, dtype=dtype)
+
+    def refused(what, call, *args):
+        with pytest.raises(ValueError, match=what):
+            call(*args)
+    for call in (c.attend, c.attend_blocks):
+        refused("7", call, rows(6), rows(6))
+        refused("heads", call, rows(heads=2), rows(heads=2))
+        refused("channels", call, rows(d=128), rows(d=128))
+        refused("storage type", call, rows(dtype=torch.float32), rows(dtype=torch.float32))
+        refused("storage type", call, rows(dtype=torch.float16), rows(dtype=torch.float16))
+        refused("not on a GPU", call, rows(), rows())
+        refused("not on a GPU", call, rows(9), rows(9))
+        refused("GPUs", call, rows(), rows().to("meta"))
+    kv = dict(heads=2)
+    refused("7", c.append, rows(6), rows(6, **kv), rows(6, **kv), rows(6))
+    refused("heads", c.append, rows(heads=2), rows(**kv), rows(**kv), rows(heads=2))
+    refused("heads", c.append, rows(), rows(), rows(), rows())
+    refused("storage type", c.append, *(rows(heads=h, dtype=torch.float32) for h in (4, 2, 2, 4)))
+    refused("not on a GPU", c.append, rows(), rows(**kv), rows(**kv), rows())
+    refused("not on a GPU", c.append, None, rows(**kv), rows(**kv), None)
+    # the pool, its means and the angles
+    K = torch.zeros(5, 2, 32, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="V"):
+        B.make_pool(K, K[:4])
+    with pytest.raises(ValueError, match="V"):
+        B.make_pool(K, K.transpose(1, 2).contiguous().transpose(1, 2))
+    with pytest.raises(ValueError, match="V"):
+        B.make_pool(K, K.float())
+    cfg = B.make_paged_config(4, 2, 64, "bf16", 0.1, K, K, rot_dim=64, block=16, last_blocks=1)
+    seqs, pages = torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, 2, dtype=torch.int32)
+    step = B.make_step(seqs, pages, 7, 7, 60)
+    pool = B.make_pool(K, K, torch.zeros(5, 2, 2, 64, dtype=torch.bfloat16))
+    for thing in (step, pool):
+        thing.device = 0                     # (as if on a GPU: what is compared after the device)
+
+    def io(angles):
+        x = B.make_new_rows(rows(), rows(**kv), rows(**kv), rows(), inv_freq=torch.zeros(angles, dtype=torch.float64))
+        x.form = (*x.form[:2], 0)
+        return x
+    refused("inv_freq", B.tkphi_kv_append, cfg, step, pool, io(31), 4096, 0, 0)
+    with pytest.raises(B.TkphiError):        # (as it should be: on to the library, which refuses the workspace)
+        B.tkphi_kv_append(cfg, step, pool, io(32), 4096, 0, 0)
+    for other in (torch.zeros(5, 2, 16, 64, dtype=torch.bfloat16), K.transpose(1, 2).contiguous().transpose(1, 2), torch.zeros(5, 4, 32, 64, dtype=torch.bfloat16)):
+        bad = B.make_pool(other, other)
+        bad.device = 0
+        refused("pool", B.tkphi_kv_append, cfg, step, bad, io(32), 4096, 0, 0)
+    bad = B.make_pool(K, K, torch.zeros(5, 2, 1, 64, dtype=torch.bfloat16))
+    bad.device = 0
+    refused("blocks per page", B.tkphi_kv_append, cfg, step, bad, io(32), 4096, 0, 0)
