@@ -32,6 +32,7 @@ class PagedCache:
         self.free = list(range(n_pages - 1, -1, -1))
         self.pages: dict = {}                  # sequence -> its page ids
         self.length: dict = {}                 # sequence -> tokens in the cache
+        self._new: dict = {}                   # sequence -> new tokens of the step that has begun
         bound = B.tkphi_step(0, 0, max_seqs, 1, max_rows, max_rows, max_len, 0)
         self.bounds = (max_seqs, max_rows, max_len)
         self.ws_bytes = max(B.tkphi_paged_workspace_bytes(c, bound) for c in (self.cfg, self.block_cfg))
@@ -77,12 +78,16 @@ class PagedCache:
                                 B.current_stream_ptr())
 
     def end_step(self) -> None:
+        """The step's tokens are in the cache (once; sequences released since begin_step stay away)."""
         for s, m in self._new.items():
             self.length[s] = self.length.get(s, 0) + m
+        self._new = {}
 
     def release(self, seq) -> None:
+        """Gives the sequence's pages back, within a step too."""
         self.free += reversed(self.pages.pop(seq, []))
         self.length.pop(seq, None)
+        self._new.pop(seq, None)
 
     def status(self) -> int:
         return B.tkphi_read_device_status(self.ws.data_ptr(), B.current_stream_ptr())

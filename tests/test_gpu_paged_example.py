@@ -32,3 +32,20 @@ def test_pages_are_taken_and_given_back():
     assert sorted(c.free) == [0, 1, 3, 4] and "a" not in c.length
     c.begin_step({"c": 40})
     assert len(c.pages["c"]) == 3
+
+
+def test_sequences_released_within_a_step_are_gone():
+    from paper_2604_05438_amd.paged import PagedCache
+    c = PagedCache(4, 2, 64, 5, 16, 3, 40, 64, block=16, last_blocks=1, device="cpu")
+    c.begin_step({"a": 17, "b": 3})
+    c.release("a")
+    c.end_step()
+    assert c.length == {"b": 3} and set(c.pages) == {"b"} and len(c.free) == 4
+    c.end_step()                          # (nothing to end)
+    assert c.length == {"b": 3}
+    c.begin_step({"a": 2, "b": 1})
+    assert c._seqs.tolist() == [[0, 2, 0, 0], [3, 1, 2, 0]]
+    c.end_step()
+    c.release("a")
+    c.end_step()
+    assert c.length == {"b": 4} and len(c.free) == 4
