@@ -45,6 +45,8 @@ class PagedCache:
         seqs, row = [], 0
         need = {s: -(-(self.length.get(s, 0) + m) // self.page_tokens) for s, m in new_tokens.items()}
         lengths = [self.length.get(s, 0) + m for s, m in new_tokens.items()]
+        if min(new_tokens.values(), default=0) < 0:
+            raise ValueError(f"negative numbers of new tokens: {new_tokens}")
         if len(new_tokens) > self.bounds[0] or sum(new_tokens.values()) > self.bounds[1] or max(lengths, default=0) > self.bounds[2]:
             raise ValueError(f"step beyond the bounds {self.bounds}")
         if sum(max(0, n - len(self.pages.get(s, ()))) for s, n in need.items()) > len(self.free):

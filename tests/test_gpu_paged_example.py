@@ -49,3 +49,13 @@ def test_sequences_released_within_a_step_are_gone():
     c.release("a")
     c.end_step()
     assert c.length == {"b": 4} and len(c.free) == 4
+
+
+def test_negative_numbers_of_tokens_are_refused():
+    from paper_2604_05438_amd.paged import PagedCache
+    c = PagedCache(4, 2, 64, 5, 16, 3, 40, 64, device="cpu")
+    with pytest.raises(ValueError):
+        c.begin_step({"a": 17, "b": -3})
+    assert not c.pages and len(c.free) == 5
+    c.begin_step({"a": 17, "b": 0})
+    assert c._seqs.tolist() == [[0, 17, 0, 0], [0, 0, 17, 0]]
