@@ -63,21 +63,31 @@ class PagedCache:
         self._seqs = torch.tensor(seqs, dtype=torch.int32).reshape(-1, 4).to(self.device)
         self._table = torch.tensor(table, dtype=torch.int32).reshape(-1, width).to(self.device)
         self._new = dict(new_tokens)
+        self._tables_on = B.current_stream_ptr() if self._seqs.is_cuda else 0
         self.step = B.make_step(self._seqs, self._table, row, max(new_tokens.values(), default=0), max(lengths, default=0))
         return self.step
+
+    def _stream(self) -> int:
+        """The current stream's handle.  The step's tables, which the next step replaces, keep their memory until the work on it is done, also where
+        begin_step ran on another stream."""
+        stream = B.current_stream_ptr()
+        if stream != self._tables_on:
+            for t in (self._seqs, self._table):
+                t.record_stream(torch.cuda.current_stream())
+        return stream
 
     def append(self, q, k, v, q_rot) -> None:
         """Rotates q into q_rot and k into the pages, copies v: rows of the step's new tokens, [rows][heads][channels]."""
         B.tkphi_kv_append(self.cfg, self.step, self.pool, B.make_new_rows(q, k, v, q_rot, inv_freq=self.inv_freq), self.ws.data_ptr(), self.ws_bytes,
-                          B.current_stream_ptr())
+                          self._stream())
 
     def attend(self, q_rot, out, lse=None) -> None:
         B.tkphi_paged_attention(self.cfg, self.step, self.pool, B.make_attention_rows(q_rot, out, lse), self.ws.data_ptr(), self.ws_bytes,
-                                B.current_stream_ptr())
+                                self._stream())
 
     def attend_blocks(self, q_rot, out) -> None:
         B.tkphi_block_attention(self.block_cfg, self.step, self.pool, B.make_attention_rows(q_rot, out), self.ws.data_ptr(), self.ws_bytes,
-                                B.current_stream_ptr())
+                                self._stream())
 
     def end_step(self) -> None:
         """The step's tokens are in the cache (once; sequences released since begin_step stay away)."""

@@ -59,3 +59,35 @@ def test_negative_numbers_of_tokens_are_refused():
     assert not c.pages and len(c.free) == 5
     c.begin_step({"a": 17, "b": 0})
     assert c._seqs.tolist() == [[0, 17, 0, 0], [0, 0, 17, 0]]
+
+
+@pytest.mark.gpu
+def test_calls_on_another_stream_keep_the_tables_of_their_step():
+    """attend waits on a side stream while later steps begin on the default one: their tables must not take the memory of its own."""
+    import torch
+    from paper_2604_05438_amd.paged import PagedCache
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    c = PagedCache(4, 2, 64, 12, 16, 4, 64, 96, dtype="f32")
+
+    def rows(n, heads):
+        return torch.randn(n, heads, 64, generator=gen, device="cuda")
+    c.begin_step({"a": 50})
+    out, q = torch.zeros(2, 50, 4, 64, device="cuda")
+    c.append(rows(50, 4), rows(50, 2), rows(50, 2), q)
+    c.end_step()
+    c.begin_step({"a": 1})
+    one, want, got = torch.zeros(3, 1, 4, 64, device="cuda")
+    c.append(rows(1, 4), rows(1, 2), rows(1, 2), one)
+    c.attend(one, want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        c.attend(one, got)
+    c.end_step()
+    for s in ("b", "c", "d"):
+        c.begin_step({s: 1})
+        c.end_step()
+    assert not side.query()
+    torch.cuda.synchronize()
+    assert c.status() == 0 and torch.equal(got, want) and not torch.equal(want, torch.zeros_like(want))
