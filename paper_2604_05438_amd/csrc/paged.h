@@ -13,7 +13,6 @@ constexpr int kPagedRows = 32;            // query rows (token x query head of o
 // as three for prompts of 4000, but 65 instead of 40 us for 300 tokens over 2000).
 constexpr int chunk_rows(int d) { return d == 64 ? 128 : 256; }
 constexpr int chunk_per_simd(int d) { return d == 64 ? 3 : 2; }      // wavefronts
-constexpr int kChunkSplitRows = 98304;    // rows of all workgroups of the chunk kernel
 constexpr int kMaxSplit = 1024;           // workgroups that the work of one attention call is spread over, at most
 constexpr int kBlockRowGroup = 512;       // query tokens whose block scores the workspace holds at once, at most
 constexpr int kMaxKept = 1024;            // blocks a query sees, at most

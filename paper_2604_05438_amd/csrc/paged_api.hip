@@ -90,7 +90,8 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   g->tile_rows = chunk ? chunk_rows(g->d) : rows <= 16 ? 16 : kPagedRows;
   const int64_t tiles = std::max<int64_t>(1, up(rows, g->tile_rows));
   g->unit_shift = g->dtype == TKPHI_BF16 && !chunk ? 7 : 6;
-  const int64_t units = (int64_t)g->n_seqs * tiles * g->Hkv * up(std::max(g->max_len, 1), 1 << g->unit_shift);      // at most
+  // at most (what counts is whether it passes 2^31: the product of all four bounds need not fit 64 bits)
+  const int64_t units = std::min<int64_t>((int64_t)g->n_seqs * tiles * up(std::max(g->max_len, 1), 1 << g->unit_shift), 1ll << 31) * g->Hkv;
   g->least = 2;      // (1 or 4: 16 and 29 instead of 20 us for 16 tokens of a 3B layer alone, 51 and 47 instead of 43 for four chunks of up to 100)
   if (chunk || tiles > 1 || g->n_seqs > 64 || units >= (1ll << 31))
     g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * tiles);
@@ -112,24 +113,38 @@ void plan_blocks(const tkphi_paged_config* c, PagedGeom* g) {
   g->splits = c->workgroups ? std::min(c->workgroups, 64) : (int)std::max<int64_t>(1, std::min(tiles, up(kBlockSplitHeads, heads)));
 }
 
+// Rows of partials that the attention of any step within these bounds needs: two per workgroup, of as many rows as an item of its kernel has.  Fewer new
+// tokens may take another kernel with shorter items and more workgroups; within one kernel all grows with all bounds.
+size_t partial_rows(const tkphi_paged_config* c, const PagedGeom& bound) {
+  size_t most = 0;
+  for (const int tokens : {16 / bound.G, kPagedRows / bound.G, bound.max_new}) {
+    PagedGeom g = bound;
+    g.max_new = std::min(g.max_new, tokens);
+    plan_attention(c, &g);
+    most = std::max(most, (size_t)g.splits * 2 * g.tile_rows);
+  }
+  return most;
+}
+
 // The largest need of any step within these bounds: every part grows with every bound, but for the block attention's partials, whose number of
-// workgroups per head shrinks with the rows (their product does not pass 512 heads and splits twice over)
+// workgroups per head shrinks with the rows (their product stays below that of the heads, and 512, together)
 PagedSpace space_of(const tkphi_paged_config* c, const PagedGeom& g0) {
   PagedGeom g = g0;
   PagedSpace s;
   const size_t row_bytes = (size_t)(g.d + 2) * sizeof(float);
   const int rg = std::min(g.rows, block_row_group(c));
   const int64_t heads = (int64_t)rg * g.Hkv;
-  plan_attention(c, &g);
   const int64_t items = (int64_t)g.rows * g.G / 16 + g.n_seqs;        // (a plan is at most that long, whichever kernel runs)
   int64_t block_slots = 0;
-  g.row_group = rg;
-  plan_blocks(c, &g);
-  if (g.block) block_slots = heads * (c->workgroups ? std::min(c->workgroups, 64) : 1) + (c->workgroups ? 0 : 2 * kBlockSplitHeads + g.Hkv * 64);
+  if (g.block) {
+    g.row_group = 1;                                                  // as many workgroups per head as there may be
+    plan_blocks(c, &g);
+    block_slots = c->workgroups ? heads * g.splits : std::min(heads * g.splits, heads + kBlockSplitHeads);
+  }
   s.arrived = 256;
   s.joins = s.arrived + padded(kMaxSplit * sizeof(uint32_t));
   s.partial = s.joins + padded(kMaxSplit * 2 * sizeof(int4));
-  s.plan_end = s.partial + padded(std::max<size_t>((size_t)std::max(kMaxSplit * kPagedRows, c->workgroups ? c->workgroups * chunk_rows(128) : kChunkSplitRows) * 2, (size_t)block_slots * 16) * row_bytes);
+  s.plan_end = s.partial + padded(std::max<size_t>(partial_rows(c, g0), (size_t)block_slots * 16) * row_bytes);
   s.plan_item = s.plan_end + padded((size_t)items * sizeof(int64_t));
   s.keys = s.plan_item + padded((size_t)items * sizeof(int2) + 256);
   s.list = s.keys + padded(g.block ? (size_t)heads * g.max_blocks * sizeof(uint64_t) : 0);

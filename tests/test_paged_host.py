@@ -191,3 +191,21 @@ def test_calls_refuse_tensors_that_do_not_fit_config_and_step(monkeypatch):
     bad = B.make_pool(K, K, torch.zeros(5, 2, 1, 64, dtype=torch.bfloat16))
     bad.device = 0
     refused("blocks per page", B.tkphi_kv_append, cfg, step, bad, io(32), 4096, 0, 0)
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,d,step,most", [
+    # (sequences, rows, max_new, max_len); two partials per workgroup: as many of those as the step has units of 64 (bf16 single tokens: 128) cached tokens, or fit the GPU
+    (0, 1, 1, 64, (1, 1, 1, 4096), 64 * 2 * 16),
+    (0, 1, 1, 64, (1, 1, 1, 100), 2 * 2 * 16),
+    (1, 32, 8, 64, (1, 1, 1, 4096), 8 * 32 * 2 * 16),
+    (1, 24, 8, 128, (32, 32, 1, 65000), 512 * 2 * 16),
+    (0, 24, 8, 128, (4, 1200, 300, 16000), 512 * 2 * 32),
+    (1, 24, 8, 128, (1, 2048, 2048, 32000), 256 * 2 * 256),
+    (1, 32, 8, 64, (4, 8000, 4000, 4000), 768 * 2 * 128),
+])
+def test_workspace_is_what_the_steps_need(dtype, hq, hkv, d, step, most):
+    cfg = B.tkphi_paged_config(hq, hkv, d, dtype, 0.1, 64, 1 << 20, 1 << 14, 1 << 10, 0)
+    n, rows, new, length = step
+    items = rows * hq // hkv // 16 + n
+    size = B.tkphi_paged_workspace_bytes(cfg, B.tkphi_step(16, 16, n, 9, rows, new, length, 0))
+    assert 0 < size <= most * (d + 2) * 4 + items * 16 + 4096 + 32768 + 6 * 256
