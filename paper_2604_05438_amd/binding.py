@@ -100,6 +100,7 @@ class tkphi_kv_pool(C.Structure):
 
 
 class tkphi_new_rows(C.Structure):
+    heads, angles = "kv_q_heads", 1 << 30          # (make_new_rows: which note of the config the heads have to match, elements of inv_freq)
     _fields_ = [
         ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_rot", C.c_void_p), ("inv_freq", C.c_void_p),
         ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
@@ -269,8 +270,8 @@ def _fits(cfg, step, pool, io, heads) -> None:
 
 def tkphi_kv_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_new_rows, workspace_ptr: int,
                     workspace_bytes: int, stream: int) -> None:
-    _fits(cfg, step, pool, io, "kv_q_heads" if io.q else "kv_heads")
-    if 2 * getattr(io, "angles", 1 << 30) < cfg.rot_dim:
+    _fits(cfg, step, pool, io, io.heads)
+    if 2 * io.angles < cfg.rot_dim:
         raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
     _check(lib().tkphi_kv_append(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
 
@@ -437,6 +438,8 @@ def make_new_rows(q, k, v, q_rot, inv_freq=None) -> tkphi_new_rows:
         _tensor("inv_freq", inv_freq, 1, torch.float64)
     io = tkphi_new_rows(_ptr(q), _ptr(k), _ptr(v), _ptr(q_rot), _ptr(inv_freq), *st)
     io.form = (k.shape[0], (_kv_dtype(k), k.shape[2], k.shape[1]) + (() if q is None else (q.shape[1],)), _one_device(k=k, v=v, q=q, q_rot=q_rot, inv_freq=inv_freq))
+    if q is None:
+        io.heads = "kv_heads"
     if inv_freq is not None:
         io.angles = inv_freq.shape[0]
     return io
