@@ -369,8 +369,9 @@ int32_t tkphi_budget_mid(int64_t L, int32_t r_bp, int32_t n_sink, int32_t n_tail
  *                          mean keys score highest against them
  * Token t of a sequence is row t % page_tokens of page pages[seq][t / page_tokens].  A step brings
  * new_tokens more tokens per sequence behind the `cached` that are there; the tokens of a sequence
- * stand one behind another in the rows of q, k, v and out, and no two sequences share a row.  tkphi_kv_append comes first: the attention
- * calls read the new tokens' keys and values from their pages, like all others.
+ * stand one behind another in the rows of q, k, v and out, and no two sequences share a row.
+ * tkphi_kv_append comes first: the attention calls read the new tokens' keys and values from their pages, like
+ * all others.
  *
  * All structs below are HOST structs, read at call time; the pointers inside are DEVICE pointers.
  * The calls allocate nothing, only enqueue, and may be captured into a HIP graph (the lengths are read
@@ -458,7 +459,9 @@ size_t tkphi_paged_workspace_bytes(const tkphi_paged_config* cfg, const tkphi_st
 tkphi_status tkphi_kv_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
                              const tkphi_new_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* out = softmax(score_scale q K^T) V and lse over the tokens t <= cached + i of the sequence (and t > cached + i - window). */
+/* out = softmax(score_scale q K^T) V and lse over the tokens t <= cached + i of the sequence (and t > cached + i - window).
+ * With bf16 storage each weight is rounded to bf16 for its product with V, and out is divided by the sum of the weights as
+ * rounded (lse takes them unrounded): a mean of the values seen, off by at most about 2^-8 sum w |v - out| / sum w, then rounded. */
 tkphi_status tkphi_paged_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
                                    const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
 

@@ -4,10 +4,11 @@
 // of tokens against 16 (or 32) query rows, S^T = K Q^T, then O^T += V^T P^T.  The rows of S^T that a lane holds are exactly the inner
 // indices it has to deliver of P^T, so P never leaves its lane; V passes through LDS, where the bf16 form reads it transposed.
 // The query rows of an item are the new tokens times the query heads of one KV head (every cached row is read once for all of
-// them); the work of all items is cut into equal pieces along the tokens, and the workgroup that finishes an item last joins its pieces.
+// them); the work of all items is cut into equal pieces along the tokens, and the workgroup that finishes an item last joins its pieces (with a plan,
+// paged_join_kernel does).
 //
 // Bound by the read stream where there is much of it: a step of 32 sequences of a 3B layer, 720000 cached tokens (2.96 GB), 455 us = 6.5 TB/s; five tokens
-// each of 8 sequences (283 MB) 62 us.  Short calls are a chain of round trips: a 1B layer over 4002 tokens 9.8 us, of which sequences 0.7, page ids and
+// each of 8 sequences (283 MB) 62 us.  Short calls are a chain of round trips: a 1B layer over 4002 tokens 9.4 us, of which sequences 0.7, page ids and
 // rows 2.5, the join of the wavefronts 0.6, partials and their count 1.5, the join of 32 pieces 2.5.
 #include "paged_attention.h"
 
@@ -396,7 +397,9 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
 // UNIFORM: 8 tokens always lie in one page
 template <typename T, int D, int RT, bool PLAN, bool UNIFORM>
 __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
-  constexpr bool STREAM = !PLAN;                                   // (several items of a sequence read the same rows)
+  // Non-temporal loads where the cache is read once for sure; with a plan several items of a sequence may read the same rows.  (128 sequences of one token have a
+  // plan too: 420 us; 375 with non-temporal loads.)
+  constexpr bool STREAM = !PLAN;
   using Wave = WaveAttend<T, D, RT, STREAM>;
   constexpr int WAVES = kPagedThreads / 64;
   __shared__ __align__(16) char lds[attend_lds<T, D, RT, STREAM>()];

@@ -5,10 +5,10 @@
 // straight to LDS a tile ahead, 64 of them at a time; S^T = K Q^T and O^T += V^T P^T on v_mfma_f32_32x32x16_bf16.  A lane holds all of S^T for one query row but the half
 // its partner lane 32 further has, and exactly what it has to deliver of P^T: maximum and sum take one exchange, P none.
 //
-// 2048 tokens over 30000 cached ones (24 / 8 heads of 128) 0.85 ms = 917 TFLOP/s, three quarters of what a large library product reaches on the same card;
-// four prompts of 1762 to 3604 tokens (32 / 8 heads of 64) 0.33 ms.  The matrix cores are busy 35 to 38 % of the time; without loads from memory the
-// former takes 6 % less, without exponentials 7, without the reads of K from LDS 11, in another order of instructions the same: what is left are
-// the dependencies of two wavefronts per SIMD (a wavefront alone with 64 rows and 512 registers: 1.65 ms).
+// 2048 tokens over 30000 cached ones (24 / 8 heads of 128) 0.84 to 0.96 ms, by the card: 810 to 930 TFLOP/s, two thirds to three quarters of what a large
+// library product reaches; four prompts of 1762 to 3604 tokens (32 / 8 heads of 64) 0.33 to 0.36 ms.  The matrix cores are busy 39 % of the time (19 % at d = 64);
+// without loads from memory the former takes 6 % less, without exponentials 7, without the reads of K from LDS 11, in another order of instructions the same:
+// what is left are the dependencies of two wavefronts per SIMD (a wavefront alone with 64 rows and 512 registers: 1.65 ms).
 #include "paged_attention.h"
 
 namespace tkphi {
@@ -48,8 +48,9 @@ struct ChunkTile {
 };
 static_assert(ChunkTile<128>::LOADS == 2 * ChunkTile<128>::HALVES && ChunkTile<64>::LOADS == 2 * ChunkTile<64>::HALVES, "");
 
-// Adds the two weights of a register, as they were rounded.  (On the matrix cores, as the split kernel does, the sum would take 16 registers that are not
-// there; unpacked and added: 924 instead of 895 us for the 2048 tokens over 30000, 360 instead of 330 for the prompts; without this sum 881 and 316.)
+// Adds the two weights of a register, as they were rounded.  (2048 tokens over 30000 / four prompts / a prompt of 16000 tokens of a 1B layer, us: 868 / 327 / 1542; without
+// this sum 849 / 314 / 1461; unpacked and added 3 and 9 % more; as 4 x 4 products with ones on the matrix cores 876 / 327 / 1498, but 45.5 instead of 43.9 for 300
+// tokens over 2000, by registers spilled; as one more channel, as in the split kernel, it would take 16 registers that are not there.)
 __device__ __forceinline__ float add_rounded(uint32_t pair, float sum) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pair), __builtin_bit_cast(bf16x2_t, 0x3f803f80u), sum, false);
 }
