@@ -471,6 +471,64 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_config* cfg, const tkphi_st
 tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
                                    const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- norms of query and key heads; the paged cache in 8 bits ---------------------------------------
+ *   tkphi_norm_append           tkphi_kv_append of queries and keys that are normed head by head first
+ *   tkphi_quant_append          the same (norms optional) into a cache of 8-bit codes
+ *   tkphi_quant_attention       tkphi_paged_attention over it
+ *   tkphi_quant_block_attention tkphi_block_attention over it
+ *   tkphi_quant_read            its tokens as rows, in any layout (as the calls on contiguous caches read them)
+ * Everything said above holds for them: steps, checks, status bits, workspaces (those of tkphi_paged_workspace_bytes), streams, capture.
+ *
+ * The cache in 8 bits.  A key or value row of a token and KV head is d_head codes in OCP e4m3 and a byte b, 1 <= b <= 254; it stands for
+ * code x 2^(b - 127), which is a bf16 number.  tkphi_quant_append takes the smallest power of two for which the row's largest finite
+ * element is at most 448 times it, within b = 10 .. 247 (a row of zeros: 10), so that an element x is stored within half a step of e4m3 (2^-4 |x|, or
+ * 2^-10 of the power of two where that is more); elements that are not finite become NaN.
+ * Rows, queries and outputs are bf16 (kv_dtype TKPHI_BF16; others: TKPHI_EUNSUPPORTED).  The config's strides count elements, here bytes, multiples of 16.
+ * Mean keys are bf16, over the keys as stored. */
+typedef struct tkphi_quant_pool {
+  void* K;               /* codes of keys and values, strides of the config                         */
+  void* V;
+  void* scales;          /* uint8 [n_pages][n_kv_heads][page_tokens][2]: b of the key, b of the value */
+  void* M;               /* as in tkphi_kv_pool                                                     */
+  int32_t n_pages;
+  int32_t reserved;      /* 0 */
+} tkphi_quant_pool;
+
+/* y = x / sqrt(mean of x^2 over the head's channels + eps) * (weight + weight_offset), in 32 bits; the rotation follows before the result is rounded. */
+typedef struct tkphi_head_norms {
+  const void* q_weight;  /* [n_q_heads][d_head] kv_dtype, stride below; NULL: y = x / sqrt(..)      */
+  const void* k_weight;  /* [n_kv_heads][d_head]                                                    */
+  int64_t q_weight_head; /* elements between heads; 0: all heads share [d_head]                     */
+  int64_t k_weight_head;
+  float eps;             /* > 0, a normal number                                                    */
+  float weight_offset;   /* 1 for weights that are stored as w - 1                                  */
+} tkphi_head_norms;
+
+typedef struct tkphi_read_rows {
+  void* k;               /* [rows][n_kv_heads][d_head]; either may be NULL                          */
+  void* v;
+  int64_t k_row, k_head, v_row, v_head;
+} tkphi_read_rows;
+
+tkphi_status tkphi_norm_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool, const tkphi_new_rows* io,
+                               const tkphi_head_norms* norms, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* norms may be NULL: q and k as they are. */
+tkphi_status tkphi_quant_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool, const tkphi_new_rows* io,
+                                const tkphi_head_norms* norms, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* What tkphi_paged_attention gives for a bf16 cache of the values that the codes stand for. */
+tkphi_status tkphi_quant_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool,
+                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+tkphi_status tkphi_quant_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool,
+                                         const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Tokens [cached, cached + new_tokens) of every sequence of the step, exactly, to the rows that the step gives them.  Tokens of absent pages read as zeros and
+ * are recorded (TKPHI_DEV_BAD_PAGE). */
+tkphi_status tkphi_quant_read(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool, const tkphi_read_rows* io,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static, never-null strings. */
 const char* tkphi_status_string(int32_t status);
 const char* tkphi_last_error(void);

@@ -18,6 +18,31 @@ def rotate(x: np.ndarray, pos: int, inv_freq: np.ndarray, adjacent: bool) -> np.
     return y
 
 
+def head_norm(x: np.ndarray, weight, eps: float, offset: float) -> np.ndarray:
+    """x [..., d] over the root of its mean square, times weight + offset (None: as it is)"""
+    y = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    return y if weight is None else y * (weight + offset)
+
+
+def e4m3(y: np.ndarray) -> np.ndarray:
+    """The nearest numbers of e4m3 (three bits behind the point from 2^-6 on, steps of 2^-9 below, ties to even), |y| <= 448; NaN stays"""
+    with np.errstate(divide="ignore"):
+        step = np.exp2(np.maximum(np.floor(np.log2(np.abs(y))), -6.0) - 3.0)
+    step = np.where(np.isnan(step), 1.0, step)
+    return np.rint(y / step) * step
+
+
+def quantise(x: np.ndarray):
+    """Rows [..., d] -> codes as the numbers they are, exponent bytes b: code * 2^(b - 127) stands for x.  The smallest power of two of which the row's largest
+    finite element is at most 448, b within 10 .. 247."""
+    x = np.where(np.isfinite(x), x, np.nan)
+    top = np.nan_to_num(np.abs(x), nan=0.0).max(-1)
+    b = np.full(top.shape, 10)
+    for _ in range(237):
+        b = np.where(top > 448 * np.exp2(b - 127.0), b + 1, b)
+    return e4m3(x / np.exp2(b - 127.0)[..., None]), b
+
+
 def gather(pool: np.ndarray, table, length: int):
     """Rows of the first `length` tokens [KV heads][length][d], and which of them are there."""
     page = pool.shape[2]

@@ -29,6 +29,7 @@ EXPORTS = (
     "tkphi_read_device_status", "tkphi_budget_paper", "tkphi_budget_mid", "tkphi_status_string",
     "tkphi_last_error",
     "tkphi_paged_workspace_bytes", "tkphi_kv_append", "tkphi_paged_attention", "tkphi_block_attention",
+    "tkphi_norm_append", "tkphi_quant_append", "tkphi_quant_attention", "tkphi_quant_block_attention", "tkphi_quant_read",
 )
 
 
@@ -115,6 +116,23 @@ class tkphi_attention_rows(C.Structure):
     ]
 
 
+class tkphi_quant_pool(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("scales", C.c_void_p), ("M", C.c_void_p), ("n_pages", C.c_int32), ("reserved", C.c_int32)]
+
+
+class tkphi_head_norms(C.Structure):
+    _fields_ = [
+        ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_weight_head", C.c_int64), ("k_weight_head", C.c_int64),
+        ("eps", C.c_float), ("weight_offset", C.c_float),
+    ]
+
+
+class tkphi_read_rows(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("k_row", C.c_int64), ("k_head", C.c_int64), ("v_row", C.c_int64), ("v_head", C.c_int64),
+    ]
+
+
 _lib = None
 _lock = threading.Lock()
 
@@ -162,6 +180,14 @@ def lib() -> C.CDLL:
             f = getattr(L, name)
             f.restype = C.c_int
             f.argtypes = [pcfg, stepp, poolp, C.POINTER(rows), C.c_void_p, C.c_size_t, C.c_void_p]
+        qpoolp, normsp = C.POINTER(tkphi_quant_pool), C.POINTER(tkphi_head_norms)
+        for name, pool, rows in (("tkphi_norm_append", poolp, [C.POINTER(tkphi_new_rows), normsp]), ("tkphi_quant_append", qpoolp, [C.POINTER(tkphi_new_rows), normsp]),
+                                 ("tkphi_quant_attention", qpoolp, [C.POINTER(tkphi_attention_rows)]),
+                                 ("tkphi_quant_block_attention", qpoolp, [C.POINTER(tkphi_attention_rows)]),
+                                 ("tkphi_quant_read", qpoolp, [C.POINTER(tkphi_read_rows)])):
+            f = getattr(L, name)
+            f.restype = C.c_int
+            f.argtypes = [pcfg, stepp, pool, *rows, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
         return L
 
@@ -288,6 +314,58 @@ def tkphi_block_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi
     _check(lib().tkphi_block_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
 
 
+def _fits_norms(cfg, io, norms) -> None:
+    """The norms' weights against the config (see _fits)"""
+    if norms is None:
+        return
+    try:
+        (q_heads, q_form), (k_heads, k_form), device, on = norms.q, norms.k, norms.device, io.form[2]
+    except AttributeError:
+        return
+    want = (cfg.kv_dtype, cfg.d_head)
+    if q_form not in (None, want) or k_form not in (None, want) or q_heads not in (0, cfg.n_q_heads) or k_heads not in (0, cfg.n_kv_heads):
+        raise ValueError(f"norms with weights of (heads, (storage type, channels)) {norms.q}, {norms.k} for a config of {cfg.n_q_heads}, {cfg.n_kv_heads} heads, {want}")
+    if device is not None and device != on:
+        raise ValueError(f"norms on GPU {device}, rows on {on} (-1: not on a GPU)")
+
+
+def _append(call, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream) -> None:
+    _fits(cfg, step, pool, io, io.heads)
+    _fits_norms(cfg, io, norms)
+    if 2 * io.angles < cfg.rot_dim:
+        raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
+    _check(call(cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream))
+
+
+def tkphi_norm_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_new_rows, norms: tkphi_head_norms, workspace_ptr: int,
+                      workspace_bytes: int, stream: int) -> None:
+    _append(lib().tkphi_norm_append, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream)
+
+
+def tkphi_quant_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_quant_pool, io: tkphi_new_rows, norms, workspace_ptr: int,
+                       workspace_bytes: int, stream: int) -> None:
+    """norms: tkphi_head_norms or None"""
+    _append(lib().tkphi_quant_append, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream)
+
+
+def tkphi_quant_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_quant_pool, io: tkphi_attention_rows, workspace_ptr: int,
+                          workspace_bytes: int, stream: int) -> None:
+    _fits(cfg, step, pool, io, "q_heads")
+    _check(lib().tkphi_quant_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
+
+
+def tkphi_quant_block_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_quant_pool, io: tkphi_attention_rows, workspace_ptr: int,
+                                workspace_bytes: int, stream: int) -> None:
+    _fits(cfg, step, pool, io, "q_heads")
+    _check(lib().tkphi_quant_block_attention(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
+
+
+def tkphi_quant_read(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_quant_pool, io: tkphi_read_rows, workspace_ptr: int, workspace_bytes: int,
+                     stream: int) -> None:
+    _fits(cfg, step, pool, io, "kv_heads")
+    _check(lib().tkphi_quant_read(cfg, step, pool, io, workspace_ptr, workspace_bytes, stream))
+
+
 # ---- marshalling helpers (device memory via torch) -----------------------------------------
 def make_config(n_q_heads, n_kv_heads, d_head, d_phi, n_sink, n_tail, dtype, score_scale, phi_in_scale,
                 phi_norm_coef, cache_features=0, phi_kind=0, d_emb=0, max_gen=0, tuning=None) -> tkphi_config:
@@ -356,6 +434,9 @@ def _storage_type(kv_dtype):
     return {TKPHI_BF16: torch.bfloat16, TKPHI_F32: torch.float32}[kv_dtype]
 
 
+E4M3 = 8        # (note of a pool in 8 bits, where others have their tkphi_dtype)
+
+
 def _kv_dtype(t):
     import torch
     if t.dtype not in (torch.bfloat16, torch.float32):
@@ -365,7 +446,8 @@ def _kv_dtype(t):
 
 def _pool_form(K):
     """Storage type, channels, heads, tokens and strides; a stride over one element does not matter (None)."""
-    return (_kv_dtype(K), K.shape[3], K.shape[1], K.shape[2], *(K.stride(i) if K.shape[i] > 1 else None for i in range(3)))
+    import torch
+    return (E4M3 if K.dtype == torch.float8_e4m3fn else _kv_dtype(K), K.shape[3], K.shape[1], K.shape[2], *(K.stride(i) if K.shape[i] > 1 else None for i in range(3)))
 
 
 def _one_device(**tensors):
@@ -379,10 +461,11 @@ def _one_device(**tensors):
 def make_paged_config(n_q_heads, n_kv_heads, d_head, dtype, score_scale, K, V, window=0, rot_dim=0, rot_adjacent=False, block=0,
                       first_blocks=0, last_blocks=0, top_blocks=0, workgroups=0) -> tkphi_paged_config:
     """K, V: the pool's tensors as [pages][KV heads][tokens per page][channels], in any memory order with adjoining channels and
-    the same strides."""
+    the same strides; of dtype, or codes (torch.float8_e4m3fn) for the calls on the cache in 8 bits, which take bf16 rows."""
+    import torch
     kv = {"bf16": TKPHI_BF16, "f32": TKPHI_F32}[dtype] if isinstance(dtype, str) else int(dtype)
     for name, t in (("K", K), ("V", V)):
-        _tensor(name, t, 4, _storage_type(kv))
+        _tensor(name, t, 4, torch.float8_e4m3fn if K.dtype == torch.float8_e4m3fn and kv == TKPHI_BF16 else _storage_type(kv))
         if t.shape != K.shape or t.stride() != K.stride() or t.shape[1] != n_kv_heads or t.shape[3] != d_head:
             raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()} do not fit K and the heads")
     cfg = tkphi_paged_config(int(n_q_heads), int(n_kv_heads), int(d_head), kv, float(score_scale), K.shape[2], K.stride(0), K.stride(1),
@@ -409,17 +492,72 @@ def make_step(seqs, pages, rows: int, max_new: int, max_len: int) -> tkphi_step:
 
 def make_pool(K, V, M=None) -> tkphi_kv_pool:
     """K, V as for make_paged_config; M: mean keys [pages][KV heads][blocks per page][channels], contiguous, or None."""
+    _kv_dtype(K)
+    _pool_tensors(K, V, M, K.dtype)
+    pool = tkphi_kv_pool(_ptr(K), _ptr(V), _ptr(M), K.shape[0], 0)
+    pool.form, pool.blocks, pool.device = _pool_form(K), 0 if M is None else M.shape[2], _one_device(K=K, V=V, M=M)
+    return pool
+
+
+def _pool_tensors(K, V, M, mean_type) -> None:
     for name, t in (("K", K), ("V", V)):
         _tensor(name, t, 4, K.dtype)
         if t.shape != K.shape or t.stride() != K.stride():
             raise ValueError(f"{name}: shape {tuple(t.shape)}, strides {t.stride()} are not those of K")
     if M is not None:
-        _tensor("M", M, 4, K.dtype)
+        _tensor("M", M, 4, mean_type)
         if not M.is_contiguous() or M.shape[:2] != K.shape[:2] or M.shape[3] != K.shape[3]:
             raise ValueError(f"M: shape {tuple(M.shape)}, strides {M.stride()} do not fit K")
-    pool = tkphi_kv_pool(_ptr(K), _ptr(V), _ptr(M), K.shape[0], 0)
-    pool.form, pool.blocks, pool.device = _pool_form(K), 0 if M is None else M.shape[2], _one_device(K=K, V=V, M=M)
+
+
+def make_quant_pool(K, V, scales, M=None) -> tkphi_quant_pool:
+    """K, V: codes (torch.float8_e4m3fn), as for make_paged_config; scales: uint8 [pages][KV heads][tokens per page][2], contiguous, the exponent bytes of
+    key and value; M: bf16, as for make_pool."""
+    import torch
+    _tensor("K", K, 4, torch.float8_e4m3fn)
+    _pool_tensors(K, V, M, torch.bfloat16)
+    _tensor("scales", scales, 4, torch.uint8)
+    if not scales.is_contiguous() or scales.shape != (*K.shape[:3], 2):
+        raise ValueError(f"scales: shape {tuple(scales.shape)}, strides {scales.stride()} do not fit K {tuple(K.shape)}")
+    pool = tkphi_quant_pool(_ptr(K), _ptr(V), _ptr(scales), _ptr(M), K.shape[0], 0)
+    pool.form, pool.blocks, pool.device = _pool_form(K), 0 if M is None else M.shape[2], _one_device(K=K, V=V, scales=scales, M=M)
     return pool
+
+
+def make_head_norms(q_weight, k_weight, eps: float, offset: float = 0.0) -> tkphi_head_norms:
+    """Weights [channels], shared by all heads, or [heads][channels], in the rows' type, or None for ones (offset does not count there)."""
+    strides, notes = [], []
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _tensor(name, w, 1 if w.dim() == 1 else 2)
+        strides.append(0 if w is None or w.dim() == 1 else w.stride(0))
+        notes.append((0, None) if w is None else (0 if w.dim() == 1 else w.shape[0], (_kv_dtype(w), w.shape[-1])))
+        if w is not None and w.dim() == 2 and w.shape[0] > 1 and w.stride(0) < w.shape[1]:
+            raise ValueError(f"{name}: strides {w.stride()}")
+    norms = tkphi_head_norms(_ptr(q_weight), _ptr(k_weight), *strides, float(eps), float(offset))
+    norms.q, norms.k = notes
+    norms.device = None if q_weight is None and k_weight is None else _one_device(q_weight=q_weight, k_weight=k_weight)
+    return norms
+
+
+def make_read_rows(k, v) -> tkphi_read_rows:
+    """[rows][KV heads][channels] bf16; either may be None"""
+    import torch
+    if k is None and v is None:
+        raise ValueError("k and v are None")
+    st, form = [], None
+    for name, t in (("k", k), ("v", v)):
+        if t is None:
+            st += [0, 0]
+            continue
+        _tensor(name, t, 3, torch.bfloat16)
+        if form is not None and form != t.shape:
+            raise ValueError(f"v: shape {tuple(t.shape)} does not fit k {tuple(form)}")
+        form = t.shape
+        st += [t.stride(0), t.stride(1)]
+    io = tkphi_read_rows(_ptr(k), _ptr(v), *st)
+    io.form = (form[0], (TKPHI_BF16, form[2], form[1]), _one_device(k=k, v=v))
+    return io
 
 
 def make_new_rows(q, k, v, q_rot, inv_freq=None) -> tkphi_new_rows:

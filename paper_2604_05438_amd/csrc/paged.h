@@ -1,4 +1,4 @@
-// Shared by the kernels on the paged key/value cache (paged_append, paged_attention, paged_blocks) and their host layer (paged_api).
+// Shared by the kernels on the paged key/value cache (paged_append, paged_attention, paged_blocks, paged_read) and their host layer (paged_api).
 #pragma once
 
 #include "tkphi_internal.h"
@@ -73,6 +73,14 @@ struct PagedGeom {
   const char *k, *v;
   const double* inv_freq;
   int64_t k_row, k_head, v_row, v_head;
+  // append: norms of query and key heads
+  int normed;
+  float eps, w_offset;
+  const char *qw, *kw;                    // weights, nullptr: ones; bytes between heads
+  int64_t qw_head, kw_head;
+  // the cache in 8 bits: scale bytes [n_pages][Hkv][tokens per page] (key, value); nullptr where the cache has the rows' type
+  uint16_t* S;
+  char *k_out, *v_out;                    // tkphi_quant_read (strides k_row, .. v_head)
   // blocks
   char* M;
   int block, first, last, top;
@@ -84,12 +92,43 @@ struct PagedGeom {
 };
 
 void launch_paged_append(const PagedGeom& g, hipStream_t s);
+void launch_paged_read(const PagedGeom& g, hipStream_t s);
 void launch_paged_attention(const PagedGeom& g, hipStream_t s);
 void launch_paged_chunk(const PagedGeom& g, hipStream_t s);
 void launch_block_select(const PagedGeom& g, hipStream_t s);
 void launch_block_attention(const PagedGeom& g, hipStream_t s);
 
+// A row of the cache in 8 bits: e4m3 codes, and a byte b: the row is codes x 2^(b - 127), the smallest power for which the largest one fits.  A finer scale
+// would gain nothing, the codes are floating point numbers themselves; codes times a power of two are bf16 numbers, which the
+// conversion instruction delivers, so everything behind it is what it is for a bf16 cache.
+struct Code8 {};
+// the type that rows and outputs have, and bytes of a cached element
+template <typename T> struct Cached {
+  using Row = T;
+  static constexpr int bytes = (int)sizeof(T);
+  static constexpr bool codes = false, bf16 = sizeof(T) == 2;
+};
+template <> struct Cached<Code8> {
+  using Row = uint16_t;
+  static constexpr int bytes = 1;
+  static constexpr bool codes = true, bf16 = true;
+};
+constexpr int kLeastScale = 10, kMostScale = 247;        // bytes (2^-117: codes times that are no smaller than the least bf16 number of full precision)
+
 #ifdef __HIPCC__
+// The scale of a key (low byte) or value (high byte) as a number
+__device__ __forceinline__ float key_scale(uint32_t both) { return __uint_as_float((both & 0xffu) << 23); }
+__device__ __forceinline__ float value_scale(uint32_t both) { return __uint_as_float(both >> 8 << 23); }
+// 8 codes times a scale, as bf16
+__device__ __forceinline__ u32x4 decode8(uint32_t a, uint32_t b, float scale) {
+  return (u32x4){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true))};
+}
+// Index of the scales of row `row` of page id for KV head h
+__device__ __forceinline__ int64_t scale_at(const PagedGeom& g, int64_t id, int h, int row) { return (id * g.Hkv + h) * g.by_page.d + row; }
+
 __device__ __forceinline__ int page_of(const PagedGeom& g, int t) { return g.by_page(t); }
 
 // A sequence as the kernels take it: new_tokens 0 if its description is out of bounds.

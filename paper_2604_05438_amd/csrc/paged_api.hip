@@ -23,7 +23,8 @@ tkphi_status hip_status(hipError_t e, const char* what) {
 }
 
 // Config and step: everything a call and the workspace's size have in common
-tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, PagedGeom* g) {
+// (codes: strides of the pool are those of a cache in 8 bits.  One that is right there is right for the rows' type too.)
+tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, PagedGeom* g, bool codes = false) {
   if (!c || !st) { set_error("cfg or step is null"); return TKPHI_EINVAL; }
   if (c->kv_dtype != TKPHI_F32 && c->kv_dtype != TKPHI_BF16) { set_error("kv_dtype=%d is not a tkphi_dtype", c->kv_dtype); return TKPHI_EINVAL; }
   if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads != 0 || c->n_q_heads / c->n_kv_heads > kMaxGroup) {
@@ -33,7 +34,8 @@ tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, Pag
   if (c->d_head != 64 && c->d_head != 128) { set_error("d_head=%d unsupported (64 or 128)", c->d_head); return TKPHI_ESHAPE; }
   if (!(c->score_scale > 0.f) || !std::isfinite(c->score_scale)) { set_error("score_scale=%g has to be positive and finite", c->score_scale); return TKPHI_EINVAL; }
   if (c->page_tokens < 1) { set_error("page_tokens=%d has to be positive", c->page_tokens); return TKPHI_ESHAPE; }
-  const int64_t es = c->kv_dtype == TKPHI_BF16 ? 2 : 4;
+  if (codes && c->kv_dtype != TKPHI_BF16) { set_error("the calls on the cache in 8 bits take bf16 rows (kv_dtype=%d)", c->kv_dtype); return TKPHI_EUNSUPPORTED; }
+  const int64_t es = codes ? 1 : c->kv_dtype == TKPHI_BF16 ? 2 : 4;
   for (const int64_t s : {c->stride_page, c->stride_head, c->stride_tok})
     if (s < 0 || s > (1ll << 48) || s * es % 16 != 0) { set_error("pool stride of %lld elements (need >= 0, 16-byte multiple)", (long long)s); return TKPHI_EALIGN; }
   if ((c->page_tokens > 1 && c->stride_tok < c->d_head) || (c->n_kv_heads > 1 && c->stride_head < c->d_head)) {
@@ -178,27 +180,38 @@ tkphi_status check_rows(const PagedGeom& g, const void* p, const char* name, int
   return TKPHI_OK;
 }
 
-// What all three calls check after the config; nothing is left to do where *empty
-tkphi_status check_call(const tkphi_paged_config* c, const tkphi_step* st, const tkphi_kv_pool* pool, const void* io, void* ws, size_t ws_bytes,
+// A pool of either kind: scales null for one of the rows' type
+struct Pool {
+  bool codes, given;
+  void *K, *V, *S, *M;
+  int32_t n_pages, reserved;
+};
+Pool pool_of(const tkphi_kv_pool* p) { return p ? Pool{false, true, p->K, p->V, nullptr, p->M, p->n_pages, p->reserved} : Pool{}; }
+Pool pool_of(const tkphi_quant_pool* p) { return p ? Pool{true, true, p->K, p->V, p->scales, p->M, p->n_pages, p->reserved} : Pool{true}; }
+
+// What all calls check after the config; nothing is left to do where *empty
+tkphi_status check_call(const tkphi_paged_config* c, const tkphi_step* st, const Pool& pool, const void* io, void* ws, size_t ws_bytes,
                         PagedGeom* g, bool* empty) {
-  tkphi_status r = check_config(c, st, g);
+  tkphi_status r = check_config(c, st, g, pool.codes);
   if (r != TKPHI_OK) return r;
-  if (!pool || !io) { set_error("pool or io is null"); return TKPHI_EINVAL; }
+  if (!pool.given || !io) { set_error("pool or io is null"); return TKPHI_EINVAL; }
   if (!ws) { set_error("workspace is null"); return TKPHI_EWORKSPACE; }
   if ((uintptr_t)ws % 256 != 0) { set_error("workspace must be 256-byte aligned"); return TKPHI_EWORKSPACE; }
   *empty = st->n_seqs == 0 || st->rows == 0 || st->max_new == 0 || st->max_len == 0;
   const PagedSpace s = space_of(c, *g);
   if (ws_bytes < s.total) { set_error("workspace too small: %zu < %zu bytes", ws_bytes, s.total); return TKPHI_EWORKSPACE; }
-  if (pool->n_pages < 0 || pool->reserved != 0) { set_error("pool: n_pages=%d reserved=%d", pool->n_pages, pool->reserved); return TKPHI_EINVAL; }
+  if (pool.n_pages < 0 || pool.reserved != 0) { set_error("pool: n_pages=%d reserved=%d", pool.n_pages, pool.reserved); return TKPHI_EINVAL; }
   if (*empty) return TKPHI_OK;
-  if (pool->n_pages < 1) { set_error("pool without pages"); return TKPHI_EINVAL; }
+  if (pool.n_pages < 1) { set_error("pool without pages"); return TKPHI_EINVAL; }
   if ((r = check_pointer(st->seqs, "seqs", 16)) != TKPHI_OK) return r;
   if (st->max_pages < 1) { set_error("page table without entries"); return TKPHI_EINVAL; }
   if ((r = check_pointer(st->pages, "pages", 4)) != TKPHI_OK) return r;
-  if ((r = check_pointer(pool->K, "K", 16)) != TKPHI_OK) return r;
-  if ((r = check_pointer(pool->V, "V", 16)) != TKPHI_OK) return r;
-  g->n_pages = pool->n_pages;
-  g->K = (char*)pool->K; g->V = (char*)pool->V; g->M = (char*)pool->M;
+  if ((r = check_pointer(pool.K, "K", 16)) != TKPHI_OK) return r;
+  if ((r = check_pointer(pool.V, "V", 16)) != TKPHI_OK) return r;
+  if (pool.codes && (r = check_pointer(pool.S, "scales", 16)) != TKPHI_OK) return r;
+  g->n_pages = pool.n_pages;
+  g->S = (uint16_t*)pool.S;
+  g->K = (char*)pool.K; g->V = (char*)pool.V; g->M = (char*)pool.M;
   char* w = (char*)ws;
   g->status = (uint32_t*)w;
   g->plan_count = (int*)(w + s.keys - 256);
@@ -224,21 +237,27 @@ tkphi_status check_attention_rows(const tkphi_attention_rows* io, PagedGeom* g) 
   return TKPHI_OK;
 }
 
-}  // namespace
-}  // namespace tkphi
-
-using namespace tkphi;
-
-extern "C" {
-
-size_t tkphi_paged_workspace_bytes(const tkphi_paged_config* cfg, const tkphi_step* step) {
-  PagedGeom g;
-  if (check_config(cfg, step, &g) != TKPHI_OK) return 0;
-  return space_of(cfg, g).total;
+tkphi_status check_norms(const tkphi_head_norms* n, PagedGeom* g) {
+  if (!(n->eps >= 1.17549435e-38f) || !std::isfinite(n->eps)) { set_error("eps=%g has to be positive and finite", n->eps); return TKPHI_EINVAL; }
+  if (!std::isfinite(n->weight_offset)) { set_error("weight_offset=%g has to be finite", n->weight_offset); return TKPHI_EINVAL; }
+  const int64_t es = g->dtype == TKPHI_BF16 ? 2 : 4;
+  const struct { const void* w; int64_t head; const char* name; } both[] = {{n->q_weight, n->q_weight_head, "q_weight"}, {n->k_weight, n->k_weight_head, "k_weight"}};
+  for (const auto& x : both) {
+    if ((uintptr_t)x.w % 16 != 0 || x.head < 0 || x.head > (1ll << 40) || x.head * es % 16 != 0 || (x.head > 0 && x.head < g->d)) {
+      set_error("%s: misaligned, or stride %lld between heads (0 or >= d_head, 16-byte multiples)", x.name, (long long)x.head);
+      return TKPHI_EALIGN;
+    }
+  }
+  g->normed = 1;
+  g->eps = n->eps;
+  g->w_offset = n->weight_offset;
+  g->qw = (const char*)n->q_weight; g->kw = (const char*)n->k_weight;
+  g->qw_head = n->q_weight_head * es; g->kw_head = n->k_weight_head * es;
+  return TKPHI_OK;
 }
 
-tkphi_status tkphi_kv_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool, const tkphi_new_rows* io,
-                             void* workspace, size_t workspace_bytes, void* hip_stream) {
+tkphi_status append(const tkphi_paged_config* cfg, const tkphi_step* step, const Pool& pool, const tkphi_new_rows* io, const tkphi_head_norms* norms,
+                    void* workspace, size_t workspace_bytes, void* hip_stream, const char* what) {
   PagedGeom g;
   bool empty = false;
   tkphi_status st = check_call(cfg, step, pool, io, workspace, workspace_bytes, &g, &empty);
@@ -255,15 +274,16 @@ tkphi_status tkphi_kv_append(const tkphi_paged_config* cfg, const tkphi_step* st
   g.q = (const char*)io->q; g.k = (const char*)io->k; g.v = (const char*)io->v;
   g.out = (char*)io->q_rot;
   g.inv_freq = io->inv_freq;
+  if (norms && (st = check_norms(norms, &g)) != TKPHI_OK) return st;
   g.by_half.set(g.rot / 2);
   g.by_lines.set((g.q ? g.G : 0) + 2);
   (void)hipGetLastError();
   launch_paged_append(g, (hipStream_t)hip_stream);
-  return hip_status(hipGetLastError(), "tkphi_kv_append launch");
+  return hip_status(hipGetLastError(), what);
 }
 
-tkphi_status tkphi_paged_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
-                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream) {
+tkphi_status attend(const tkphi_paged_config* cfg, const tkphi_step* step, const Pool& pool, const tkphi_attention_rows* io, void* workspace,
+                    size_t workspace_bytes, void* hip_stream, const char* what) {
   PagedGeom g;
   bool empty = false;
   tkphi_status st = check_call(cfg, step, pool, io, workspace, workspace_bytes, &g, &empty);
@@ -272,18 +292,18 @@ tkphi_status tkphi_paged_attention(const tkphi_paged_config* cfg, const tkphi_st
   plan_attention(cfg, &g);
   (void)hipGetLastError();
   launch_paged_attention(g, (hipStream_t)hip_stream);
-  return hip_status(hipGetLastError(), "tkphi_paged_attention launch");
+  return hip_status(hipGetLastError(), what);
 }
 
-tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
-                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream) {
+tkphi_status attend_blocks(const tkphi_paged_config* cfg, const tkphi_step* step, const Pool& pool, const tkphi_attention_rows* io, void* workspace,
+                           size_t workspace_bytes, void* hip_stream, const char* name) {
   PagedGeom g;
   bool empty = false;
   tkphi_status st = check_call(cfg, step, pool, io, workspace, workspace_bytes, &g, &empty);
   if (st != TKPHI_OK) return st;
-  if (g.block == 0) { set_error("tkphi_block_attention needs cfg.block"); return TKPHI_EINVAL; }
+  if (g.block == 0) { set_error("%s needs cfg.block", name); return TKPHI_EINVAL; }
   if (g.last < 1) { set_error("last_blocks=%d: a query sees its own block", g.last); return TKPHI_EINVAL; }
-  if (g.window != 0) { set_error("tkphi_block_attention takes no window"); return TKPHI_EUNSUPPORTED; }
+  if (g.window != 0) { set_error("%s takes no window", name); return TKPHI_EUNSUPPORTED; }
   if (empty) return TKPHI_OK;
   if ((st = check_attention_rows(io, &g)) != TKPHI_OK) return st;
   if ((st = check_pointer(g.M, "M", 16)) != TKPHI_OK) return st;
@@ -296,7 +316,72 @@ tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_st
     launch_block_select(g, (hipStream_t)hip_stream);
     launch_block_attention(g, (hipStream_t)hip_stream);
   }
-  return hip_status(hipGetLastError(), "tkphi_block_attention launch");
+  return hip_status(hipGetLastError(), name);
+}
+
+}  // namespace
+}  // namespace tkphi
+
+using namespace tkphi;
+
+extern "C" {
+
+size_t tkphi_paged_workspace_bytes(const tkphi_paged_config* cfg, const tkphi_step* step) {
+  PagedGeom g;
+  if (check_config(cfg, step, &g) != TKPHI_OK) return 0;
+  return space_of(cfg, g).total;
+}
+
+tkphi_status tkphi_kv_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool, const tkphi_new_rows* io,
+                             void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return append(cfg, step, pool_of(pool), io, nullptr, workspace, workspace_bytes, hip_stream, "tkphi_kv_append launch");
+}
+
+tkphi_status tkphi_norm_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool, const tkphi_new_rows* io,
+                               const tkphi_head_norms* norms, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (!norms) { set_error("norms is null"); return TKPHI_EINVAL; }
+  return append(cfg, step, pool_of(pool), io, norms, workspace, workspace_bytes, hip_stream, "tkphi_norm_append launch");
+}
+
+tkphi_status tkphi_quant_append(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool, const tkphi_new_rows* io,
+                                const tkphi_head_norms* norms, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return append(cfg, step, pool_of(pool), io, norms, workspace, workspace_bytes, hip_stream, "tkphi_quant_append launch");
+}
+
+tkphi_status tkphi_paged_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
+                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend(cfg, step, pool_of(pool), io, workspace, workspace_bytes, hip_stream, "tkphi_paged_attention launch");
+}
+
+tkphi_status tkphi_quant_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool,
+                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend(cfg, step, pool_of(pool), io, workspace, workspace_bytes, hip_stream, "tkphi_quant_attention launch");
+}
+
+tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_kv_pool* pool,
+                                   const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend_blocks(cfg, step, pool_of(pool), io, workspace, workspace_bytes, hip_stream, "tkphi_block_attention");
+}
+
+tkphi_status tkphi_quant_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool,
+                                         const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return attend_blocks(cfg, step, pool_of(pool), io, workspace, workspace_bytes, hip_stream, "tkphi_quant_block_attention");
+}
+
+tkphi_status tkphi_quant_read(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool, const tkphi_read_rows* io,
+                              void* workspace, size_t workspace_bytes, void* hip_stream) {
+  PagedGeom g;
+  bool empty = false;
+  tkphi_status st = check_call(cfg, step, pool_of(pool), io, workspace, workspace_bytes, &g, &empty);
+  if (st != TKPHI_OK || empty) return st;
+  if (!io->k && !io->v) { set_error("k and v are null"); return TKPHI_EINVAL; }
+  if (io->k && (st = check_rows(g, io->k, "k", g.Hkv, io->k_row, io->k_head, &g.k_row, &g.k_head)) != TKPHI_OK) return st;
+  if (io->v && (st = check_rows(g, io->v, "v", g.Hkv, io->v_row, io->v_head, &g.v_row, &g.v_head)) != TKPHI_OK) return st;
+  g.k_out = (char*)io->k;
+  g.v_out = (char*)io->v;
+  (void)hipGetLastError();
+  launch_paged_read(g, (hipStream_t)hip_stream);
+  return hip_status(hipGetLastError(), "tkphi_quant_read launch");
 }
 
 }  // extern "C"

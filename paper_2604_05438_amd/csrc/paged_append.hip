@@ -1,5 +1,8 @@
-// tkphi_kv_append: new queries and keys turned to their positions, keys and values to their pages, mean keys of filled blocks.
+// tkphi_kv_append, tkphi_norm_append, tkphi_quant_append: new queries and keys, normed by head where asked for, turned to their positions, keys and values
+// to their pages, in the rows' own type or in 8 bits, mean keys of filled blocks.
 //
+// Norm: y = x / sqrt(mean x^2 + eps) (w + offset), in 32 bits with the rotation behind it, rounded once.  8 bits: see Code8; the scale is that of the
+// row as it would be stored in 32 bits.
 // A pair of channels (a, b) of the token at position p becomes (a cos - b sin, a sin + b cos) at the angle p inv_freq[j].
 // A workgroup takes a tile of consecutive cache positions of one sequence (a whole block where means are kept, so that the mean has one
 // writer and a fixed order) and one KV head with its query heads.  Bound by memory: every row is read once and written
@@ -45,8 +48,45 @@ template <> __device__ __forceinline__ u32x4 pack16<uint16_t>(const float* x) {
 typedef __attribute__((address_space(1))) u32x4* gout128;
 __device__ __forceinline__ void gstore128(void* p, u32x4 v) { *(gout128)p = v; }
 
-template <typename T, int D>
+// Rows of the cache in 8 bits from the two pieces x, y of a row that a lane holds (the row's `lanes` lanes ask together): codes of both, and the scale
+// byte.  Values that are not finite become NaN and leave the scale alone.
+struct Coded {
+  uint32_t x[2], y[2];
+  uint32_t scale;
+};
+__device__ __forceinline__ Coded encode(float* x, float* y, int lanes) {
+  float top = 0.f;
+  const auto size = [](float v) { return __uint_as_float(__float_as_uint(v) & 0x7fffffffu); };
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float a = size(x[e]), b = size(y[e]);
+    if (!(a < INFINITY)) x[e] = __uint_as_float(0x7fc00000u);
+    if (!(b < INFINITY)) y[e] = __uint_as_float(0x7fc00000u);
+    top = fmaxf(top, a < INFINITY ? a : 0.f);
+    top = fmaxf(top, b < INFINITY ? b : 0.f);
+  }
+  top = lanes_reduce(top, lanes, MaxOp());
+  // top = f 2^k with 1 <= f < 2; the largest code is 1.75 x 2^8
+  const uint32_t bits = __float_as_uint(top);
+  const int byte = min(max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u), kLeastScale), kMostScale);
+  const float by = __uint_as_float((uint32_t)(254 - byte) << 23);         // (an exact product: the code is the only rounding)
+  Coded c;
+  c.scale = (uint32_t)byte;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    c.x[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k] * by, x[4 * k + 1] * by, 0, false);
+    c.x[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2] * by, x[4 * k + 3] * by, (int)c.x[k], true);
+    c.y[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k] * by, y[4 * k + 1] * by, 0, false);
+    c.y[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2] * by, y[4 * k + 3] * by, (int)c.y[k], true);
+  }
+  return c;
+}
+
+// C: the cache's type; NORM: heads of q and k are normed first
+template <typename C, int D, bool NORM>
 __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g, int tile) {
+  using T = typename Cached<C>::Row;
+  constexpr bool CODES = Cached<C>::codes;
   constexpr int EPL = Elem<T>::per16, PAIRS = D / (2 * EPL);     // pairs of 16-byte pieces per row
   extern __shared__ __align__(16) char lds[];
   const int h = blockIdx.y, tid = threadIdx.x;
@@ -69,8 +109,16 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
   if (fills && lo > t0) {                                      // older keys of the block
     const char* src = g.K + (int64_t)max(page_id(g, f.index, block_entry), 0) * g.st_page + h * g.st_head + (int64_t)block_row * g.st_tok;
     constexpr int PIECES = D / EPL;
-    for (int i = tid; i < (lo - t0) * PIECES; i += kPagedThreads)
-      *(u32x4*)(kept + (i / PIECES) * D + (i % PIECES) * EPL) = gload128(src + (int64_t)(i / PIECES) * g.st_tok + (i % PIECES) * 16);
+    if constexpr (CODES) {
+      const uint16_t* scales = g.S + scale_at(g, max(page_id(g, f.index, block_entry), 0), h, block_row);
+      for (int i = tid; i < (lo - t0) * PIECES; i += kPagedThreads) {
+        const uint64_t w = *(const __attribute__((address_space(1))) uint64_t*)(src + (int64_t)(i / PIECES) * g.st_tok + (i % PIECES) * 8);
+        *(u32x4*)(kept + (i / PIECES) * D + (i % PIECES) * EPL) = decode8((uint32_t)w, (uint32_t)(w >> 32), key_scale(scales[i / PIECES]));
+      }
+    } else {
+      for (int i = tid; i < (lo - t0) * PIECES; i += kPagedThreads)
+        *(u32x4*)(kept + (i / PIECES) * D + (i % PIECES) * EPL) = gload128(src + (int64_t)(i / PIECES) * g.st_tok + (i % PIECES) * 16);
+    }
   }
   for (int i = tid; i < n * half; i += kPagedThreads) {
     const int t = g.by_half(i), j = i - t * half;
@@ -90,19 +138,49 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
     const int pa = turns && !g.adjacent ? p : 2 * p, pb = turns && !g.adjacent ? p + rotated : 2 * p + 1;
     u32x4 ua = gload128(src + pa * 16), ub = gload128(src + pb * 16);
     char* dst;
+    uint8_t* scale_dst = nullptr;
     if (line < lines - 2) {
       dst = g.out + (int64_t)(first_row + t) * g.out_row + (int64_t)(h * g.G + line) * g.out_head;
     } else {
       const int pt = page_of(g, lo + t), id = page_id(g, f.index, pt, &lost);
       dst = id < 0 ? nullptr : (is_v ? g.V : g.K) + (int64_t)id * g.st_page + h * g.st_head + (int64_t)(lo + t - pt * g.by_page.d) * g.st_tok;
       lost = lost || id < 0;
+      if constexpr (CODES) scale_dst = (uint8_t*)(g.S + scale_at(g, max(id, 0), h, lo + t - pt * g.by_page.d)) + is_v;
     }
-    if (turns) {
+    const bool codes = CODES && (is_k || is_v);
+    if (turns || codes || (NORM && !is_v)) {
       float a[EPL], b[EPL], x[EPL], y[EPL];
       Elem<T>::unpack(make_uint4(ua.x, ua.y, ua.z, ua.w), a);
       Elem<T>::unpack(make_uint4(ub.x, ub.y, ub.z, ub.w), b);
+      if constexpr (NORM)
+        if (!is_v) {                                             // (a row's lanes are PAIRS neighbours)
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) sum = fmaf(a[e], a[e], fmaf(b[e], b[e], sum));
+          sum = lanes_sum(sum, PAIRS);
+          const float by = __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, g.eps));
+          const char* w = is_k ? g.kw : g.qw;
+          if (w) {
+            w += is_k ? h * g.kw_head : (int64_t)(h * g.G + line) * g.qw_head;
+            float wa[EPL], wb[EPL];
+            const u32x4 va = gload128(w + pa * 16), vb = gload128(w + pb * 16);
+            Elem<T>::unpack(make_uint4(va.x, va.y, va.z, va.w), wa);
+            Elem<T>::unpack(make_uint4(vb.x, vb.y, vb.z, vb.w), wb);
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+              a[e] = a[e] * by * (wa[e] + g.w_offset);
+              b[e] = b[e] * by * (wb[e] + g.w_offset);
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) { a[e] *= by; b[e] *= by; }
+          }
+        }
       const float2* cs = turn + t * half + p * EPL;
-      if (g.adjacent) {
+      if ((CODES || NORM) && !turns) {
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) { x[e] = a[e]; y[e] = b[e]; }
+      } else if (g.adjacent) {
 #pragma unroll
         for (int e = 0; e < EPL; e += 2) {
           const float2 c = cs[e / 2], c2 = cs[EPL / 2 + e / 2];
@@ -119,8 +197,24 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
           y[e] = a[e] * c.y + b[e] * c.x;
         }
       }
-      ua = pack16<T>(x);
-      ub = pack16<T>(y);
+      if constexpr (CODES)
+        if (codes) {
+          const Coded c = encode(x, y, PAIRS);
+          if (dst) {
+            typedef __attribute__((address_space(1))) uint64_t* gout64;
+            *(gout64)(dst + pa * 8) = (uint64_t)c.x[1] << 32 | c.x[0];
+            *(gout64)(dst + pb * 8) = (uint64_t)c.y[1] << 32 | c.y[0];
+            if (p == 0) *scale_dst = (uint8_t)c.scale;
+            dst = nullptr;
+          }
+          const float scale = __uint_as_float(c.scale << 23);    // (the key as stored, for the mean)
+          ua = decode8(c.x[0], c.x[1], scale);
+          ub = decode8(c.y[0], c.y[1], scale);
+        }
+      if (!codes) {
+        ua = pack16<T>(x);
+        ub = pack16<T>(y);
+      }
     }
     if (dst) {
       gstore128(dst + pa * 16, ua);
@@ -147,6 +241,11 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
   }
 }
 
+template <typename C, int D>
+static void launch_append(const PagedGeom& g, dim3 grid, size_t lds, int tile, hipStream_t s) {
+  if (g.normed) hipLaunchKernelGGL((paged_append_kernel<C, D, true>), grid, dim3(kPagedThreads), lds, s, g, tile);
+  else hipLaunchKernelGGL((paged_append_kernel<C, D, false>), grid, dim3(kPagedThreads), lds, s, g, tile);
+}
 void launch_paged_append(const PagedGeom& g, hipStream_t s) {
   const int tile = g.block ? g.block : 16;
   // sequence by sequence a tile at either end may be cut
@@ -154,12 +253,15 @@ void launch_paged_append(const PagedGeom& g, hipStream_t s) {
   const unsigned tiles = (unsigned)(by_rows < by_seqs ? by_rows : by_seqs);
   const dim3 grid(tiles + 1, g.Hkv);                             // (the last one has a tile only where sequences share rows)
   const size_t lds = (size_t)tile * (g.rot / 2) * sizeof(float2) + (g.block ? (size_t)tile * g.d * (g.dtype == TKPHI_BF16 ? 2 : 4) : 0);
-  if (g.dtype == TKPHI_BF16) {
-    if (g.d == 64) hipLaunchKernelGGL((paged_append_kernel<uint16_t, 64>), grid, dim3(kPagedThreads), lds, s, g, tile);
-    else hipLaunchKernelGGL((paged_append_kernel<uint16_t, 128>), grid, dim3(kPagedThreads), lds, s, g, tile);
+  if (g.S) {
+    if (g.d == 64) launch_append<Code8, 64>(g, grid, lds, tile, s);
+    else launch_append<Code8, 128>(g, grid, lds, tile, s);
+  } else if (g.dtype == TKPHI_BF16) {
+    if (g.d == 64) launch_append<uint16_t, 64>(g, grid, lds, tile, s);
+    else launch_append<uint16_t, 128>(g, grid, lds, tile, s);
   } else {
-    if (g.d == 64) hipLaunchKernelGGL((paged_append_kernel<float, 64>), grid, dim3(kPagedThreads), lds, s, g, tile);
-    else hipLaunchKernelGGL((paged_append_kernel<float, 128>), grid, dim3(kPagedThreads), lds, s, g, tile);
+    if (g.d == 64) launch_append<float, 64>(g, grid, lds, tile, s);
+    else launch_append<float, 128>(g, grid, lds, tile, s);
   }
 }
 

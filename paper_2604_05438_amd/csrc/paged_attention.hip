@@ -37,11 +37,13 @@ __device__ __forceinline__ pa_u32x2 lds_read_transposed(const char* p) {
 // (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of 6.5.)
 template <typename T, int D, int RT, bool STREAM>
 struct WaveAttend {
-  static constexpr bool BF = sizeof(T) == 2;
-  static constexpr int RB = D * (int)sizeof(T);                   // bytes of a row
+  using Row = typename Cached<T>::Row;
+  static constexpr bool BF = Cached<T>::bf16, CODES = Cached<T>::codes;
+  static constexpr int RB = D * (int)sizeof(Row);                 // bytes of a row, as it is contracted
   static constexpr int SUB = BF ? 2 : 1;                          // subtiles of 16 tokens that are loaded and contracted together
   static constexpr int TOK = 16 * SUB;
   static constexpr int NF = RB / 64;                              // 16-byte pieces of a row per lane
+  static constexpr int NL = D * Cached<T>::bytes / 64;            // of the row in the cache: fewer for codes (one, a whole row by 4 lanes, at D = 64)
   static constexpr int VROW = RB + 32;                            // LDS row of V
   static constexpr int LDS = TOK * VROW;                          // LDS bytes per wavefront
   static constexpr int CT = D / 16;
@@ -70,26 +72,44 @@ struct WaveAttend {
   struct Rows {
     int64_t off[GR];
     int pos[GR], mask[GR];
+    int64_t scale;                                                 // codes: where the scales of token lane % TOK of the tile are
   };
-  static __device__ __forceinline__ int lane_offset() { return ((threadIdx.x >> 3) & 1) * 64 + ((threadIdx.x >> 4) & 3) * 16; }
-
-  // `at`: what the lane adds to the groups' offsets
-  __device__ __forceinline__ void load(const char* base, uint32_t at, const Rows& r, PagedFrag (&f)[SUB][NF]) {
-#pragma unroll
-    for (int s = 0; s < SUB; ++s)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int j = 0; j < NF / 2; ++j) {
-          const char* p = base + r.off[2 * s + u] + at + j * 128;
-          f[s][2 * j + u].u = STREAM ? gload128_stream(p) : gload128(p);
-        }
+  static __device__ __forceinline__ int lane_offset() { return (NL > 1 ? ((threadIdx.x >> 3) & 1) * 64 : 0) + ((threadIdx.x >> 4) & 3) * 16; }
+  // where query piece f of a lane lies in its row: the channels that piece f of a key has
+  static __device__ __forceinline__ int query_offset(int f) {
+    const int kg = (threadIdx.x >> 4) & 3;
+    return CODES ? (f >> 1) * 128 + kg * 32 + (f & 1) * 16 : f * 64 + kg * 16;
   }
+  // `at`: what the lane adds to the groups' offsets
+  __device__ __forceinline__ void load(const char* base, uint32_t at, const Rows& r, PagedFrag (&f)[SUB][NL]) {
+#pragma unroll
+    for (int s = 0; s < SUB; ++s) {
+      if constexpr (NL == 1) {
+        const int64_t first = r.off[2 * s], second = r.off[2 * s + 1];          // (chosen by value: an address chosen by the lane would put Rows in scratch)
+        const char* p = base + (threadIdx.x & 8 ? second : first) + at;
+        f[s][0].u = STREAM ? gload128_stream(p) : gload128(p);
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int j = 0; j < NL / 2; ++j) {
+            const char* p = base + r.off[2 * s + u] + at + j * 128;
+            f[s][2 * j + u].u = STREAM ? gload128_stream(p) : gload128(p);
+          }
+      }
+    }
+  }
+  static __device__ __forceinline__ uint32_t load_scales(const PagedGeom& g, const Rows& r) {
+    if constexpr (CODES) return *(const __attribute__((address_space(1))) uint16_t*)(g.S + r.scale);
+    else return 0;
+  }
+  // of the scales that load_scales brought, those of token t of the tile
+  static __device__ __forceinline__ uint32_t scales_of(uint32_t mine, int t) { return (uint32_t)__builtin_amdgcn_ds_bpermute(t * 4, (int)mine); }
 
   // the operands of 16 rows out of what two groups loaded: lanes 8 .. 15 of each row of 16 of the one <-> lanes 0 .. 7 of the other
-  static __device__ __forceinline__ void to_operands(PagedFrag (&f)[NF]) {
+  static __device__ __forceinline__ void to_operands(PagedFrag (&f)[NL]) {
 #pragma unroll
-    for (int j = 0; j < NF; j += 2) {
+    for (int j = 0; j + 1 < NL; j += 2) {
       const PagedFrag a = f[j], b = f[j + 1];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -97,6 +117,12 @@ struct WaveAttend {
         f[j + 1].u[e] = (uint32_t)__builtin_amdgcn_update_dpp((int)b.u[e], (int)a.u[e], 0x128, 0xf, 0x3, false);
       }
     }
+  }
+
+  // pieces of a row of codes as they are contracted
+  static __device__ __forceinline__ void decode(const PagedFrag (&c)[NL], float scale, PagedFrag (&k)[NF]) {
+#pragma unroll
+    for (int j = 0; j < NF; ++j) k[j].u = decode8(c[j / 2].u[2 * (j & 1)], c[j / 2].u[2 * (j & 1) + 1], scale);
   }
 
   __device__ __forceinline__ pa_floatx4 score(const PagedFrag (&k)[NF], const PagedFrag (&qq)[NF]) {
@@ -148,7 +174,7 @@ struct WaveAttend {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[rt][ct][i] = fmaf(weight, Elem<T>::load1(v, ct * 16 + kg * 4 + i), o[rt][ct][i]);
+              for (int i = 0; i < 4; ++i) o[rt][ct][i] = fmaf(weight, Elem<Row>::load1(v, ct * 16 + kg * 4 + i), o[rt][ct][i]);
           }
         }
   }
@@ -160,10 +186,11 @@ struct WaveAttend {
     const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, r7 = lane & 7;
     const char* Kb = g.K + h * g.st_head;
     const char* Vb = g.V + h * g.st_head;
-    char* const vw = vlds + r7 * VROW + lane_offset();
-    PagedFrag kf[SUB][NF], vf[SUB][NF];
+    char* const vw = vlds + (NL > 1 ? r7 : r) * VROW + lane_offset() * (CODES ? 2 : 1);
+    PagedFrag kf[SUB][NL], vf[SUB][NL];
     Rows cur = rows_of(0);
     load(Kb, lane_at, cur, kf);
+    uint32_t scales = load_scales(g, cur), scales_next = 0;
     load(Vb, lane_at, cur, vf);
     Rows nxt = rows_of(min(1, n - 1));
     for (int i = 0; i < n; ++i) {
@@ -174,10 +201,20 @@ struct WaveAttend {
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         to_operands(kf[u]);
+        if constexpr (CODES) {
+          PagedFrag k[NF];
+          decode(kf[u], key_scale(scales_of(scales, 16 * u + r)), k);
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[u][rt] = score(kf[u], q[rt]);
+          for (int rt = 0; rt < RT; ++rt) s[u][rt] = score(k, q[rt]);
+        } else {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) s[u][rt] = score(kf[u], q[rt]);
+        }
       }
-      if (i + 1 < n) load(Kb, lane_at, cur, kf);
+      if (i + 1 < n) {
+        load(Kb, lane_at, cur, kf);
+        scales_next = load_scales(g, cur);
+      }
       nxt = rows_of(min(i + 2, n - 1));
       // ---- what nobody may see
       bool all = clean(i);
@@ -235,17 +272,37 @@ struct WaveAttend {
       }
       // ---- V through LDS; rows that nobody sees as zeros, whatever they hold
       bool odd = false;                                            // a value that is no number, or infinite, which some rows may not see
+      if constexpr (CODES) {
+        constexpr int PER = NL > 1 ? 1 : 2;                        // groups of 8 rows per load
 #pragma unroll
-      for (int u = 0; u < GR; ++u)
+        for (int u = 0; u < GR; u += PER) {
+          const int first = here.mask[u], second = here.mask[u + PER - 1], mask = lane & 8 && PER == 2 ? second : first;
+          const float scale = value_scale(scales_of(scales, 8 * u + (PER == 1 ? r7 : r)));
+          const u32x4 c = vf[u / 2][PER == 1 ? u % 2 : 0].u;
 #pragma unroll
-        for (int j = 0; j < NF / 2; ++j) {
-          u32x4 w = vf[u / 2][2 * j + u % 2].u;
-          if (!all) {
-            if (!((here.mask[u] >> r7) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
-            odd = odd || not_finite(w);
+          for (int x = 0; x < 2; ++x) {
+            u32x4 w = decode8(c[2 * x], c[2 * x + 1], scale);
+            if (!all) {
+              if (!((mask >> r7) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
+              odd = odd || not_finite(w);
+            }
+            *(u32x4*)(vw + u * 8 * VROW + x * 16) = w;
           }
-          *(u32x4*)(vw + u * 8 * VROW + j * 128) = w;
         }
+        scales = scales_next;
+      } else {
+#pragma unroll
+        for (int u = 0; u < GR; ++u)
+#pragma unroll
+          for (int j = 0; j < NF / 2; ++j) {
+            u32x4 w = vf[u / 2][2 * j + u % 2].u;
+            if (!all) {
+              if (!((here.mask[u] >> r7) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
+              odd = odd || not_finite(w);
+            }
+            *(u32x4*)(vw + u * 8 * VROW + j * 128) = w;
+          }
+      }
       if (i + 1 < n) load(Vb, lane_at, cur, vf);
       if constexpr (BF) {
         PagedFrag ones;
@@ -296,7 +353,7 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM>& w, char
   for (int rt = 0; rt < RT; ++rt) {
     const float l = across_32(across_16(w.l[rt], AddOp()), AddOp());
     float f = 1.f;
-    if constexpr (sizeof(T) == 2) f = to_sum(l, w.lr[rt][0]);
+    if constexpr (Cached<T>::bf16) f = to_sum(l, w.lr[rt][0]);
     float* row = mine + (rt * 16 + r) * STR;
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct)
@@ -404,7 +461,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   constexpr int WAVES = kPagedThreads / 64;
   __shared__ __align__(16) char lds[attend_lds<T, D, RT, STREAM>()];
   __shared__ int sh_last;
-  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
   const int w = blockIdx.x;
   const auto sh = share_of<PLAN>(g, w);
@@ -432,7 +489,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
 #pragma unroll
       for (int f = 0; f < Wave::NF; ++f) {
         at.q[rt][f].u = (u32x4){0u, 0u, 0u, 0u};
-        if (live) at.q[rt][f].u = gload128(src + f * 64 + kg * 16);
+        if (live) at.q[rt][f].u = gload128(src + Wave::query_offset(f));
       }
     }
     const int seen_all = s.cached + (PLAN ? g.by_group(p.tile * g.tile_rows) : 0);         // last token that every row sees
@@ -455,7 +512,12 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
                  rows.off[u] = (int64_t)max(gid, 0) * g.st_page + (int64_t)(tu - gp * g.by_page.d) * g.st_tok;
                  rows.pos[u] = tu;
                  rows.mask[u] = gid < 0 || from >= to ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
+                 if constexpr (Wave::CODES) {
+                   const int64_t at_scale = scale_at(g, max(gid, 0), h, tu - gp * g.by_page.d);
+                   rows.scale = u == 0 || ((lane >> 3) % Wave::GR) == u ? at_scale : rows.scale;
+                 }
                }
+               if constexpr (Wave::CODES) rows.scale += lane & 7;
              } else {
 #pragma unroll
                for (int u = 0; u < Wave::GR; ++u) {
@@ -464,6 +526,10 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
                  rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
                  rows.pos[u] = tb + u * 8;
                  rows.mask[u] = (int)(__ballot(id >= 0) & 0xff);
+                 if constexpr (Wave::CODES) {
+                   const int64_t at_scale = scale_at(g, max(id, 0), h, t - pt * g.by_page.d);
+                   rows.scale = u == 0 || ((lane >> 3) % Wave::GR) == u ? at_scale : rows.scale;
+                 }
                }
              }
              return rows;
@@ -477,7 +543,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
       if (whole) {
         int token, head;
         p.place(g, row, &token, &head);
-        store_out<T>(g, token, head, c, o, m, l);
+        store_out<typename Wave::Row>(g, token, head, c, o, m, l);
       } else if constexpr (PLAN) {
         *(float2*)(slot + row * D + c) = o;
         if (c == 0) *(float2*)(slot + g.tile_rows * D + row * 2) = make_float2(m, l);
@@ -488,7 +554,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     });
     report_pages(g, bad);
     if constexpr (!PLAN) {
-      if (!whole) finish_item<T, D, kPagedThreads>(g, sh, p, lds, &sh_last);
+      if (!whole) finish_item<typename Wave::Row, D, kPagedThreads>(g, sh, p, lds, &sh_last);
     }
     if constexpr (PLAN) join.note(g, sh, p, w, x == sh.begin);
     __syncthreads();
@@ -525,7 +591,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   constexpr int WAVES = kPagedThreads / 64;
   __shared__ __align__(16) char lds[attend_lds<T, D, 1, true>()];
   __shared__ int sh_last;
-  const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int h = blockIdx.y, local = blockIdx.z, token = g.row0 + local, split = blockIdx.x;
   const int64_t at_list = (int64_t)local * g.Hkv + h;
   const int4 head = g.list_head[at_list];                          // entries, position of the query, its sequence; 0 entries: a row of no sequence
@@ -542,7 +608,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
 #pragma unroll
   for (int f = 0; f < Wave::NF; ++f) {
     at.q[0][f].u = (u32x4){0u, 0u, 0u, 0u};
-    if (r < g.G) at.q[0][f].u = gload128(src + f * 64 + kg * 16);
+    if (r < g.G) at.q[0][f].u = gload128(src + Wave::query_offset(f));
   }
   at.reset();
   const int per = g.by_page.d / g.block, shift = 31 - __builtin_clz(g.block);          // (a power of two of at least 16 tokens, in one page)
@@ -560,7 +626,12 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
              rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(__builtin_amdgcn_readlane(first, u) + in) * g.st_tok;
              rows.pos[u] = pos;
              rows.mask[u] = id < 0 || n <= 0 || t0 + u * 8 >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
+             if constexpr (Wave::CODES) {
+               const int64_t at_scale = scale_at(g, max(id, 0), h, __builtin_amdgcn_readlane(first, u) + in);
+               rows.scale = u == 0 || ((lane >> 3) % Wave::GR) == u ? at_scale : rows.scale;
+             }
            }
+           if constexpr (Wave::CODES) rows.scale += lane & 7;
            return rows;
          },
          [&](int) { return true; });                               // (all rows are the same token's)
@@ -573,14 +644,14 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   float* slot = part + (int64_t)piece * 16 * (D + 2);
   join_waves<T, D, 1, true>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
-      store_out<T>(g, token, h * g.G + row, c, o, m, l);
+      store_out<typename Wave::Row>(g, token, h * g.G + row, c, o, m, l);
     } else {
       store_pair(slot + row * D + c, o.x, o.y);
       if (c == 0) store_pair(slot + 16 * D + row * 2, m, l);
     }
   });
   if (!whole && last_to_arrive(g.arrived + at_list, pieces, &sh_last))
-    join_pieces<T, D, kPagedThreads, true>(g, pieces, 0, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
+    join_pieces<typename Wave::Row, D, kPagedThreads, true>(g, pieces, 0, g.G, 16, lds, [&](int p) { return part + (int64_t)p * 16 * (D + 2); },
                       [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
 }
 
@@ -597,10 +668,13 @@ static void launch_attend(const PagedGeom& g, hipStream_t s) {
   if (g.tile_rows > kPagedRows) launch_paged_chunk(g, s);
   else if (g.tile_rows <= 16) launch_split<T, D, 1>(g, s);
   else launch_split<T, D, 2>(g, s);
-  if (g.plan_room) hipLaunchKernelGGL((paged_join_kernel<T, D>), dim3(g.splits, kJoinGroups), dim3(kPagedThreads), 0, s, g);
+  if (g.plan_room) hipLaunchKernelGGL((paged_join_kernel<typename Cached<T>::Row, D>), dim3(g.splits, kJoinGroups), dim3(kPagedThreads), 0, s, g);
 }
 void launch_paged_attention(const PagedGeom& g, hipStream_t s) {
-  if (g.dtype == TKPHI_BF16) {
+  if (g.S) {
+    if (g.d == 64) launch_attend<Code8, 64>(g, s);
+    else launch_attend<Code8, 128>(g, s);
+  } else if (g.dtype == TKPHI_BF16) {
     if (g.d == 64) launch_attend<uint16_t, 64>(g, s);
     else launch_attend<uint16_t, 128>(g, s);
   } else {
@@ -611,7 +685,10 @@ void launch_paged_attention(const PagedGeom& g, hipStream_t s) {
 
 void launch_block_attention(const PagedGeom& g, hipStream_t s) {
   const dim3 grid(g.splits, g.Hkv, g.row_group);
-  if (g.dtype == TKPHI_BF16) {
+  if (g.S) {
+    if (g.d == 64) hipLaunchKernelGGL((block_attend_kernel<Code8, 64>), grid, dim3(kPagedThreads), 0, s, g);
+    else hipLaunchKernelGGL((block_attend_kernel<Code8, 128>), grid, dim3(kPagedThreads), 0, s, g);
+  } else if (g.dtype == TKPHI_BF16) {
     if (g.d == 64) hipLaunchKernelGGL((block_attend_kernel<uint16_t, 64>), grid, dim3(kPagedThreads), 0, s, g);
     else hipLaunchKernelGGL((block_attend_kernel<uint16_t, 128>), grid, dim3(kPagedThreads), 0, s, g);
   } else {

@@ -45,7 +45,10 @@ struct ChunkTile {
   static constexpr int WAVES = chunk_rows(D) / 32, THREADS = 64 * WAVES;
   static constexpr int WAVE_TOKENS = TOKENS / WAVES, GROUPS = WAVE_TOKENS / 16;     // rows of a tile that a wavefront loads, 16 at a time
   static constexpr int LOADS = WAVE_TOKENS / ROWS, EACH = LOADS / GROUPS;                // loads per wavefront of K, and of V; and per 16 rows
+  // codes: of 64 tokens a wavefront loads, and decodes, the rows that 64 lanes x 16 codes cover, of K and of V
+  static constexpr int CODE_ROWS = kChunkTokens / WAVES, CODE_LANES = D / 16, CODE_BYTES = WAVES * 2048;
 };
+static_assert(ChunkTile<128>::CODE_ROWS * 128 == 1024 && ChunkTile<64>::CODE_ROWS * 64 == 1024, "");
 static_assert(ChunkTile<128>::LOADS == 2 * ChunkTile<128>::HALVES && ChunkTile<64>::LOADS == 2 * ChunkTile<64>::HALVES, "");
 
 // Adds the two weights of a register, as they were rounded.  (2048 tokens over 30000 / four prompts / a prompt of 16000 tokens of a 1B layer, us: 868 / 327 / 1542; without
@@ -56,7 +59,9 @@ __device__ __forceinline__ float add_rounded(uint32_t pair, float sum) {
 }
 
 // UNIFORM: 16 tokens always lie in one page
-template <int D, bool UNIFORM>
+// T = Code8: codes go from memory to LDS, 64 tokens at a time and half a tile ahead, where the lane that asked for 16 of them decodes them into the tile
+// that is worked on next; all else is as for a bf16 cache.
+template <typename T, int D, bool UNIFORM>
 __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_per_eu(chunk_per_simd(D), chunk_per_simd(D)))) void paged_chunk_kernel(PagedGeom g) {
   using Tile = ChunkTile<D>;
   constexpr int THREADS = Tile::THREADS, RB = Tile::RB, NF = D / 16, CT = D / 32, BUFS = Tile::BUFS;
@@ -65,6 +70,8 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
   __shared__ int sh_page[kPageCache];
   __shared__ __align__(8) uint16_t sh_present[BUFS][Tile::TOKENS / 16];      // which tokens of the tile anyone may see
   __shared__ int sh_odd[4];
+  constexpr bool CODES = Cached<T>::codes;
+  __shared__ __align__(16) char raw[CODES ? Tile::CODE_BYTES : 16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hi = lane >> 5, i16 = lane & 15, grp = (lane >> 4) & 1;
   const uint32_t lds0 = (uint32_t)(size_t)(lds_ptr)lds;
@@ -171,18 +178,82 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
       }
     };
 
-    request(0, true);
+    // Codes: asks for the 64 tokens after those of `ahead`, and decodes what the wavefront asked for last into their tile
+    uint32_t ahead_present = 0, ahead_scale = 0;                   // (bits, a lane's scales)
+    const auto fetch = [&](int j) {
+      if constexpr (CODES) {
+        constexpr int ROWS = Tile::CODE_ROWS;
+        const int r = lane / Tile::CODE_LANES, tw = ts + j * kChunkTokens + wave * ROWS;
+        const uint32_t dst = (uint32_t)(size_t)(lds_ptr)raw + wave * 2048, piece = lane % Tile::CODE_LANES * 16;
+        if constexpr (UNIFORM) {
+          const int pt = page_of(g, tw), a = max(it.low - tw, 0), z = min(te - tw, ROWS), in = tw - pt * g.by_page.d;      // tokens [a, z) of them
+          const int id = a < z ? __builtin_amdgcn_readfirstlane(sh_page[pt - page0]) : -1;
+          ahead_present = id >= 0 ? ((1u << z) - 1u) & ~((1u << a) - 1u) : 0u;
+          const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)in * g.st_tok;
+          const uint32_t off = (uint32_t)(r * (int)g.st_tok) + piece;
+          load_to_lds16(Kh + at, off, dst);
+          load_to_lds16(Vh + at, off, dst + 1024);
+          ahead_scale = *(const __attribute__((address_space(1))) uint16_t*)(g.S + scale_at(g, max(id, 0), p.h, in) + r);
+        } else {
+          const int t = tw + r, pt = page_of(g, t), in = t - pt * g.by_page.d;
+          const int id = t >= it.low && t < te ? sh_page[pt - page0] : -1;
+          const int64_t at = (int64_t)max(id, 0) * g.st_page + (int64_t)in * g.st_tok + piece;
+          load_to_lds16(Kh + at, dst);
+          load_to_lds16(Vh + at, dst + 1024);
+          ahead_scale = *(const __attribute__((address_space(1))) uint16_t*)(g.S + scale_at(g, max(id, 0), p.h, in));
+          const uint64_t there = __ballot(id >= 0);
+          ahead_present = 0;
+#pragma unroll
+          for (int y = 0; y < ROWS; ++y) ahead_present |= (uint32_t)((there >> (y * Tile::CODE_LANES)) & 1) << y;
+        }
+      }
+    };
+    const auto unpack = [&](int j) {
+      if constexpr (CODES) {
+        wait_vm_loads<0>();
+        const int r = wave * Tile::CODE_ROWS + lane / Tile::CODE_LANES, c = 2 * (lane % Tile::CODE_LANES), half = j % Tile::HALVES, buf = j / Tile::HALVES % BUFS;
+        const u32x4 k = *(const u32x4*)(raw + wave * 2048 + lane * 16), v = *(const u32x4*)(raw + wave * 2048 + 1024 + lane * 16);
+        char* const row = lds + buf * 2 * Tile::BYTES + (half * kChunkTokens + r) * RB;
+        const int kd = (c ^ key_swap<D>(r)) * 16, vd = Tile::BYTES + (c ^ value_swap<D>(r)) * 16;
+        const float ks = key_scale(ahead_scale), vs = value_scale(ahead_scale);
+        *(u32x4*)(row + kd) = decode8(k.x, k.y, ks);
+        *(u32x4*)(row + (kd ^ 16)) = decode8(k.z, k.w, ks);
+        *(u32x4*)(row + vd) = decode8(v.x, v.y, vs);
+        *(u32x4*)(row + (vd ^ 16)) = decode8(v.z, v.w, vs);
+        if (lane == 0) {
+          if constexpr (Tile::CODE_ROWS == 8) ((uint8_t*)sh_present[buf])[half * 8 + wave] = (uint8_t)ahead_present;
+          else sh_present[buf][half * 4 + wave] = (uint16_t)ahead_present;
+        }
+      }
+    };
+
+    if constexpr (CODES) {
+#pragma unroll 1
+      for (int j = 0; j < Tile::HALVES; ++j) {
+        fetch(j);
+        unpack(j);
+      }
+      if (n > 1) fetch(Tile::HALVES);
+    } else {
+      request(0, true);
+    }
     for (int i = 0; i < n; ++i) {
       // tile i is there, tile i - 1 is done with
-      wait_vm_loads<0>();
+      if constexpr (!CODES) wait_vm_loads<0>();
       lds_barrier();
       if (tid < 2) sh_odd[2 * (1 - (i & 1)) + tid] = 0;
       const int buf = i % BUFS;
       const bool more = i + 1 < n;
-      if (more) request(i + 1, false);
+      if constexpr (!CODES)
+        if (more) request(i + 1, false);
       // one load at each of four places per 64 tokens: first those of K, then those of V
       const auto spread = [&](int half, int y) {
-        if constexpr (UNIFORM) {
+        if constexpr (CODES) {                                     // (decoded while the products with the keys are under way)
+          const int j = (i + 1) * Tile::HALVES + half;
+          if (!more || y != 1) return;
+          unpack(j);
+          if (j + 1 < n * Tile::HALVES) fetch(j + 1);
+        } else if constexpr (UNIFORM) {
           if (!more) return;
           const bool v = Tile::HALVES == 2 ? half == 1 : y >= Tile::LOADS;
           const int k = y % Tile::LOADS;
@@ -337,13 +408,19 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
           const float weight = __uint_as_float(slot & 1 ? word & 0xffff0000u : word << 16);
           if (!((present >> slot) & 1)) continue;
           const int pt = page_of(g, t), id = max(page_id(g, p.seq, pt), 0);
-          const uint16_t* v = (const uint16_t*)(g.V + (int64_t)id * g.st_page + p.h * g.st_head + (int64_t)(t - pt * g.by_page.d) * g.st_tok);
+          const int in = t - pt * g.by_page.d;
+          const char* v = g.V + (int64_t)id * g.st_page + p.h * g.st_head + (int64_t)in * g.st_tok;
           const bool sees = t <= lim && t >= low;
+          float scale = 1.f;
+          if constexpr (CODES) scale = value_scale(g.S[scale_at(g, id, p.h, in)]);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-              const uint16_t bits = v[32 * ct + 8 * (e / 4) + 4 * hi + e % 4];
+              const int c = 32 * ct + 8 * (e / 4) + 4 * hi + e % 4;
+              uint16_t bits;
+              if constexpr (CODES) bits = (uint16_t)__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)((const uint8_t*)v)[c], scale, false));
+              else bits = ((const uint16_t*)v)[c];
               if (sees && (bits & 0x7f80) == 0x7f80) o[ct][e] = fmaf(weight, bf16_bits_to_float(bits), o[ct][e]);
             }
         }
@@ -392,10 +469,15 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
   join.store(g, w);
 }
 
-void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
+template <typename T>
+static void launch_chunk(const PagedGeom& g, hipStream_t s) {
   const bool uniform = g.by_page.d % 16 == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
-  if (g.d == 64) hipLaunchKernelGGL((uniform ? paged_chunk_kernel<64, true> : paged_chunk_kernel<64, false>), dim3(g.splits), dim3(ChunkTile<64>::THREADS), 0, s, g);
-  else hipLaunchKernelGGL((uniform ? paged_chunk_kernel<128, true> : paged_chunk_kernel<128, false>), dim3(g.splits), dim3(ChunkTile<128>::THREADS), 0, s, g);
+  if (g.d == 64) hipLaunchKernelGGL((uniform ? paged_chunk_kernel<T, 64, true> : paged_chunk_kernel<T, 64, false>), dim3(g.splits), dim3(ChunkTile<64>::THREADS), 0, s, g);
+  else hipLaunchKernelGGL((uniform ? paged_chunk_kernel<T, 128, true> : paged_chunk_kernel<T, 128, false>), dim3(g.splits), dim3(ChunkTile<128>::THREADS), 0, s, g);
+}
+void launch_paged_chunk(const PagedGeom& g, hipStream_t s) {
+  if (g.S) launch_chunk<Code8>(g, s);
+  else launch_chunk<uint16_t>(g, s);
 }
 
 }  // namespace tkphi

@@ -1,0 +1,63 @@
+// tkphi_quant_read: tokens of a cache in 8 bits as bf16 rows, in any layout (for the calls on contiguous caches).
+//
+// Codes times their row's power of two: one conversion per pair.  A workgroup takes 64 consecutive positions of one sequence and KV head; a lane has
+// 16 codes of up to 4 rows on their way before it converts the first.  Bound by memory.
+#include "paged.h"
+
+namespace tkphi {
+
+constexpr int kReadTile = 64;
+
+template <int D>
+__global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(PagedGeom g) {
+  constexpr int PIECES = D / 16, EACH = kReadTile * 2 * PIECES / kPagedThreads;      // 16 codes each; per thread
+  const int h = blockIdx.y, tid = threadIdx.x;
+  const FoundSeq f = find_seq(g, blockIdx.x, [&](const PagedSeq& s) { return (s.cached + s.fresh - 1) / kReadTile - s.cached / kReadTile + 1; });
+  if (f.index < 0) return;
+  if (blockIdx.x == gridDim.x - 1) {                             // past what the rows allow for: sequences share some (tiles from here on are left out)
+    if (h == 0 && tid == 0) atomicOr(g.status, TKPHI_DEV_BAD_LENGTH);
+    return;
+  }
+  const int t0 = (f.s.cached / kReadTile + ((int)blockIdx.x - f.before)) * kReadTile;
+  const int lo = max(t0, f.s.cached), hi = min(t0 + kReadTile, f.s.cached + f.s.fresh);
+  const int first_row = f.s.row + (lo - f.s.cached);
+  bool lost = false;
+  u32x4 w[EACH];
+  uint32_t scale[EACH];
+  int row[EACH];
+  bool there[EACH];
+#pragma unroll
+  for (int k = 0; k < EACH; ++k) {
+    const int i = tid + k * kPagedThreads, p = i % PIECES, is_v = i / PIECES % 2, t = lo + i / (2 * PIECES);
+    row[k] = t < hi ? first_row + t - lo : -1;
+    if (t >= hi) continue;
+    const int pt = page_of(g, t), id = page_id(g, f.index, pt, &lost), in = t - pt * g.by_page.d;
+    there[k] = id >= 0;
+    lost = lost || id < 0;
+    w[k] = gload128((is_v ? g.V : g.K) + (int64_t)max(id, 0) * g.st_page + h * g.st_head + (int64_t)in * g.st_tok + p * 16);
+    scale[k] = ((const uint8_t*)(g.S + scale_at(g, max(id, 0), h, in)))[is_v];
+  }
+#pragma unroll
+  for (int k = 0; k < EACH; ++k) {
+    const int i = tid + k * kPagedThreads, p = i % PIECES, is_v = i / PIECES % 2;
+    char* const base = is_v ? g.v_out : g.k_out;
+    if (row[k] < 0 || !base) continue;
+    char* dst = base + (int64_t)row[k] * (is_v ? g.v_row : g.k_row) + h * (is_v ? g.v_head : g.k_head) + p * 32;
+    const float by = __uint_as_float(scale[k] << 23);
+    u32x4 a = decode8(w[k].x, w[k].y, by), b = decode8(w[k].z, w[k].w, by);
+    if (!there[k]) a = b = (u32x4){0u, 0u, 0u, 0u};
+    *(__attribute__((address_space(1))) u32x4*)dst = a;
+    *(__attribute__((address_space(1))) u32x4*)(dst + 16) = b;
+  }
+  report_pages(g, lost);
+}
+
+void launch_paged_read(const PagedGeom& g, hipStream_t s) {
+  // sequence by sequence a tile at either end may be cut
+  const int64_t by_rows = g.rows / kReadTile + 2ll * g.n_seqs, by_seqs = (int64_t)g.n_seqs * ((g.max_new - 2 + kReadTile) / kReadTile + 1);
+  const dim3 grid((unsigned)(by_rows < by_seqs ? by_rows : by_seqs) + 1, g.Hkv);          // (the last one has a tile only where sequences share rows)
+  if (g.d == 64) hipLaunchKernelGGL(paged_read_kernel<64>, grid, dim3(kPagedThreads), 0, s, g);
+  else hipLaunchKernelGGL(paged_read_kernel<128>, grid, dim3(kPagedThreads), 0, s, g);
+}
+
+}  // namespace tkphi
