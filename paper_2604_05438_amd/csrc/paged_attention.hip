@@ -30,6 +30,10 @@ __device__ __forceinline__ pa_u32x2 lds_read_transposed(const char* p) {
   return __builtin_bit_cast(pa_u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pa_s16x4*)p));
 }
 
+__device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
+  return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)x, lane) | (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32;
+}
+
 // One wavefront's share of an item piece.
 // T, D: storage, head dimension; RT: tiles of 16 query rows; STREAM: the cache is read once (non-temporal loads)
 // A load instruction covers 8 rows x 128 bytes, whole cache lines: lane (r, kg) takes 16 bytes of row r mod 8, in the first half of its line for
@@ -256,10 +260,12 @@ struct WaveAttend {
             sum += x[u][e];
           }
         l[rt] = fmaf(l[rt], fix, sum);
+        if (__any(fix != 1.f)) {                                   // (a maximum is rarely passed after the first tiles)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) o[rt][ct] *= fix;
+          for (int ct = 0; ct < CT; ++ct) o[rt][ct] *= fix;
+          if constexpr (BF) lr[rt] *= fix;
+        }
         if constexpr (BF) {                                        // (the weights enter the product in the cache's own type)
-          lr[rt] *= fix;
 #pragma unroll
           for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -502,22 +508,21 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
            [&](int i) {
              typename Wave::Rows rows;
              const int tb = tile0(i);
-             if constexpr (UNIFORM) {                              // lane u < GR looks up the page of group u
-               const int t = tb + min(lane, Wave::GR - 1) * 8, pt = page_of(g, t);
-               const int id = t + 7 >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
+             if constexpr (UNIFORM) {                              // lanes 8 u .. 8 u + 7 look up the page of group u (scalar code took twice as long as all else)
+               const int t = tb + (lane >> 3) % Wave::GR * 8, pt = page_of(g, t), in = t - pt * g.by_page.d;
+               const int from = max(it.low - t, 0), to = min(t1 - t, 8);                        // tokens [from, to) of the group
+               bool odd = false;
+               const int id = page_id(g, seq, pt, &odd), there = from < to ? id : -1;
+               bad = bad || (odd && from < to);
+               const int mask = there < 0 ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
+               const int64_t off = (int64_t)max(there, 0) * g.st_page + (int64_t)in * g.st_tok;
 #pragma unroll
                for (int u = 0; u < Wave::GR; ++u) {
-                 const int tu = tb + u * 8, gid = __builtin_amdgcn_readlane(id, u), gp = __builtin_amdgcn_readlane(pt, u);
-                 const int from = max(it.low - tu, 0), to = min(t1 - tu, 8);                    // tokens [from, to) of the group
-                 rows.off[u] = (int64_t)max(gid, 0) * g.st_page + (int64_t)(tu - gp * g.by_page.d) * g.st_tok;
-                 rows.pos[u] = tu;
-                 rows.mask[u] = gid < 0 || from >= to ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
-                 if constexpr (Wave::CODES) {
-                   const int64_t at_scale = scale_at(g, max(gid, 0), h, tu - gp * g.by_page.d);
-                   rows.scale = u == 0 || ((lane >> 3) % Wave::GR) == u ? at_scale : rows.scale;
-                 }
+                 rows.off[u] = of_lane(off, 8 * u);
+                 rows.pos[u] = tb + u * 8;
+                 rows.mask[u] = __builtin_amdgcn_readlane(mask, 8 * u);
                }
-               if constexpr (Wave::CODES) rows.scale += lane & 7;
+               if constexpr (Wave::CODES) rows.scale = scale_at(g, max(there, 0), h, in) + (lane & 7);
              } else {
 #pragma unroll
                for (int u = 0; u < Wave::GR; ++u) {
@@ -616,22 +621,18 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   at.run(g, h, lds + wave * Wave::LDS, (b - a - wave + WAVES - 1) / WAVES, Wave::lane_offset() + (uint32_t)(lane & 7) * (uint32_t)g.st_tok,
          [&](int i) {
            typename Wave::Rows rows;
-           const int t0 = tile_slot(i), e = (t0 + min(lane, Wave::GR - 1) * 8) >> shift;
-           const int2 blk = list[min(e, head.x - 1)];              // lane u < GR: the block of group u
-           const int first = blk.y % per << shift;
+           const int t0 = tile_slot(i), t = t0 + (lane >> 3) % Wave::GR * 8, in = t & (g.block - 1);      // lanes 8 u .. 8 u + 7: group u
+           const int2 blk = list[min(t >> shift, head.x - 1)];
+           const int page_row = (blk.y % per << shift) + in, pos = (blk.y << shift) + in, n = head.y + 1 - pos;          // tokens up to the query's own
+           const int mask = blk.x < 0 || n <= 0 || t >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
+           const int64_t off = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)page_row * g.st_tok;
 #pragma unroll
            for (int u = 0; u < Wave::GR; ++u) {
-             const int in = (t0 + u * 8) & (g.block - 1), id = __builtin_amdgcn_readlane(blk.x, u);
-             const int pos = (__builtin_amdgcn_readlane(blk.y, u) << shift) + in, n = head.y + 1 - pos;         // tokens up to the query's own
-             rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(__builtin_amdgcn_readlane(first, u) + in) * g.st_tok;
-             rows.pos[u] = pos;
-             rows.mask[u] = id < 0 || n <= 0 || t0 + u * 8 >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
-             if constexpr (Wave::CODES) {
-               const int64_t at_scale = scale_at(g, max(id, 0), h, __builtin_amdgcn_readlane(first, u) + in);
-               rows.scale = u == 0 || ((lane >> 3) % Wave::GR) == u ? at_scale : rows.scale;
-             }
+             rows.off[u] = of_lane(off, 8 * u);
+             rows.pos[u] = __builtin_amdgcn_readlane(pos, 8 * u);
+             rows.mask[u] = __builtin_amdgcn_readlane(mask, 8 * u);
            }
-           if constexpr (Wave::CODES) rows.scale += lane & 7;
+           if constexpr (Wave::CODES) rows.scale = scale_at(g, max(blk.x, 0), h, page_row) + (lane & 7);
            return rows;
          },
          [&](int) { return true; });                               // (all rows are the same token's)
