@@ -35,11 +35,11 @@ __device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
 }
 
 // One wavefront's share of an item piece.
-// T, D: storage, head dimension; RT: tiles of 16 query rows; STREAM: the cache is read once (non-temporal loads)
+// T, D: storage, head dimension; RT: tiles of 16 query rows; STREAM: the cache is read once (non-temporal loads); UNIFORM: 8 tokens always lie in one page
 // A load instruction covers 8 rows x 128 bytes, whole cache lines: lane (r, kg) takes 16 bytes of row r mod 8, in the first half of its line for
 // r < 8, in the second for r >= 8.  Keys of 16 rows then change places between two registers to make plain operands; values go to LDS anyway.
 // (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of 6.5.)
-template <typename T, int D, int RT, bool STREAM>
+template <typename T, int D, int RT, bool STREAM, bool UNIFORM>
 struct WaveAttend {
   using Row = typename Cached<T>::Row;
   static constexpr bool BF = Cached<T>::bf16, CODES = Cached<T>::codes;
@@ -71,12 +71,19 @@ struct WaveAttend {
 
   static constexpr int GR = TOK / 8;                              // groups of 8 tokens per tile
 
-  // The cached rows of a tile: byte offset of the lane's row of each group of 8, the position of the group's first token, and which of
-  // its tokens anyone may see (the rows of the others are readable all the same).
+  // The cached rows of a tile, in groups of 8 tokens; lanes 8 u .. 8 u + 7 (of GR x 8) hold what is said of group u, in vector registers (as scalars they would be
+  // spilled to those): the byte offset of the group's first row (not UNIFORM: off[u], of the lane's row of group u), the position of its first token,
+  // and which of its tokens anyone may see (the rows of the others are readable all the same).
   struct Rows {
-    int64_t off[GR];
-    int pos[GR], mask[GR];
+    int64_t off[UNIFORM ? 1 : GR];
+    int pos, mask;
     int64_t scale;                                                 // codes: where the scales of token lane % TOK of the tile are
+    __device__ __forceinline__ int64_t offset(int u) const {
+      if constexpr (UNIFORM) return of_lane(off[0], 8 * u);
+      else return off[u];
+    }
+    __device__ __forceinline__ int pos_of(int u) const { return __builtin_amdgcn_readlane(pos, 8 * u); }
+    __device__ __forceinline__ int mask_of(int u) const { return __builtin_amdgcn_readlane(mask, 8 * u); }
   };
   static __device__ __forceinline__ int lane_offset() { return (NL > 1 ? ((threadIdx.x >> 3) & 1) * 64 : 0) + ((threadIdx.x >> 4) & 3) * 16; }
   // where query piece f of a lane lies in its row: the channels that piece f of a key has
@@ -89,7 +96,7 @@ struct WaveAttend {
 #pragma unroll
     for (int s = 0; s < SUB; ++s) {
       if constexpr (NL == 1) {
-        const int64_t first = r.off[2 * s], second = r.off[2 * s + 1];          // (chosen by value: an address chosen by the lane would put Rows in scratch)
+        const int64_t first = r.offset(2 * s), second = r.offset(2 * s + 1);
         const char* p = base + (threadIdx.x & 8 ? second : first) + at;
         f[s][0].u = STREAM ? gload128_stream(p) : gload128(p);
       } else {
@@ -97,7 +104,7 @@ struct WaveAttend {
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int j = 0; j < NL / 2; ++j) {
-            const char* p = base + r.off[2 * s + u] + at + j * 128;
+            const char* p = base + r.offset(2 * s + u) + at + j * 128;
             f[s][2 * j + u].u = STREAM ? gload128_stream(p) : gload128(p);
           }
       }
@@ -167,8 +174,8 @@ struct WaveAttend {
       for (int e = 0; e < 4; ++e)
         for (int k = 0; k < 4; ++k) {
           const int slot = 4 * k + e, in = slot & 7;
-          const int pos = (k >> 1 ? rows.pos[2 * u + 1] : rows.pos[2 * u]) + in;
-          const bool there = ((k >> 1 ? rows.mask[2 * u + 1] : rows.mask[2 * u]) >> in) & 1;
+          const int pos = (k >> 1 ? rows.pos_of(2 * u + 1) : rows.pos_of(2 * u)) + in;
+          const bool there = ((k >> 1 ? rows.mask_of(2 * u + 1) : rows.mask_of(2 * u)) >> in) & 1;
           const char* v = vlds + (u * 16 + slot) * VROW;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
@@ -221,14 +228,12 @@ struct WaveAttend {
       }
       nxt = rows_of(min(i + 2, n - 1));
       // ---- what nobody may see
-      bool all = clean(i);
-#pragma unroll
-      for (int u = 0; u < GR; ++u) all = all && here.mask[u] == 0xff;
+      const bool all = clean(i) && __all(here.mask == 0xff);
       if (!all) {
 #pragma unroll
         for (int u = 0; u < SUB; ++u) {
-          const int pos0 = (kg < 2 ? here.pos[2 * u] : here.pos[2 * u + 1]) + 4 * (kg & 1);
-          const int bits = (kg < 2 ? here.mask[2 * u] : here.mask[2 * u + 1]) >> (4 * (kg & 1));
+          const int pos0 = (kg < 2 ? here.pos_of(2 * u) : here.pos_of(2 * u + 1)) + 4 * (kg & 1);
+          const int bits = (kg < 2 ? here.mask_of(2 * u) : here.mask_of(2 * u + 1)) >> (4 * (kg & 1));
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -282,7 +287,7 @@ struct WaveAttend {
         constexpr int PER = NL > 1 ? 1 : 2;                        // groups of 8 rows per load
 #pragma unroll
         for (int u = 0; u < GR; u += PER) {
-          const int first = here.mask[u], second = here.mask[u + PER - 1], mask = lane & 8 && PER == 2 ? second : first;
+          const int first = here.mask_of(u), second = here.mask_of(u + PER - 1), mask = lane & 8 && PER == 2 ? second : first;
           const float scale = value_scale(scales_of(scales, 8 * u + (PER == 1 ? r7 : r)));
           const u32x4 c = vf[u / 2][PER == 1 ? u % 2 : 0].u;
 #pragma unroll
@@ -303,7 +308,7 @@ struct WaveAttend {
           for (int j = 0; j < NF / 2; ++j) {
             u32x4 w = vf[u / 2][2 * j + u % 2].u;
             if (!all) {
-              if (!((here.mask[u] >> r7) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
+              if (!((here.mask_of(u) >> r7) & 1)) w = (u32x4){0u, 0u, 0u, 0u};
               odd = odd || not_finite(w);
             }
             *(u32x4*)(vw + u * 8 * VROW + j * 128) = w;
@@ -345,12 +350,12 @@ struct WaveAttend {
 };
 
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
-template <typename T, int D, int RT, bool STREAM>
-constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT, STREAM>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
+template <typename T, int D, int RT>
+constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT, true, true>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
 
 // Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
-template <typename T, int D, int RT, bool STREAM, typename Emit>
-__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM>& w, char* lds, int rows, Emit&& emit) {
+template <typename T, int D, int RT, bool STREAM, bool UNIFORM, typename Emit>
+__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM, UNIFORM>& w, char* lds, int rows, Emit&& emit) {
   constexpr int W = kPagedThreads / 64, R = 16 * RT, STR = D + 2;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = threadIdx.x >> 6;
   float* mine = (float*)lds + (size_t)wave * R * STR;
@@ -463,9 +468,9 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   // Non-temporal loads where the cache is read once for sure; with a plan several items of a sequence may read the same rows.  (128 sequences of one token have a
   // plan too: 420 us; 375 with non-temporal loads.)
   constexpr bool STREAM = !PLAN;
-  using Wave = WaveAttend<T, D, RT, STREAM>;
+  using Wave = WaveAttend<T, D, RT, STREAM, UNIFORM>;
   constexpr int WAVES = kPagedThreads / 64;
-  __shared__ __align__(16) char lds[attend_lds<T, D, RT, STREAM>()];
+  __shared__ __align__(16) char lds[attend_lds<T, D, RT>()];
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
@@ -506,7 +511,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     const uint32_t lane_at = Wave::lane_offset() + (UNIFORM ? (uint32_t)(lane & 7) * (uint32_t)g.st_tok : 0u);
     at.run(g, h, lds + wave * Wave::LDS, mine, lane_at,
            [&](int i) {
-             typename Wave::Rows rows;
+             typename Wave::Rows rows{};
              const int tb = tile0(i);
              if constexpr (UNIFORM) {                              // lanes 8 u .. 8 u + 7 look up the page of group u (scalar code took twice as long as all else)
                const int t = tb + (lane >> 3) % Wave::GR * 8, pt = page_of(g, t), in = t - pt * g.by_page.d;
@@ -514,26 +519,23 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
                bool odd = false;
                const int id = page_id(g, seq, pt, &odd), there = from < to ? id : -1;
                bad = bad || (odd && from < to);
-               const int mask = there < 0 ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
-               const int64_t off = (int64_t)max(there, 0) * g.st_page + (int64_t)in * g.st_tok;
-#pragma unroll
-               for (int u = 0; u < Wave::GR; ++u) {
-                 rows.off[u] = of_lane(off, 8 * u);
-                 rows.pos[u] = tb + u * 8;
-                 rows.mask[u] = __builtin_amdgcn_readlane(mask, 8 * u);
-               }
+               rows.off[0] = (int64_t)max(there, 0) * g.st_page + (int64_t)in * g.st_tok;
+               rows.pos = t;
+               rows.mask = there < 0 ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
                if constexpr (Wave::CODES) rows.scale = scale_at(g, max(there, 0), h, in) + (lane & 7);
              } else {
+               const int mine = (lane >> 3) % Wave::GR;
+               rows.pos = tb + mine * 8;
 #pragma unroll
                for (int u = 0; u < Wave::GR; ++u) {
                  const int t = tb + u * 8 + (lane & 7), pt = page_of(g, t);
                  const int id = t >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
                  rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
-                 rows.pos[u] = tb + u * 8;
-                 rows.mask[u] = (int)(__ballot(id >= 0) & 0xff);
+                 const int mask = (int)(__ballot(id >= 0) & 0xff);
+                 rows.mask = u == mine ? mask : rows.mask;
                  if constexpr (Wave::CODES) {
                    const int64_t at_scale = scale_at(g, max(id, 0), h, t - pt * g.by_page.d);
-                   rows.scale = u == 0 || ((lane >> 3) % Wave::GR) == u ? at_scale : rows.scale;
+                   rows.scale = u == mine ? at_scale : rows.scale;
                  }
                }
              }
@@ -544,7 +546,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     // ---- out, or a partial
     const bool whole = p.whole();
     float* slot = partial_slot(g, w, x == sh.begin);
-    join_waves<T, D, RT, STREAM>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
+    join_waves<T, D, RT, STREAM, UNIFORM>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
       if (whole) {
         int token, head;
         p.place(g, row, &token, &head);
@@ -592,9 +594,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join_kernel(PagedGeom g) 
 // ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g) {
-  using Wave = WaveAttend<T, D, 1, true>;
+  using Wave = WaveAttend<T, D, 1, true, true>;
   constexpr int WAVES = kPagedThreads / 64;
-  __shared__ __align__(16) char lds[attend_lds<T, D, 1, true>()];
+  __shared__ __align__(16) char lds[attend_lds<T, D, 1>()];
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int h = blockIdx.y, local = blockIdx.z, token = g.row0 + local, split = blockIdx.x;
@@ -620,18 +622,13 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   const auto tile_slot = [&](int i) { return (a + wave + i * WAVES) * Wave::TOK; };
   at.run(g, h, lds + wave * Wave::LDS, (b - a - wave + WAVES - 1) / WAVES, Wave::lane_offset() + (uint32_t)(lane & 7) * (uint32_t)g.st_tok,
          [&](int i) {
-           typename Wave::Rows rows;
+           typename Wave::Rows rows{};
            const int t0 = tile_slot(i), t = t0 + (lane >> 3) % Wave::GR * 8, in = t & (g.block - 1);      // lanes 8 u .. 8 u + 7: group u
            const int2 blk = list[min(t >> shift, head.x - 1)];
            const int page_row = (blk.y % per << shift) + in, pos = (blk.y << shift) + in, n = head.y + 1 - pos;          // tokens up to the query's own
-           const int mask = blk.x < 0 || n <= 0 || t >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
-           const int64_t off = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)page_row * g.st_tok;
-#pragma unroll
-           for (int u = 0; u < Wave::GR; ++u) {
-             rows.off[u] = of_lane(off, 8 * u);
-             rows.pos[u] = __builtin_amdgcn_readlane(pos, 8 * u);
-             rows.mask[u] = __builtin_amdgcn_readlane(mask, 8 * u);
-           }
+           rows.off[0] = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)page_row * g.st_tok;
+           rows.pos = pos;
+           rows.mask = blk.x < 0 || n <= 0 || t >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
            if constexpr (Wave::CODES) rows.scale = scale_at(g, max(blk.x, 0), h, page_row) + (lane & 7);
            return rows;
          },
@@ -643,7 +640,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   if (a == b) return;
   const int piece = tiles < g.splits ? a : split;
   float* slot = part + (int64_t)piece * 16 * (D + 2);
-  join_waves<T, D, 1, true>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
+  join_waves<T, D, 1, true, true>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
       store_out<typename Wave::Row>(g, token, h * g.G + row, c, o, m, l);
     } else {
