@@ -67,6 +67,7 @@ struct PagedGeom {
   int4* joins;                            // [splits][2] what paged_join_kernel has to know of the item that starts in a share and ends in another
   int plan_room;                          // items the plan has room for; 0: none needed
   int least;                              // units that a workgroup gets at least, with a plan
+  int wide;                               // split kernel: 64 tokens at a time instead of 32
   // append
   int dtype, rot, adjacent;
   Divisor by_half, by_lines;              // rot / 2; rows per token and KV head: query heads, key, value

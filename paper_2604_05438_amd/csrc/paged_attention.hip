@@ -39,13 +39,15 @@ __device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
 // A load instruction covers 8 rows x 128 bytes, whole cache lines: lane (r, kg) takes 16 bytes of row r mod 8, in the first half of its line for
 // r < 8, in the second for r >= 8.  Keys of 16 rows then change places between two registers to make plain operands; values go to LDS anyway.
 // (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of 6.5.)
-template <typename T, int D, int RT, bool STREAM, bool UNIFORM>
+// WIDE: twice as many tokens at a time (codes of 64 channels, whose tiles are otherwise half as large as all others; see paged_api)
+template <typename T, int D, int RT, bool STREAM, bool UNIFORM, bool WIDE = false>
 struct WaveAttend {
   using Row = typename Cached<T>::Row;
   static constexpr bool BF = Cached<T>::bf16, CODES = Cached<T>::codes;
   static constexpr int RB = D * (int)sizeof(Row);                 // bytes of a row, as it is contracted
-  static constexpr int SUB = BF ? 2 : 1;                          // subtiles of 16 tokens that are loaded and contracted together
+  static constexpr int SUB = WIDE ? 4 : BF ? 2 : 1;                          // subtiles of 16 tokens that are loaded and contracted together
   static constexpr int TOK = 16 * SUB;
+  static constexpr int NP = (SUB + 1) / 2;                        // operands of weights: of 32 tokens each (fp32: 16)
   static constexpr int NF = RB / 64;                              // 16-byte pieces of a row per lane
   static constexpr int NL = D * Cached<T>::bytes / 64;            // of the row in the cache: fewer for codes (one, a whole row by 4 lanes, at D = 64)
   static constexpr int VROW = RB + 32;                            // LDS row of V
@@ -166,7 +168,7 @@ struct WaveAttend {
   }
 
   // O^T += V^T P^T of a tile, token by token for the rows that see it
-  __device__ __forceinline__ void add_seen(const PagedFrag (&p)[RT][(SUB + 1) / 2], const Rows& rows, const char* vlds) {
+  __device__ __forceinline__ void add_seen(const PagedFrag (&p)[RT][NP], const Rows& rows, const char* vlds) {
     const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4;
 #pragma unroll
     for (int u = 0; u < SUB; ++u)
@@ -179,7 +181,7 @@ struct WaveAttend {
           const char* v = vlds + (u * 16 + slot) * VROW;
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) {
-            const uint32_t word = __shfl(p[rt][0].u[BF ? 2 * u + e / 2 : e], 16 * k + r);
+            const uint32_t word = __shfl(p[rt][u / 2].u[BF ? 2 * (u & 1) + e / 2 : e], 16 * k + r);
             const float weight = __uint_as_float(!BF ? word : e & 1 ? word & 0xffff0000u : word << 16);
             if (!there || pos < low[rt] || pos > lim[rt]) continue;
 #pragma unroll
@@ -242,7 +244,7 @@ struct WaveAttend {
         }
       }
       // ---- running maximum and sum
-      PagedFrag p[RT][(SUB + 1) / 2];
+      PagedFrag p[RT][NP];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
         float x[SUB][4], mx = -INFINITY;
@@ -275,7 +277,7 @@ struct WaveAttend {
           for (int u = 0; u < SUB; ++u)
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-              p[rt][0].u[2 * u + e] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)x[u][2 * e], (__bf16)x[u][2 * e + 1]});
+              p[rt][u / 2].u[2 * (u & 1) + e] = __builtin_bit_cast(uint32_t, (bf16x2_t){(__bf16)x[u][2 * e], (__bf16)x[u][2 * e + 1]});
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e) p[rt][0].u[e] = __float_as_uint(x[0][e]);
@@ -319,7 +321,9 @@ struct WaveAttend {
         PagedFrag ones;
         ones.u = (u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) lr[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones.v, p[rt][0].v, lr[rt], 0, 0, 0);
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int x = 0; x < NP; ++x) lr[rt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones.v, p[rt][x].v, lr[rt], 0, 0, 0);
       }
       if (!all && __ballot(odd)) {                                 // (0 times such a value is not 0: row by row, without what they do not see)
         add_seen(p, here, vlds);
@@ -327,14 +331,16 @@ struct WaveAttend {
       }
       if constexpr (BF) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          PagedFrag a;
-          const char* at = vlds + (kg * 4 + (r >> 2)) * VROW + ct * 32 + (r & 3) * 8;
-          a.h[0] = lds_read_transposed(at);
-          a.h[1] = lds_read_transposed(at + 16 * VROW);
+        for (int x = 0; x < NP; ++x)
 #pragma unroll
-          for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, p[rt][0].v, o[rt][ct], 0, 0, 0);
-        }
+          for (int ct = 0; ct < CT; ++ct) {
+            PagedFrag a;
+            const char* at = vlds + (x * 32 + kg * 4 + (r >> 2)) * VROW + ct * 32 + (r & 3) * 8;
+            a.h[0] = lds_read_transposed(at);
+            a.h[1] = lds_read_transposed(at + 16 * VROW);
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, p[rt][x].v, o[rt][ct], 0, 0, 0);
+          }
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -350,12 +356,12 @@ struct WaveAttend {
 };
 
 constexpr int pmax(int a, int b) { return a > b ? a : b; }
-template <typename T, int D, int RT>
-constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT, true, true>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
+template <typename T, int D, int RT, bool WIDE = false>
+constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT, true, true, WIDE>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
 
 // Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
-template <typename T, int D, int RT, bool STREAM, bool UNIFORM, typename Emit>
-__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM, UNIFORM>& w, char* lds, int rows, Emit&& emit) {
+template <typename T, int D, int RT, bool STREAM, bool UNIFORM, bool WIDE, typename Emit>
+__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM, UNIFORM, WIDE>& w, char* lds, int rows, Emit&& emit) {
   constexpr int W = kPagedThreads / 64, R = 16 * RT, STR = D + 2;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = threadIdx.x >> 6;
   float* mine = (float*)lds + (size_t)wave * R * STR;
@@ -463,14 +469,14 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
 }
 
 // UNIFORM: 8 tokens always lie in one page
-template <typename T, int D, int RT, bool PLAN, bool UNIFORM>
+template <typename T, int D, int RT, bool PLAN, bool UNIFORM, bool WIDE = false>
 __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
   // Non-temporal loads where the cache is read once for sure; with a plan several items of a sequence may read the same rows.  (128 sequences of one token have a
   // plan too: 420 us; 375 with non-temporal loads.)
   constexpr bool STREAM = !PLAN;
-  using Wave = WaveAttend<T, D, RT, STREAM, UNIFORM>;
+  using Wave = WaveAttend<T, D, RT, STREAM, UNIFORM, WIDE>;
   constexpr int WAVES = kPagedThreads / 64;
-  __shared__ __align__(16) char lds[attend_lds<T, D, RT>()];
+  __shared__ __align__(16) char lds[attend_lds<T, D, RT, WIDE>()];
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
 
@@ -546,7 +552,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     // ---- out, or a partial
     const bool whole = p.whole();
     float* slot = partial_slot(g, w, x == sh.begin);
-    join_waves<T, D, RT, STREAM, UNIFORM>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
+    join_waves<T, D, RT, STREAM, UNIFORM, WIDE>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
       if (whole) {
         int token, head;
         p.place(g, row, &token, &head);
@@ -640,7 +646,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   if (a == b) return;
   const int piece = tiles < g.splits ? a : split;
   float* slot = part + (int64_t)piece * 16 * (D + 2);
-  join_waves<T, D, 1, true, true>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
+  join_waves<T, D, 1, true, true, false>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
       store_out<typename Wave::Row>(g, token, h * g.G + row, c, o, m, l);
     } else {
@@ -656,6 +662,11 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
 template <typename T, int D, int RT>
 static void launch_split(const PagedGeom& g, hipStream_t s) {
   const bool uniform = g.by_page.d % 8 == 0 && g.st_tok < (1ll << 28);           // (offsets of 32 bits within 8 tokens)
+  if constexpr (Cached<T>::codes && D == 64 && RT == 1)
+    if (g.wide && uniform) {
+      hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, false, true, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+      return;
+    }
   const auto kernel = g.plan_room ? uniform ? paged_attend_kernel<T, D, RT, true, true> : paged_attend_kernel<T, D, RT, true, false>
                                   : uniform ? paged_attend_kernel<T, D, RT, false, true> : paged_attend_kernel<T, D, RT, false, false>;
   hipLaunchKernelGGL(kernel, dim3(g.splits), dim3(kPagedThreads), 0, s, g);
