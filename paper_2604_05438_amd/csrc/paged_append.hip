@@ -48,37 +48,70 @@ template <> __device__ __forceinline__ u32x4 pack16<uint16_t>(const float* x) {
 typedef __attribute__((address_space(1))) u32x4* gout128;
 __device__ __forceinline__ void gstore128(void* p, u32x4 v) { *(gout128)p = v; }
 
-// Rows of the cache in 8 bits from the two pieces x, y of a row that a lane holds (the row's `lanes` lanes ask together): codes of both, and the scale
-// byte.  Values that are not finite become NaN and leave the scale alone.
+// A row of the cache in 8 bits out of the two pieces of it that a lane holds (the row's `lanes` lanes ask together): codes of both, and the scale byte.
+// The scale goes by the largest finite element; what is not finite becomes NaN by the conversion.
 struct Coded {
   uint32_t x[2], y[2];
   uint32_t scale;
 };
-__device__ __forceinline__ Coded encode(float* x, float* y, int lanes) {
-  float top = 0.f;
-  const auto size = [](float v) { return __uint_as_float(__float_as_uint(v) & 0x7fffffffu); };
+// top: bits of the row's largest size, f 2^k with 1 <= f < 2; the largest code is 1.75 x 2^8
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  return (uint32_t)min(max((int)(top >> 23) - 8 + ((top & 0x7fffffu) > 0x600000u), kLeastScale), kMostScale);
+}
+typedef short pp_short2 __attribute__((ext_vector_type(2)));
+typedef unsigned short pp_ushort2 __attribute__((ext_vector_type(2)));
+// (the conversions divide by the scale, exactly: the code is the only rounding)
+__device__ __forceinline__ uint32_t codes_of(const float* v, float scale) {
+  pp_short2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, v[0], v[1], scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, v[2], v[3], scale, true);
+  return __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ uint32_t codes_of(uint32_t a, uint32_t b, float scale) {
+  pp_short2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, a), scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, b), scale, true);
+  return __builtin_bit_cast(uint32_t, r);
+}
+// of 32-bit numbers; their sizes compare as integers
+__device__ __forceinline__ Coded encode(const float* x, const float* y, int lanes) {
+  const auto size = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
+  uint32_t top = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float a = size(x[e]), b = size(y[e]);
-    if (!(a < INFINITY)) x[e] = __uint_as_float(0x7fc00000u);
-    if (!(b < INFINITY)) y[e] = __uint_as_float(0x7fc00000u);
-    top = fmaxf(top, a < INFINITY ? a : 0.f);
-    top = fmaxf(top, b < INFINITY ? b : 0.f);
+  for (int e = 0; e < 8; ++e) top = max(top, max(size(x[e]), size(y[e])));
+  if (__any(top >= 0x7f800000u)) {
+    const auto finite = [&](float v) { return size(v) < 0x7f800000u ? size(v) : 0u; };
+    top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, max(finite(x[e]), finite(y[e])));
   }
-  top = lanes_reduce(top, lanes, MaxOp());
-  // top = f 2^k with 1 <= f < 2; the largest code is 1.75 x 2^8
-  const uint32_t bits = __float_as_uint(top);
-  const int byte = min(max((int)(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u), kLeastScale), kMostScale);
-  const float by = __uint_as_float((uint32_t)(254 - byte) << 23);         // (an exact product: the code is the only rounding)
   Coded c;
-  c.scale = (uint32_t)byte;
+  c.scale = scale_byte(lanes_reduce(top, lanes, MaxOp()));
+  const float scale = __uint_as_float(c.scale << 23);
+  c.x[0] = codes_of(x, scale); c.x[1] = codes_of(x + 4, scale);
+  c.y[0] = codes_of(y, scale); c.y[1] = codes_of(y + 4, scale);
+  return c;
+}
+// of bf16 pairs as they are
+__device__ __forceinline__ Coded encode(u32x4 x, u32x4 y, int lanes) {
+  const auto sizes = [](uint32_t w) { return __builtin_bit_cast(pp_ushort2, w & 0x7fff7fffu); };
+  pp_ushort2 both = {0, 0};
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    c.x[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k] * by, x[4 * k + 1] * by, 0, false);
-    c.x[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * k + 2] * by, x[4 * k + 3] * by, (int)c.x[k], true);
-    c.y[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k] * by, y[4 * k + 1] * by, 0, false);
-    c.y[k] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * k + 2] * by, y[4 * k + 3] * by, (int)c.y[k], true);
+  for (int e = 0; e < 4; ++e) both = __builtin_elementwise_max(both, __builtin_elementwise_max(sizes(x[e]), sizes(y[e])));
+  if (__any(max((uint32_t)both.x, (uint32_t)both.y) >= 0x7f80u)) {
+    const auto finite = [&](uint32_t w) {
+      const pp_ushort2 s = sizes(w);
+      return (pp_ushort2){s.x < 0x7f80 ? s.x : (unsigned short)0, s.y < 0x7f80 ? s.y : (unsigned short)0};
+    };
+    both = (pp_ushort2){0, 0};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) both = __builtin_elementwise_max(both, __builtin_elementwise_max(finite(x[e]), finite(y[e])));
   }
+  Coded c;
+  c.scale = scale_byte(lanes_reduce(max((uint32_t)both.x, (uint32_t)both.y) << 16, lanes, MaxOp()));
+  const float scale = __uint_as_float(c.scale << 23);
+  c.x[0] = codes_of(x.x, x.y, scale); c.x[1] = codes_of(x.z, x.w, scale);
+  c.y[0] = codes_of(y.x, y.y, scale); c.y[1] = codes_of(y.z, y.w, scale);
   return c;
 }
 
@@ -127,8 +160,11 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
   __syncthreads();
   const int lines = g.by_lines.d;                                // query heads, the key, the value
   const int rotated = g.rot / (2 * EPL);                         // pairs of pieces that turn
-  for (int i = tid; i < n * lines * PAIRS; i += kPagedThreads) {
-    const int p = i % PAIRS, t = g.by_lines(i / PAIRS), line = i / PAIRS - t * lines;
+  // line by line (query heads, key, value), so that the lanes of a wavefront do the same; (i + 1/2) / m in 32 bits is off by less than 2^-11 below 2^14
+  const int m = n * PAIRS;
+  const float each = 1.f / (float)m;
+  for (int i = tid; i < lines * m; i += kPagedThreads) {
+    const int line = (int)(((float)i + 0.5f) * each), j = i - line * m, p = j % PAIRS, t = j / PAIRS;
     const bool is_v = line == lines - 1, is_k = line == lines - 2;
     const char* src = is_v   ? g.v + (int64_t)(first_row + t) * g.v_row + h * g.v_head
                       : is_k ? g.k + (int64_t)(first_row + t) * g.k_row + h * g.k_head
@@ -137,6 +173,16 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
     // the two pieces: first and second halves of the pairs, or neighbours
     const int pa = turns && !g.adjacent ? p : 2 * p, pb = turns && !g.adjacent ? p + rotated : 2 * p + 1;
     u32x4 ua = gload128(src + pa * 16), ub = gload128(src + pb * 16);
+    u32x4 wa, wb;
+    const char* weights = nullptr;
+    if constexpr (NORM) {
+      weights = is_v ? nullptr : is_k ? g.kw : g.qw;
+      if (weights) {
+        weights += is_k ? h * g.kw_head : (int64_t)(h * g.G + line) * g.qw_head;
+        wa = gload128(weights + pa * 16);
+        wb = gload128(weights + pb * 16);
+      }
+    }
     char* dst;
     uint8_t* scale_dst = nullptr;
     if (line < lines - 2) {
@@ -147,35 +193,26 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
       lost = lost || id < 0;
       if constexpr (CODES) scale_dst = (uint8_t*)(g.S + scale_at(g, max(id, 0), h, lo + t - pt * g.by_page.d)) + is_v;
     }
-    const bool codes = CODES && (is_k || is_v);
-    if (turns || codes || (NORM && !is_v)) {
+    Coded c;
+    if (turns || (!is_v && (NORM || (CODES && is_k)))) {
       float a[EPL], b[EPL], x[EPL], y[EPL];
       Elem<T>::unpack(make_uint4(ua.x, ua.y, ua.z, ua.w), a);
       Elem<T>::unpack(make_uint4(ub.x, ub.y, ub.z, ub.w), b);
-      if constexpr (NORM)
-        if (!is_v) {                                             // (a row's lanes are PAIRS neighbours)
-          float sum = 0.f;
+      if constexpr (NORM) {                                      // (a row's lanes are PAIRS neighbours)
+        float sum = 0.f;
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) sum = fmaf(a[e], a[e], fmaf(b[e], b[e], sum));
-          sum = lanes_sum(sum, PAIRS);
-          const float by = __builtin_amdgcn_rsqf(fmaf(sum, 1.f / D, g.eps));
-          const char* w = is_k ? g.kw : g.qw;
-          if (w) {
-            w += is_k ? h * g.kw_head : (int64_t)(h * g.G + line) * g.qw_head;
-            float wa[EPL], wb[EPL];
-            const u32x4 va = gload128(w + pa * 16), vb = gload128(w + pb * 16);
-            Elem<T>::unpack(make_uint4(va.x, va.y, va.z, va.w), wa);
-            Elem<T>::unpack(make_uint4(vb.x, vb.y, vb.z, vb.w), wb);
+        for (int e = 0; e < EPL; ++e) sum = fmaf(a[e], a[e], fmaf(b[e], b[e], sum));
+        const float by = __builtin_amdgcn_rsqf(fmaf(lanes_sum(sum, PAIRS), 1.f / D, g.eps));
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) {
-              a[e] = a[e] * by * (wa[e] + g.w_offset);
-              b[e] = b[e] * by * (wb[e] + g.w_offset);
-            }
-          } else {
+        for (int e = 0; e < EPL; ++e) { a[e] *= by; b[e] *= by; }
+        if (weights) {
+          float fa[EPL], fb[EPL];
+          Elem<T>::unpack(make_uint4(wa.x, wa.y, wa.z, wa.w), fa);
+          Elem<T>::unpack(make_uint4(wb.x, wb.y, wb.z, wb.w), fb);
 #pragma unroll
-            for (int e = 0; e < EPL; ++e) { a[e] *= by; b[e] *= by; }
-          }
+          for (int e = 0; e < EPL; ++e) { a[e] *= fa[e] + g.w_offset; b[e] *= fb[e] + g.w_offset; }
         }
+      }
       const float2* cs = turn + t * half + p * EPL;
       if ((CODES || NORM) && !turns) {
 #pragma unroll
@@ -183,39 +220,46 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
       } else if (g.adjacent) {
 #pragma unroll
         for (int e = 0; e < EPL; e += 2) {
-          const float2 c = cs[e / 2], c2 = cs[EPL / 2 + e / 2];
-          x[e] = a[e] * c.x - a[e + 1] * c.y;
-          x[e + 1] = a[e] * c.y + a[e + 1] * c.x;
+          const float2 c0 = cs[e / 2], c2 = cs[EPL / 2 + e / 2];
+          x[e] = a[e] * c0.x - a[e + 1] * c0.y;
+          x[e + 1] = a[e] * c0.y + a[e + 1] * c0.x;
           y[e] = b[e] * c2.x - b[e + 1] * c2.y;
           y[e + 1] = b[e] * c2.y + b[e + 1] * c2.x;
         }
       } else {
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
-          const float2 c = cs[e];
-          x[e] = a[e] * c.x - b[e] * c.y;
-          y[e] = a[e] * c.y + b[e] * c.x;
+          const float2 c0 = cs[e];
+          x[e] = a[e] * c0.x - b[e] * c0.y;
+          y[e] = a[e] * c0.y + b[e] * c0.x;
         }
       }
-      if constexpr (CODES)
-        if (codes) {
-          const Coded c = encode(x, y, PAIRS);
-          if (dst) {
-            typedef __attribute__((address_space(1))) uint64_t* gout64;
-            *(gout64)(dst + pa * 8) = (uint64_t)c.x[1] << 32 | c.x[0];
-            *(gout64)(dst + pb * 8) = (uint64_t)c.y[1] << 32 | c.y[0];
-            if (p == 0) *scale_dst = (uint8_t)c.scale;
-            dst = nullptr;
-          }
-          const float scale = __uint_as_float(c.scale << 23);    // (the key as stored, for the mean)
-          ua = decode8(c.x[0], c.x[1], scale);
-          ub = decode8(c.y[0], c.y[1], scale);
-        }
-      if (!codes) {
+      bool packed = true;
+      if constexpr (CODES) {
+        packed = !is_k;
+        if (is_k) c = encode(x, y, PAIRS);
+      }
+      if (packed) {
         ua = pack16<T>(x);
         ub = pack16<T>(y);
       }
     }
+    if constexpr (CODES)
+      if (is_k || is_v) {
+        if (is_v) c = encode(ua, ub, PAIRS);
+        if (dst) {
+          typedef __attribute__((address_space(1))) uint64_t* gout64;
+          *(gout64)(dst + pa * 8) = (uint64_t)c.x[1] << 32 | c.x[0];
+          *(gout64)(dst + pb * 8) = (uint64_t)c.y[1] << 32 | c.y[0];
+          if (p == 0) *scale_dst = (uint8_t)c.scale;
+          dst = nullptr;
+        }
+        if (is_k && fills) {                                     // the key as stored, for the mean
+          const float scale = __uint_as_float(c.scale << 23);
+          ua = decode8(c.x[0], c.x[1], scale);
+          ub = decode8(c.y[0], c.y[1], scale);
+        }
+      }
     if (dst) {
       gstore128(dst + pa * 16, ua);
       gstore128(dst + pb * 16, ub);
