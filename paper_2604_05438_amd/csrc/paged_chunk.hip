@@ -216,10 +216,14 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
         char* const row = lds + buf * 2 * Tile::BYTES + (half * kChunkTokens + r) * RB;
         const int kd = (c ^ key_swap<D>(r)) * 16, vd = Tile::BYTES + (c ^ value_swap<D>(r)) * 16;
         const float ks = key_scale(ahead_scale), vs = value_scale(ahead_scale);
-        *(u32x4*)(row + kd) = decode8(k.x, k.y, ks);
-        *(u32x4*)(row + (kd ^ 16)) = decode8(k.z, k.w, ks);
-        *(u32x4*)(row + vd) = decode8(v.x, v.y, vs);
-        *(u32x4*)(row + (vd ^ 16)) = decode8(v.z, v.w, vs);
+        // d = 128: 8 lanes write 128 bytes at a time, half of them the second piece first, so that they meet in no bank (7 % of the whole; at d = 64, where only
+        // values meet, and registers are short, it costs 2 %)
+        const bool x = D == 128 && (lane & 4);
+        const int k1 = kd ^ (x ? 16 : 0), v1 = vd ^ (x ? 16 : 0);
+        *(u32x4*)(row + k1) = decode8(x ? k.z : k.x, x ? k.w : k.y, ks);
+        *(u32x4*)(row + (k1 ^ 16)) = decode8(x ? k.x : k.z, x ? k.y : k.w, ks);
+        *(u32x4*)(row + v1) = decode8(x ? v.z : v.x, x ? v.w : v.y, vs);
+        *(u32x4*)(row + (v1 ^ 16)) = decode8(x ? v.x : v.z, x ? v.y : v.w, vs);
         if (lane == 0) {
           if constexpr (Tile::CODE_ROWS == 8) ((uint8_t*)sh_present[buf])[half * 8 + wave] = (uint8_t)ahead_present;
           else sh_present[buf][half * 4 + wave] = (uint16_t)ahead_present;
@@ -248,9 +252,9 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
         if (more) request(i + 1, false);
       // one load at each of four places per 64 tokens: first those of K, then those of V
       const auto spread = [&](int half, int y) {
-        if constexpr (CODES) {                                     // (decoded while the products with the keys are under way)
+        if constexpr (CODES) {                                     // (before the products with the keys: behind them 1.5 % more, among the weights 2.5 %)
           const int j = (i + 1) * Tile::HALVES + half;
-          if (!more || y != 1) return;
+          if (!more || y != 0) return;
           unpack(j);
           if (j + 1 < n * Tile::HALVES) fetch(j + 1);
         } else if constexpr (UNIFORM) {
