@@ -170,8 +170,9 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
                       : is_k ? g.k + (int64_t)(first_row + t) * g.k_row + h * g.k_head
                              : g.q + (int64_t)(first_row + t) * g.q_row + (int64_t)(h * g.G + line) * g.q_head;
     const bool turns = !is_v && p < rotated;
-    // the two pieces: first and second halves of the pairs, or neighbours
-    const int pa = turns && !g.adjacent ? p : 2 * p, pb = turns && !g.adjacent ? p + rotated : 2 * p + 1;
+    // the two pieces: first and second halves of the pairs; of the row, which a row's lanes then read and write without gaps; or neighbours
+    const bool whole = is_v || rotated == PAIRS || rotated == 0, first = whole || (turns && !g.adjacent);
+    const int pa = first ? p : 2 * p, pb = whole ? p + PAIRS : first ? p + rotated : 2 * p + 1;
     u32x4 ua = gload128(src + pa * 16), ub = gload128(src + pb * 16);
     u32x4 wa, wb;
     const char* weights = nullptr;
@@ -213,14 +214,14 @@ __global__ __launch_bounds__(kPagedThreads) void paged_append_kernel(PagedGeom g
           for (int e = 0; e < EPL; ++e) { a[e] *= fa[e] + g.w_offset; b[e] *= fb[e] + g.w_offset; }
         }
       }
-      const float2* cs = turn + t * half + p * EPL;
+      const float2* cs = turn + t * half + (g.adjacent ? pa * (EPL / 2) : p * EPL);
       if ((CODES || NORM) && !turns) {
 #pragma unroll
         for (int e = 0; e < EPL; ++e) { x[e] = a[e]; y[e] = b[e]; }
       } else if (g.adjacent) {
 #pragma unroll
         for (int e = 0; e < EPL; e += 2) {
-          const float2 c0 = cs[e / 2], c2 = cs[EPL / 2 + e / 2];
+          const float2 c0 = cs[e / 2], c2 = cs[(pb - pa) * (EPL / 2) + e / 2];
           x[e] = a[e] * c0.x - a[e + 1] * c0.y;
           x[e + 1] = a[e] * c0.y + a[e + 1] * c0.x;
           y[e] = b[e] * c2.x - b[e + 1] * c2.y;

@@ -10,7 +10,7 @@ constexpr int kReadTile = 64;
 
 template <int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(PagedGeom g) {
-  constexpr int PIECES = D / 16, EACH = kReadTile * 2 * PIECES / kPagedThreads;      // 16 codes each; per thread
+  constexpr int PIECES = D / 8, EACH = kReadTile * 2 * PIECES / kPagedThreads;       // 8 codes, 16 bytes of a row; per thread
   const int h = blockIdx.y, tid = threadIdx.x;
   const FoundSeq f = find_seq(g, blockIdx.x, [&](const PagedSeq& s) { return (s.cached + s.fresh - 1) / kReadTile - s.cached / kReadTile + 1; });
   if (f.index < 0) return;
@@ -20,34 +20,29 @@ __global__ __launch_bounds__(kPagedThreads) void paged_read_kernel(PagedGeom g) 
   }
   const int t0 = (f.s.cached / kReadTile + ((int)blockIdx.x - f.before)) * kReadTile;
   const int lo = max(t0, f.s.cached), hi = min(t0 + kReadTile, f.s.cached + f.s.fresh);
-  const int first_row = f.s.row + (lo - f.s.cached);
+  const int first_row = f.s.row + (lo - f.s.cached), p = tid % PIECES;
   bool lost = false;
-  u32x4 w[EACH];
+  uint64_t w[EACH];
   uint32_t scale[EACH];
-  int row[EACH];
-  bool there[EACH];
 #pragma unroll
-  for (int k = 0; k < EACH; ++k) {
-    const int i = tid + k * kPagedThreads, p = i % PIECES, is_v = i / PIECES % 2, t = lo + i / (2 * PIECES);
-    row[k] = t < hi ? first_row + t - lo : -1;
-    if (t >= hi) continue;
+  for (int k = 0; k < EACH; ++k) {                               // keys, then values; absent tokens read page 0
+    const int i = (tid + k * kPagedThreads) / PIECES, is_v = i / kReadTile, t = min(lo + i % kReadTile, hi - 1);
     const int pt = page_of(g, t), id = page_id(g, f.index, pt, &lost), in = t - pt * g.by_page.d;
-    there[k] = id >= 0;
     lost = lost || id < 0;
-    w[k] = gload128((is_v ? g.V : g.K) + (int64_t)max(id, 0) * g.st_page + h * g.st_head + (int64_t)in * g.st_tok + p * 16);
-    scale[k] = ((const uint8_t*)(g.S + scale_at(g, max(id, 0), h, in)))[is_v];
+    w[k] = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint64_t*)((is_v ? g.V : g.K) + (int64_t)max(id, 0) * g.st_page + h * g.st_head +
+                                                                                          (int64_t)in * g.st_tok + p * 8));
+    scale[k] = ((const __attribute__((address_space(1))) uint8_t*)(g.S + scale_at(g, max(id, 0), h, in)))[is_v];
+    if (id < 0) scale[k] = 0x100;
   }
 #pragma unroll
   for (int k = 0; k < EACH; ++k) {
-    const int i = tid + k * kPagedThreads, p = i % PIECES, is_v = i / PIECES % 2;
+    const int i = (tid + k * kPagedThreads) / PIECES, is_v = i / kReadTile, t = lo + i % kReadTile;
     char* const base = is_v ? g.v_out : g.k_out;
-    if (row[k] < 0 || !base) continue;
-    char* dst = base + (int64_t)row[k] * (is_v ? g.v_row : g.k_row) + h * (is_v ? g.v_head : g.k_head) + p * 32;
-    const float by = __uint_as_float(scale[k] << 23);
-    u32x4 a = decode8(w[k].x, w[k].y, by), b = decode8(w[k].z, w[k].w, by);
-    if (!there[k]) a = b = (u32x4){0u, 0u, 0u, 0u};
+    if (t >= hi || !base) continue;
+    char* dst = base + (int64_t)(first_row + t - lo) * (is_v ? g.v_row : g.k_row) + h * (is_v ? g.v_head : g.k_head) + p * 16;
+    u32x4 a = decode8((uint32_t)w[k], (uint32_t)(w[k] >> 32), __uint_as_float((scale[k] & 0xffu) << 23));
+    if (scale[k] & 0x100u) a = (u32x4){0u, 0u, 0u, 0u};
     *(__attribute__((address_space(1))) u32x4*)dst = a;
-    *(__attribute__((address_space(1))) u32x4*)(dst + 16) = b;
   }
   report_pages(g, lost);
 }
