@@ -315,23 +315,22 @@ def tkphi_block_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi
 
 
 def _fits_norms(cfg, io, norms) -> None:
-    """The norms' weights against the config (see _fits)"""
-    if norms is None:
-        return
+    """The norms' weights against the config and the rows (see _fits)"""
     try:
-        (q_heads, q_form), (k_heads, k_form), device, on = norms.q, norms.k, norms.device, io.form[2]
+        form, device, forms, on = norms.form, norms.device, cfg.norm_forms, io.form[2]
     except AttributeError:
         return
-    want = (cfg.kv_dtype, cfg.d_head)
-    if q_form not in (None, want) or k_form not in (None, want) or q_heads not in (0, cfg.n_q_heads) or k_heads not in (0, cfg.n_kv_heads):
-        raise ValueError(f"norms with weights of (heads, (storage type, channels)) {norms.q}, {norms.k} for a config of {cfg.n_q_heads}, {cfg.n_kv_heads} heads, {want}")
+    if form not in forms:
+        raise ValueError(f"norms with weights of (query heads, KV heads, (storage type, channels)) {form}, 0 heads where all share them, for a config of "
+                         f"{cfg.n_q_heads}, {cfg.n_kv_heads}, {(cfg.kv_dtype, cfg.d_head)}")
     if device is not None and device != on:
         raise ValueError(f"norms on GPU {device}, rows on {on} (-1: not on a GPU)")
 
 
 def _append(call, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream) -> None:
     _fits(cfg, step, pool, io, io.heads)
-    _fits_norms(cfg, io, norms)
+    if norms is not None:
+        _fits_norms(cfg, io, norms)
     if 2 * io.angles < cfg.rot_dim:
         raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
     _check(call(cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream))
@@ -472,6 +471,7 @@ def make_paged_config(n_q_heads, n_kv_heads, d_head, dtype, score_scale, K, V, w
                              K.stride(2), int(window), int(rot_dim), int(bool(rot_adjacent)), int(block), int(first_blocks), int(last_blocks),
                              int(top_blocks), int(workgroups))
     cfg.pool, cfg.blocks = _pool_form(K), K.shape[2] // cfg.block if cfg.block > 0 else 0
+    cfg.norm_forms = {(a, b, w) for a in (0, cfg.n_q_heads) for b in (0, cfg.n_kv_heads) for w in (None, (kv, cfg.d_head))}
     cfg.q_heads, cfg.kv_heads, cfg.kv_q_heads = (kv, cfg.d_head, cfg.n_q_heads), (kv, cfg.d_head, cfg.n_kv_heads), (kv, cfg.d_head, cfg.n_kv_heads, cfg.n_q_heads)
     return cfg
 
@@ -526,17 +526,21 @@ def make_quant_pool(K, V, scales, M=None) -> tkphi_quant_pool:
 
 def make_head_norms(q_weight, k_weight, eps: float, offset: float = 0.0) -> tkphi_head_norms:
     """Weights [channels], shared by all heads, or [heads][channels], in the rows' type, or None for ones (offset does not count there)."""
-    strides, notes = [], []
+    strides, heads, form = [], [], None
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _tensor(name, w, 1 if w.dim() == 1 else 2)
-        strides.append(0 if w is None or w.dim() == 1 else w.stride(0))
-        notes.append((0, None) if w is None else (0 if w.dim() == 1 else w.shape[0], (_kv_dtype(w), w.shape[-1])))
-        if w is not None and w.dim() == 2 and w.shape[0] > 1 and w.stride(0) < w.shape[1]:
-            raise ValueError(f"{name}: strides {w.stride()}")
+        if w is None:
+            strides.append(0)
+            heads.append(0)
+            continue
+        _tensor(name, w, 1 if w.dim() == 1 else 2)
+        strides.append(w.stride(0) if w.dim() == 2 and w.shape[0] > 1 else 0)
+        heads.append(w.shape[0] if w.dim() == 2 else 0)
+        if form is not None and form != (_kv_dtype(w), w.shape[-1]):
+            raise ValueError(f"k_weight: {w.dtype}, {w.shape[-1]} channels do not fit q_weight")
+        form = _kv_dtype(w), w.shape[-1]
     norms = tkphi_head_norms(_ptr(q_weight), _ptr(k_weight), *strides, float(eps), float(offset))
-    norms.q, norms.k = notes
-    norms.device = None if q_weight is None and k_weight is None else _one_device(q_weight=q_weight, k_weight=k_weight)
+    norms.form = (*heads, form)
+    norms.device = None if form is None else _one_device(q_weight=q_weight, k_weight=k_weight)
     return norms
 
 

@@ -123,6 +123,30 @@ def test_later_tokens_do_not_touch_earlier_queries(model, lens, token, window, w
             assert not np.isfinite(out[i, G:, 5]).any()
 
 
+@pytest.mark.parametrize("model,lens", [("odd", [(1500, 2), (1100, 1), (5, 1)]), ("one", [(4000, 1)]), ("1b", [(1027, 2), (0, 1)])])
+@pytest.mark.parametrize("page", [16, 56])
+def test_single_tokens_of_64_channels_with_much_work_per_workgroup(model, lens, page):
+    """64 tokens at a time: absent pages, garbage that nobody sees, a value and a scale that are no numbers, windows"""
+    hq, hkv, d = HEADS[model]
+    for case in ("plain", "absent", "garbage", "overflow", "window"):
+        window = 700 if case == "window" else 0
+        st = Q.Step(hq, hkv, d, lens, page, seed=8, garbage=float("nan") if case == "garbage" else None)
+        if case == "absent":
+            st.table[0, [1, 2, 5]] = -1
+        token = lens[0][0]                       # the first new token of the first sequence; later ones, if there are any, see it
+        if case == "overflow":
+            at = st.table[0, token // page], hkv - 1, token % page
+            st.V8[(*at, 5)] = 448.0
+            st.S[(*at, 1)] = 254
+            st.take_values()
+        want = P.attention_oracle(st, window=window)
+        if case == "garbage":
+            st.S[torch.isnan(st.K).any(-1)] = 255
+        st.upload()
+        out, lse = st.call(B.tkphi_quant_attention, st.config(workgroups=1, window=window))
+        P.check(st, out, lse, want)
+
+
 def test_absent_pages_are_seen_by_nobody():
     for model in ("odd", "five"):
         lens = [(100, 1), (40, 30), (30, 1), (3, 2)]
