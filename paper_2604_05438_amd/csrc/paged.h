@@ -68,6 +68,8 @@ struct PagedGeom {
   int plan_room;                          // items the plan has room for; 0: none needed
   int least;                              // units that a workgroup gets at least, with a plan
   int wide;                               // split kernel: 64 tokens at a time instead of 32
+  int pairs;                              // two adjoining KV heads of codes as one item
+  int item_heads;                         // (no plan) items per sequence: KV heads, or pairs of them
   // append
   int dtype, rot, adjacent;
   Divisor by_half, by_lines;              // rot / 2; rows per token and KV head: query heads, key, value

@@ -96,8 +96,13 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   g->tile_rows = chunk ? chunk_rows(g->d) : rows <= 16 ? 16 : kPagedRows;
   const int64_t tiles = std::max<int64_t>(1, up(rows, g->tile_rows));
   g->unit_shift = g->dtype == TKPHI_BF16 && !chunk ? 7 : 6;
+  // Codes of 64 channels whose heads adjoin (tokens outermost): half a cache line per row and head, which two workgroups would fetch twice.  Where the rows of two heads
+  // fit one tile, an item has both: one token each of 32 sequences of 16000 to 32000 tokens 141 instead of 237 us.
+  g->pairs = g->S && g->d == 64 && rows <= 8 && g->n_seqs <= 64 && g->Hkv % 2 == 0 && g->st_head == 64 && g->st_tok >= 128 && g->by_page.d % 8 == 0 && g->st_tok < (1ll << 28);
+  g->item_heads = g->pairs ? g->Hkv / 2 : g->Hkv;
   // at most (what counts is whether it passes 2^31: the product of all four bounds need not fit 64 bits)
-  const int64_t units = std::min<int64_t>((int64_t)g->n_seqs * tiles * up(std::max(g->max_len, 1), 1 << g->unit_shift), 1ll << 31) * g->Hkv;
+  int64_t units = std::min<int64_t>((int64_t)g->n_seqs * tiles * up(std::max(g->max_len, 1), 1 << g->unit_shift), 1ll << 31) * g->item_heads;
+  if (g->pairs && units >= (1ll << 31)) { g->pairs = 0; g->item_heads = g->Hkv; units *= 2; }
   g->least = 2;      // (1 or 4: 16 and 29 instead of 20 us for 16 tokens of a 3B layer alone, 51 and 47 instead of 43 for four chunks of up to 100)
   if (chunk || tiles > 1 || g->n_seqs > 64 || units >= (1ll << 31))
     g->plan_room = (int)std::min<int64_t>((int64_t)g->rows * g->G / g->tile_rows + g->n_seqs, (int64_t)g->n_seqs * tiles);
@@ -105,7 +110,7 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   // Codes of 64 channels, where 32 tokens are 2 KB and a wavefront waits for them most of the time: with 64 at a time one token of each of 32 sequences of 1000,
   // 6000 and 24000 takes 23, 46 and 135 us instead of 22, 56 and 176; one of 32000, 65000 and 131000 tokens 22.4, 23.8 and 31.9 instead of 19.3, 26.4 and 37.9.
   // (128 channels: 234 and 235 for 32 sequences, 9.2 instead of 8.2 for the small ones.)
-  g->wide = g->S && g->d == 64 && !g->plan_room && g->tile_rows == 16 && units >= 8ll * g->splits;
+  g->wide = g->S && g->d == 64 && !g->pairs && !g->plan_room && g->tile_rows == 16 && units >= 8ll * g->splits;
 }
 
 // Query tokens whose scores and pieces the workspace holds at once: where several workgroups share a KV head of one of them it has a

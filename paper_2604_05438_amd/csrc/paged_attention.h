@@ -261,7 +261,7 @@ __device__ __forceinline__ Share<PLAN> share_of(const PagedGeom& g, int w) {
     r.units_incl = wave_scan_incl(r.units);
     r.per_head = __builtin_amdgcn_readlane(r.units_incl, 63);
   }
-  r.all = r.per_head * g.Hkv;
+  r.all = r.per_head * (PLAN ? g.Hkv : g.item_heads);
   r.W = (int)min((Int)g.splits, PLAN ? (r.all + g.least - 1) / g.least : r.all);
   r.begin = r.end = r.each = 0;
   r.rest = 0;
@@ -353,14 +353,13 @@ struct JoinRecord {
 };
 
 // After this workgroup's partial of an item that is not whole is stored: the last one to arrive joins the item's pieces.  (With a plan a
-// kernel of its own does, in which many workgroups share the rows of an item: paged_join_kernel.)
-template <typename T, int D, int NT>
-__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share<false>& sh, const Piece<false>& p, char* lds, int* sh_last) {
+// kernel of its own does, in which many workgroups share the rows of an item: paged_join_kernel.)  rows of the item; row_of: token and query head of one
+template <typename T, int D, int NT, typename RowOf>
+__device__ __forceinline__ void finish_item(const PagedGeom& g, const Share<false>& sh, const Piece<false>& p, int rows, RowOf&& row_of, char* lds, int* sh_last) {
   const int w0 = sh.owner(p.item0), w1 = sh.owner(p.item1 - 1);
   if (!last_to_arrive(g.arrived + w0, w1 - w0 + 1, sh_last)) return;
   const bool first = sh.first_of(w0) == p.item0;          // the first workgroup's share starts with this item
-  join_pieces<T, D, NT, true>(g, w1 - w0 + 1, 0, p.it.rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); },
-                              [&](int row, int* token, int* head) { p.place(g, row, token, head); });
+  join_pieces<T, D, NT, true>(g, w1 - w0 + 1, 0, rows, g.tile_rows, lds, [&](int k) { return partial_slot(g, w0 + k, k > 0 || first); }, row_of);
 }
 
 }  // namespace tkphi

@@ -40,7 +40,9 @@ __device__ __forceinline__ int64_t of_lane(int64_t x, int lane) {
 // r < 8, in the second for r >= 8.  Keys of 16 rows then change places between two registers to make plain operands; values go to LDS anyway.
 // (Half lines at a time: 5.8 TB/s for a step of 32 sequences instead of 6.5.)
 // WIDE: twice as many tokens at a time (codes of 64 channels, whose tiles are otherwise half as large as all others; see paged_api)
-template <typename T, int D, int RT, bool STREAM, bool UNIFORM, bool WIDE = false>
+// PAIR: rows of codes of two KV heads of 64 channels that adjoin, as one of D = 128: query rows 0 .. 7 are of the first, 8 .. 15 of the second; a score takes the
+// head's half of the channels, and of an output row only that half counts
+template <typename T, int D, int RT, bool STREAM, bool UNIFORM, bool WIDE = false, bool PAIR = false>
 struct WaveAttend {
   using Row = typename Cached<T>::Row;
   static constexpr bool BF = Cached<T>::bf16, CODES = Cached<T>::codes;
@@ -91,6 +93,7 @@ struct WaveAttend {
   // where query piece f of a lane lies in its row: the channels that piece f of a key has
   static __device__ __forceinline__ int query_offset(int f) {
     const int kg = (threadIdx.x >> 4) & 3;
+    if constexpr (PAIR) return kg * 32 + (f & 1) * 16;             // (of the row's own head)
     return CODES ? (f >> 1) * 128 + kg * 32 + (f & 1) * 16 : f * 64 + kg * 16;
   }
   // `at`: what the lane adds to the groups' offsets
@@ -113,7 +116,9 @@ struct WaveAttend {
     }
   }
   static __device__ __forceinline__ uint32_t load_scales(const PagedGeom& g, const Rows& r) {
-    if constexpr (CODES) return *(const __attribute__((address_space(1))) uint16_t*)(g.S + r.scale);
+    typedef const __attribute__((address_space(1))) uint16_t* scales_ptr;
+    if constexpr (PAIR) return *(scales_ptr)(g.S + r.scale) | (uint32_t)*(scales_ptr)(g.S + r.scale + g.by_page.d) << 16;
+    else if constexpr (CODES) return *(scales_ptr)(g.S + r.scale);
     else return 0;
   }
   // of the scales that load_scales brought, those of token t of the tile
@@ -133,14 +138,23 @@ struct WaveAttend {
   }
 
   // pieces of a row of codes as they are contracted
-  static __device__ __forceinline__ void decode(const PagedFrag (&c)[NL], float scale, PagedFrag (&k)[NF]) {
+  static __device__ __forceinline__ void decode(const PagedFrag (&c)[NL], uint32_t scales, PagedFrag (&k)[NF]) {
 #pragma unroll
-    for (int j = 0; j < NF; ++j) k[j].u = decode8(c[j / 2].u[2 * (j & 1)], c[j / 2].u[2 * (j & 1) + 1], scale);
+    for (int j = 0; j < NF; ++j) k[j].u = decode8(c[j / 2].u[2 * (j & 1)], c[j / 2].u[2 * (j & 1) + 1], key_scale(PAIR && j >= NF / 2 ? scales >> 16 : scales));
   }
 
   __device__ __forceinline__ pa_floatx4 score(const PagedFrag (&k)[NF], const PagedFrag (&qq)[NF]) {
     pa_floatx4 p = (pa_floatx4){0.f, 0.f, 0.f, 0.f};
-    if constexpr (BF) {
+    if constexpr (PAIR) {                                          // (each half by itself: a key of the one head may be no number)
+      pa_floatx4 p1 = p;
+#pragma unroll
+      for (int j = 0; j < NF / 2; ++j) {
+        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j].v, qq[j].v, p, 0, 0, 0);
+        p1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[NF / 2 + j].v, qq[NF / 2 + j].v, p1, 0, 0, 0);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p[e] = threadIdx.x & 8 ? p1[e] : p[e];
+    } else if constexpr (BF) {
 #pragma unroll
       for (int j = 0; j < NF; ++j) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[j].v, qq[j].v, p, 0, 0, 0);
     } else {
@@ -216,7 +230,7 @@ struct WaveAttend {
         to_operands(kf[u]);
         if constexpr (CODES) {
           PagedFrag k[NF];
-          decode(kf[u], key_scale(scales_of(scales, 16 * u + r)), k);
+          decode(kf[u], scales_of(scales, 16 * u + r), k);
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt) s[u][rt] = score(k, q[rt]);
         } else {
@@ -290,7 +304,8 @@ struct WaveAttend {
 #pragma unroll
         for (int u = 0; u < GR; u += PER) {
           const int first = here.mask_of(u), second = here.mask_of(u + PER - 1), mask = lane & 8 && PER == 2 ? second : first;
-          const float scale = value_scale(scales_of(scales, 8 * u + (PER == 1 ? r7 : r)));
+          const uint32_t both = scales_of(scales, 8 * u + (PER == 1 ? r7 : r));
+          const float scale = value_scale(PAIR ? (lane & 8 ? both >> 16 : both & 0xffffu) : both);
           const u32x4 c = vf[u / 2][PER == 1 ? u % 2 : 0].u;
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
@@ -360,8 +375,8 @@ template <typename T, int D, int RT, bool WIDE = false>
 constexpr int attend_lds() { return pmax(pmax(WaveAttend<T, D, RT, true, true, WIDE>::LDS, 16 * RT * (D + 2) * 4) * (kPagedThreads / 64), join_lds(kPagedThreads, 16 * RT)); }
 
 // Joins the wavefronts of the workgroup through LDS, [waves][rows][D + 2] (O, m, l); emit(row, channel, O of it and the next one, m, l).
-template <typename T, int D, int RT, bool STREAM, bool UNIFORM, bool WIDE, typename Emit>
-__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM, UNIFORM, WIDE>& w, char* lds, int rows, Emit&& emit) {
+template <typename T, int D, int RT, bool STREAM, bool UNIFORM, bool WIDE, bool PAIR, typename Emit>
+__device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM, UNIFORM, WIDE, PAIR>& w, char* lds, int rows, Emit&& emit) {
   constexpr int W = kPagedThreads / 64, R = 16 * RT, STR = D + 2;
   const int lane = threadIdx.x & 63, r = lane & 15, kg = lane >> 4, wave = threadIdx.x >> 6;
   float* mine = (float*)lds + (size_t)wave * R * STR;
@@ -469,13 +484,14 @@ __global__ __launch_bounds__(1024) void paged_plan_kernel(PagedGeom g) {
 }
 
 // UNIFORM: 8 tokens always lie in one page
-template <typename T, int D, int RT, bool PLAN, bool UNIFORM, bool WIDE = false>
+// WIDE, PAIR: see WaveAttend
+template <typename T, int D, int RT, bool PLAN, bool UNIFORM, bool WIDE = false, bool PAIR = false>
 __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
   // Non-temporal loads where the cache is read once for sure; with a plan several items of a sequence may read the same rows.  (128 sequences of one token have a
   // plan too: 420 us; 375 with non-temporal loads.)
   constexpr bool STREAM = !PLAN;
-  using Wave = WaveAttend<T, D, RT, STREAM, UNIFORM, WIDE>;
-  constexpr int WAVES = kPagedThreads / 64;
+  using Wave = WaveAttend<T, D, RT, STREAM, UNIFORM, WIDE, PAIR>;
+  constexpr int WAVES = kPagedThreads / 64, HD = PAIR ? D / 2 : D;
   __shared__ __align__(16) char lds[attend_lds<T, D, RT, WIDE>()];
   __shared__ int sh_last;
   const int lane = threadIdx.x & 63, r = lane & 15, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -489,16 +505,26 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     const auto p = piece_at<PLAN>(g, sh, x, &hint);
     const PagedSeq s = p.s;
     const ItemRange it = p.it;
-    const int h = p.h, seq = p.seq;
+    const int h = PAIR ? 2 * p.h : p.h, seq = p.seq;
+    const int rows = PAIR ? 2 * it.rows : it.rows;                 // (PAIR: those of the second head behind those of the first)
+    const auto place = [&](int row, int* token, int* head) {
+      if constexpr (PAIR) {
+        const int second = row >= it.rows, x = row - (second ? it.rows : 0), i = g.by_group(x);
+        *token = s.row + i;
+        *head = (h + second) * g.G + x - i * g.G;
+      } else {
+        p.place(g, row, token, head);
+      }
+    };
     const int t0 = it.begin + (p.u0 << g.unit_shift), t1 = min(it.begin + (p.u1 << g.unit_shift), it.end);
     bool bad = false;
 
     // ---- this piece: tokens [t0, t1)
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const bool live = rt * 16 + r < it.rows;
+      const bool live = PAIR ? (r & 7) < it.rows : rt * 16 + r < it.rows;
       int token, head;
-      p.place(g, rt * 16 + r, &token, &head);
+      place(PAIR ? (r & 7) + (r >> 3) * it.rows : rt * 16 + r, &token, &head);
       const int i = token - s.row;
       at.lim[rt] = live ? s.cached + i : -1;
       at.low[rt] = live ? (g.window > 0 ? max(0, s.cached + i + 1 - g.window) : 0) : 1;
@@ -506,7 +532,7 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
 #pragma unroll
       for (int f = 0; f < Wave::NF; ++f) {
         at.q[rt][f].u = (u32x4){0u, 0u, 0u, 0u};
-        if (live) at.q[rt][f].u = gload128(src + Wave::query_offset(f));
+        if (live && (!PAIR || f / (Wave::NF / 2) == r >> 3)) at.q[rt][f].u = gload128(src + Wave::query_offset(f));
       }
     }
     const int seen_all = s.cached + (PLAN ? g.by_group(p.tile * g.tile_rows) : 0);         // last token that every row sees
@@ -552,22 +578,28 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
     // ---- out, or a partial
     const bool whole = p.whole();
     float* slot = partial_slot(g, w, x == sh.begin);
-    join_waves<T, D, RT, STREAM, UNIFORM, WIDE>(at, lds, it.rows, [&](int row, int c, float2 o, float m, float l) {
+    join_waves<T, D, RT, STREAM, UNIFORM, WIDE, PAIR>(at, lds, PAIR ? 8 + it.rows : it.rows, [&](int row, int c, float2 o, float m, float l) {
+      if constexpr (PAIR) {
+        const int second = row >> 3;
+        if ((row & 7) >= it.rows || (c >= HD) != (second != 0)) return;
+        row = (row & 7) + (second ? it.rows : 0);
+        c -= second ? HD : 0;
+      }
       if (whole) {
         int token, head;
-        p.place(g, row, &token, &head);
+        place(row, &token, &head);
         store_out<typename Wave::Row>(g, token, head, c, o, m, l);
       } else if constexpr (PLAN) {
-        *(float2*)(slot + row * D + c) = o;
-        if (c == 0) *(float2*)(slot + g.tile_rows * D + row * 2) = make_float2(m, l);
+        *(float2*)(slot + row * HD + c) = o;
+        if (c == 0) *(float2*)(slot + g.tile_rows * HD + row * 2) = make_float2(m, l);
       } else {
-        store_pair(slot + row * D + c, o.x, o.y);
-        if (c == 0) store_pair(slot + g.tile_rows * D + row * 2, m, l);
+        store_pair(slot + row * HD + c, o.x, o.y);
+        if (c == 0) store_pair(slot + g.tile_rows * HD + row * 2, m, l);
       }
     });
     report_pages(g, bad);
     if constexpr (!PLAN) {
-      if (!whole) finish_item<typename Wave::Row, D, kPagedThreads>(g, sh, p, lds, &sh_last);
+      if (!whole) finish_item<typename Wave::Row, HD, kPagedThreads>(g, sh, p, rows, place, lds, &sh_last);
     }
     if constexpr (PLAN) join.note(g, sh, p, w, x == sh.begin);
     __syncthreads();
@@ -646,7 +678,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
   if (a == b) return;
   const int piece = tiles < g.splits ? a : split;
   float* slot = part + (int64_t)piece * 16 * (D + 2);
-  join_waves<T, D, 1, true, true, false>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
+  join_waves<T, D, 1, true, true, false, false>(at, lds, g.G, [&](int row, int c, float2 o, float m, float l) {
     if (whole) {
       store_out<typename Wave::Row>(g, token, h * g.G + row, c, o, m, l);
     } else {
@@ -662,11 +694,16 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
 template <typename T, int D, int RT>
 static void launch_split(const PagedGeom& g, hipStream_t s) {
   const bool uniform = g.by_page.d % 8 == 0 && g.st_tok < (1ll << 28);           // (offsets of 32 bits within 8 tokens)
-  if constexpr (Cached<T>::codes && D == 64 && RT == 1)
+  if constexpr (Cached<T>::codes && D == 64 && RT == 1) {
+    if (g.pairs) {
+      hipLaunchKernelGGL((paged_attend_kernel<T, 128, RT, false, true, false, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
+      return;
+    }
     if (g.wide && uniform) {
       hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, false, true, true>), dim3(g.splits), dim3(kPagedThreads), 0, s, g);
       return;
     }
+  }
   const auto kernel = g.plan_room ? uniform ? paged_attend_kernel<T, D, RT, true, true> : paged_attend_kernel<T, D, RT, true, false>
                                   : uniform ? paged_attend_kernel<T, D, RT, false, true> : paged_attend_kernel<T, D, RT, false, false>;
   hipLaunchKernelGGL(kernel, dim3(g.splits), dim3(kPagedThreads), 0, s, g);

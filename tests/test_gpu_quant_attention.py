@@ -147,6 +147,45 @@ def test_single_tokens_of_64_channels_with_much_work_per_workgroup(model, lens, 
         P.check(st, out, lse, want)
 
 
+PAIRS = {"1b": (32, 8, 64), "odd": (14, 2, 64), "mha": (4, 4, 64), "wide": (16, 2, 64)}
+
+
+@pytest.mark.parametrize("model,lens", [("1b", [(0, 1), (1, 1), (31, 1), (500, 1), (2000, 2), (63, 2)]), ("odd", [(0, 1), (15, 1), (127, 1), (1500, 1)]),
+                                        ("mha", [(0, 8), (100, 5), (7, 1), (900, 3), (3, 0)]), ("wide", [(700, 1), (64, 1)])])
+@pytest.mark.parametrize("page,workgroups", [(16, 0), (8, 1), (104, 3), (64, 40)])
+def test_two_heads_that_adjoin(model, lens, page, workgroups):
+    """Tokens outermost and 64 channels: heads by twos.  Absent pages, garbage, windows; codes of the one head that are no numbers do not touch the other's rows."""
+    hq, hkv, d = PAIRS[model]
+    for case in ("plain", "absent", "garbage", "window", "V", "K"):
+        window = 40 if case == "window" else 0
+        st = Q.Step(hq, hkv, d, lens, page, heads_first=False, seed=8, garbage=float("nan") if case == "garbage" else None, slack_rows=1)
+        if case == "absent":
+            st.table[-1, 0] = -1
+        if case in "VK":
+            n, m = lens[-1]
+            st_at = st.table[-1, n // page], n % page
+            getattr(st, case + "8")[st_at[0], 1, st_at[1], 5] = float("nan")
+            if m:
+                st.take_values()
+        want = P.attention_oracle(st, window=window)
+        if case == "garbage":
+            st.S[torch.isnan(st.K).any(-1)] = 255
+        st.upload()
+        cfg = st.config(workgroups=workgroups, window=window)
+        assert (cfg.stride_head, cfg.stride_tok) == (64, 64 * hkv)
+        out, lse = st.call(B.tkphi_quant_attention, cfg)
+        if case == "K":                          # rows of the head itself: the NaN's weight, and so what comes out, is undefined where the token is seen
+            G = hq // hkv
+            for g in range(hq):
+                if g // G != 1:
+                    for i, (n, m) in enumerate(lens):
+                        for k in range(m):
+                            by, bl = P.bounds("bf16", d, n + m, *want[i][k][g])
+                            assert (np.abs(out[st.first[i] + k, g] - want[i][k][g][0]) <= by).all() and abs(lse[st.first[i] + k, g] - want[i][k][g][1]) <= bl
+        else:
+            P.check(st, out, lse, want)
+
+
 def test_absent_pages_are_seen_by_nobody():
     for model in ("odd", "five"):
         lens = [(100, 1), (40, 30), (30, 1), (3, 2)]
