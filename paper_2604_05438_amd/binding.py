@@ -323,28 +323,28 @@ def _fits_norms(cfg, io, norms) -> None:
     if form not in forms:
         raise ValueError(f"norms with weights of (query heads, KV heads, (storage type, channels)) {form}, 0 heads where all share them, for a config of "
                          f"{cfg.n_q_heads}, {cfg.n_kv_heads}, {(cfg.kv_dtype, cfg.d_head)}")
-    if device is not None and device != on:
+    if device != on and device is not None:
         raise ValueError(f"norms on GPU {device}, rows on {on} (-1: not on a GPU)")
-
-
-def _append(call, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream) -> None:
-    _fits(cfg, step, pool, io, io.heads)
-    if norms is not None:
-        _fits_norms(cfg, io, norms)
-    if 2 * io.angles < cfg.rot_dim:
-        raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
-    _check(call(cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream))
 
 
 def tkphi_norm_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_kv_pool, io: tkphi_new_rows, norms: tkphi_head_norms, workspace_ptr: int,
                       workspace_bytes: int, stream: int) -> None:
-    _append(lib().tkphi_norm_append, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream)
+    _fits(cfg, step, pool, io, io.heads)
+    _fits_norms(cfg, io, norms)
+    if 2 * io.angles < cfg.rot_dim:
+        raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
+    _check(lib().tkphi_norm_append(cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream))
 
 
 def tkphi_quant_append(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_quant_pool, io: tkphi_new_rows, norms, workspace_ptr: int,
                        workspace_bytes: int, stream: int) -> None:
     """norms: tkphi_head_norms or None"""
-    _append(lib().tkphi_quant_append, cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream)
+    _fits(cfg, step, pool, io, io.heads)
+    if norms is not None:
+        _fits_norms(cfg, io, norms)
+    if 2 * io.angles < cfg.rot_dim:
+        raise ValueError(f"inv_freq has {io.angles} elements for rot_dim = {cfg.rot_dim}")
+    _check(lib().tkphi_quant_append(cfg, step, pool, io, norms, workspace_ptr, workspace_bytes, stream))
 
 
 def tkphi_quant_attention(cfg: tkphi_paged_config, step: tkphi_step, pool: tkphi_quant_pool, io: tkphi_attention_rows, workspace_ptr: int,
