@@ -7,7 +7,9 @@
 // A workgroup takes a tile of consecutive cache positions of one sequence (a whole block where means are kept, so that the mean has one
 // writer and a fixed order) and one KV head with its query heads.  Bound by memory: every row is read once and written
 // once, 16 bytes per lane; the angles (64 bits: at position 10^6 a 32-bit product is off by 0.06 rad) are taken once per
-// token, pair and workgroup and shared through LDS.  A chunk of 16001 tokens of a 3B layer (24 / 8 heads of 128): 77 us = 4.3 TB/s, where a large copy
+// token, pair and workgroup and shared through LDS.  A chunk of 16001 tokens of a 3B layer (24 / 8 heads of 128): 77 us = 4.3 TB/s, normed 79 (74 with
+// angles that cost nothing); 12946 tokens of nine sequences of a 1B layer into codes, normed, 43 us = 3.4 TB/s (neither normed nor turned, without means: 37).  Line by
+// line, so that a wavefront's lanes do the same, the last one took 44 us, before 50; with the next task's rows requested ahead 54.  A large copy
 // runs at 4.85; 64 single tokens 5 us.  Several KV heads per workgroup, which share the angles: 76 us, but 21 instead of 11 us for 3000 tokens of
 // a 1B layer; non-temporal loads: 14 instead of 11 us there; two or four tasks per thread at a time: no faster.
 #include "paged.h"

@@ -7,8 +7,8 @@
 // them); the work of all items is cut into equal pieces along the tokens, and the workgroup that finishes an item last joins its pieces (with a plan,
 // paged_join_kernel does).
 //
-// Bound by the read stream where there is much of it: a step of 32 sequences of a 3B layer, 720000 cached tokens (2.96 GB), 455 us = 6.5 TB/s; five tokens
-// each of 8 sequences (283 MB) 62 us.  Short calls are a chain of round trips: a 1B layer over 4002 tokens 9.4 us, of which sequences 0.7, page ids and
+// Bound by the read stream where there is much of it: a step of 32 sequences of a 3B layer, 720000 cached tokens (2.96 GB), 450 us = 6.6 TB/s, as codes (1.49 GB)
+// 235 us = 6.3 TB/s; five tokens each of 8 sequences (283 MB) 61 us.  Short calls are a chain of round trips: a 1B layer over 4002 tokens 8.5 us, of which sequences 0.7, page ids and
 // rows 2.5, the join of the wavefronts 0.6, partials and their count 1.5, the join of 32 pieces 2.5.
 #include "paged_attention.h"
 
