@@ -29,7 +29,7 @@ def weights(st, kind, offset, seed=5):
     return dev, ref
 
 
-def check(st, rot, adjacent=False, norm="shared", offset=0.0, eps=EPS, skip=(), with_q=True, status=0, change=None, spoil=None):
+def check(st, rot, adjacent=False, norm="shared", offset=0.0, eps=EPS, skip=(), with_q=True, status=0, change=None):
     """norm: kind of weights, or None.  change(qkv): the inputs, before they are used."""
     quant = isinstance(st, Q.Step)
     gen = torch.Generator().manual_seed(77)
@@ -231,6 +231,22 @@ def test_codes_of_many_sequences_in_another_order_of_rows():
     r = np.random.default_rng(2)
     lens = [(int(r.integers(0, 40)), int(r.integers(0, 20))) for _ in range(130)]
     check(Q.Step(2, 1, 64, lens, 32, block=16, order=list(r.permutation(130)), slack_rows=5), 64)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_queries_in_place(d):
+    """q_rot may be q itself: the same as in rows of their own, with norms and codes"""
+    st = Q.Step(6, 2, d, [(3, 20), (9, 1)], 16).upload()
+    qkv = torch.randn(st.rows, 10, d, generator=torch.Generator().manual_seed(3)).bfloat16().cuda()
+    q_rot = torch.empty(st.rows, 6, d, device="cuda", dtype=torch.bfloat16)
+    freq, weight = torch.from_numpy(inv_freq(d)).cuda(), torch.full((d,), 0.75, device="cuda", dtype=torch.bfloat16)
+    cfg, step, norms = st.config(rot_dim=d), st.step(), B.make_head_norms(weight, weight, EPS)
+    ws = B.alloc_paged_workspace(B.tkphi_paged_workspace_bytes(cfg, step))
+    for out in (q_rot, qkv[:, :6]):
+        io = B.make_new_rows(qkv[:, :6], qkv[:, 6:8], qkv[:, 8:], out, inv_freq=freq)
+        B.tkphi_quant_append(cfg, step, st.pool(), io, norms, ws.data_ptr(), ws.numel(), B.current_stream_ptr())
+    torch.cuda.synchronize()
+    assert torch.equal(qkv[:, :6], q_rot)
 
 
 # ---- read back ------------------------------------------------------------------------------------------------------------------------
