@@ -98,6 +98,8 @@ void launch_paged_append(const PagedGeom& g, hipStream_t s);
 void launch_paged_read(const PagedGeom& g, hipStream_t s);
 void launch_paged_attention(const PagedGeom& g, hipStream_t s);
 void launch_paged_chunk(const PagedGeom& g, hipStream_t s);
+void launch_split_codes(const PagedGeom& g, hipStream_t s);
+void launch_blocks_codes(const PagedGeom& g, hipStream_t s);
 void launch_block_select(const PagedGeom& g, hipStream_t s);
 void launch_block_attention(const PagedGeom& g, hipStream_t s);
 

@@ -110,7 +110,7 @@ void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   // Codes of 64 channels, where 32 tokens are 2 KB and a wavefront waits for them most of the time: with 64 at a time one token of each of 32 sequences of 1000,
   // 6000 and 24000 takes 23, 46 and 135 us instead of 22, 56 and 176; one of 32000, 65000 and 131000 tokens 22.4, 23.8 and 31.9 instead of 19.3, 26.4 and 37.9.
   // (128 channels: 234 and 235 for 32 sequences, 9.2 instead of 8.2 for the small ones.)
-  g->wide = g->S && g->d == 64 && !g->pairs && !g->plan_room && g->tile_rows == 16 && units >= 8ll * g->splits;
+  g->wide = g->S && g->d == 64 && !g->pairs && g->tile_rows == 16 && units >= 8ll * g->splits;
 }
 
 // Query tokens whose scores and pieces the workspace holds at once: where several workgroups share a KV head of one of them it has a

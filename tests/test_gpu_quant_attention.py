@@ -65,6 +65,15 @@ def test_many_sequences():
     run("five", [(int(r.integers(0, 90)), int(r.integers(0, 12))) for _ in range(90)], 16, slack_rows=1)
 
 
+@pytest.mark.parametrize("model,workgroups", [("one", 1), ("1b", 3), ("odd", 2), ("five", 7)])
+@pytest.mark.parametrize("heads_first", [True, False])
+def test_many_sequences_with_much_work_per_workgroup(model, workgroups, heads_first):
+    r = np.random.default_rng(7)
+    lens = [(int(r.integers(0, 300)), int(r.integers(0, 2))) for _ in range(70)] + [(900, 1)]
+    run(model, lens, 16, workgroups=workgroups, heads_first=heads_first, garbage=float("nan"), slack_rows=1)
+    run(model, lens, 16, workgroups=workgroups, heads_first=heads_first, window=50)
+
+
 def spread_scales(st):
     """Rows whose sizes differ by powers of ten, in keys and values"""
     gen = torch.Generator().manual_seed(9)
