@@ -89,7 +89,7 @@ tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, Pag
 // Up to 32 query rows per KV head (bf16) go to the split kernel, more to the chunk kernel, the whole call by the sequence with the most: 8 sequences of a 3B
 // layer with 1000 to 16000 cached tokens and 30 rows each take 88 us there and 100 in the chunk kernel, with 33 rows 127 (two items) and 87. (One sequence over
 // 4000: 33 and 30 us with 30 rows, 29 and 30 with 33.)  A plan, a launch of one workgroup and one that joins, is made where items have to be numbered: more than
-// one per sequence and KV head, or more than 64 sequences, a lane each (64 sequences of up to 8000 tokens: 206 us without, 239 with; of up to 1000: 43 and 49).
+// one per sequence and KV head, or more than 64 sequences, a lane each (64 sequences of up to 8000 tokens: 201 us without, 203 with; of up to 1000: 40 and 43).
 void plan_attention(const tkphi_paged_config* c, PagedGeom* g) {
   const int64_t rows = (int64_t)g->max_new * g->G;
   const bool chunk = g->dtype == TKPHI_BF16 && rows > kPagedRows;
