@@ -79,15 +79,19 @@ struct WaveAttend {
   static constexpr int GR = TOK / 8;                              // groups of 8 tokens per tile
 
   // The cached rows of a tile, in groups of 8 tokens; lanes 8 u .. 8 u + 7 (of GR x 8) hold what is said of group u, in vector registers (as scalars they would be
-  // spilled to those): the byte offset of the group's first row (not UNIFORM: off[u], of the lane's row of group u), the position of its first token,
+  // spilled to those): the byte offset of the group's first row (not UNIFORM: of its row lane % 8), the position of its first token,
   // and which of its tokens anyone may see (the rows of the others are readable all the same).
   struct Rows {
-    int64_t off[UNIFORM ? 1 : GR];
+    int64_t off;
     int pos, mask;
     int64_t scale;                                                 // codes: where the scales of token lane % TOK of the tile are
     __device__ __forceinline__ int64_t offset(int u) const {
-      if constexpr (UNIFORM) return of_lane(off[0], 8 * u);
-      else return off[u];
+      if constexpr (UNIFORM) {
+        return of_lane(off, 8 * u);
+      } else {                                                     // (looked up by every lane for all its rows, the lookups took longer than all else)
+        const int from = (8 * u + (threadIdx.x & 7)) * 4;
+        return (int64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(from, (int)(uint32_t)off) | (int64_t)__builtin_amdgcn_ds_bpermute(from, (int)(off >> 32)) << 32;
+      }
     }
     __device__ __forceinline__ int pos_of(int u) const { return __builtin_amdgcn_readlane(pos, 8 * u); }
     __device__ __forceinline__ int mask_of(int u) const { return __builtin_amdgcn_readlane(mask, 8 * u); }
@@ -482,25 +486,17 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
                bool odd = false;
                const int id = page_id(g, seq, pt, &odd), there = from < to ? id : -1;
                bad = bad || (odd && from < to);
-               rows.off[0] = (int64_t)max(there, 0) * g.st_page + (int64_t)in * g.st_tok;
+               rows.off = (int64_t)max(there, 0) * g.st_page + (int64_t)in * g.st_tok;
                rows.pos = t;
                rows.mask = there < 0 ? 0 : ((1 << to) - 1) & ~((1 << from) - 1);
                if constexpr (Wave::CODES) rows.scale = scale_at(g, max(there, 0), h, in) + (lane & 7);
-             } else {
-               const int mine = (lane >> 3) % Wave::GR;
+             } else {                                              // every lane its token
+               const int mine = (lane >> 3) % Wave::GR, t = tb + lane % Wave::TOK, pt = page_of(g, t), in = t - pt * g.by_page.d;
+               const int id = t >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
+               rows.off = (int64_t)max(id, 0) * g.st_page + (int64_t)in * g.st_tok;
                rows.pos = tb + mine * 8;
-#pragma unroll
-               for (int u = 0; u < Wave::GR; ++u) {
-                 const int t = tb + u * 8 + (lane & 7), pt = page_of(g, t);
-                 const int id = t >= it.low && t < t1 ? page_id(g, seq, pt, &bad) : -1;
-                 rows.off[u] = (int64_t)max(id, 0) * g.st_page + (int64_t)(t - pt * g.by_page.d) * g.st_tok;
-                 const int mask = (int)(__ballot(id >= 0) & 0xff);
-                 rows.mask = u == mine ? mask : rows.mask;
-                 if constexpr (Wave::CODES) {
-                   const int64_t at_scale = scale_at(g, max(id, 0), h, t - pt * g.by_page.d);
-                   rows.scale = u == mine ? at_scale : rows.scale;
-                 }
-               }
+               rows.mask = (int)(__ballot(id >= 0) >> (8 * mine) & 0xff);
+               if constexpr (Wave::CODES) rows.scale = scale_at(g, max(id, 0), h, in);
              }
              return rows;
            },
@@ -574,7 +570,7 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
            const int t0 = tile_slot(i), t = t0 + (lane >> 3) % Wave::GR * 8, in = t & (g.block - 1);      // lanes 8 u .. 8 u + 7: group u
            const int2 blk = list[min(t >> shift, head.x - 1)];
            const int page_row = (blk.y % per << shift) + in, pos = (blk.y << shift) + in, n = head.y + 1 - pos;          // tokens up to the query's own
-           rows.off[0] = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)page_row * g.st_tok;
+           rows.off = (int64_t)max(blk.x, 0) * g.st_page + (int64_t)page_row * g.st_tok;
            rows.pos = pos;
            rows.mask = blk.x < 0 || n <= 0 || t >= slots ? 0 : n >= 8 ? 0xff : (1 << n) - 1;
            if constexpr (Wave::CODES) rows.scale = scale_at(g, max(blk.x, 0), h, page_row) + (lane & 7);
