@@ -482,7 +482,8 @@ tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_st
  * The cache in 8 bits.  A key or value row of a token and KV head is d_head codes in OCP e4m3 and a byte b, 1 <= b <= 254; it stands for
  * code x 2^(b - 127), which is a bf16 number.  tkphi_quant_append takes the smallest power of two for which the row's largest finite
  * element is at most 448 times it, within b = 10 .. 247 (a row of zeros: 10), so that an element x is stored within half a step of e4m3 (2^-4 |x|, or
- * 2^-10 of the power of two where that is more); elements that are not finite become NaN.
+ * 2^-10 of the power of two where that is more); elements of 1.9375 2^127 and more, for which half a step would be 2^128, take 240 2^120 (2^-4 |x| too);
+ * elements that are not finite become NaN.
  * Rows, queries and outputs are bf16 (kv_dtype TKPHI_BF16; others: TKPHI_EUNSUPPORTED).  The config's strides count elements, here bytes, multiples of 16.
  * Mean keys are bf16, over the keys as stored. */
 typedef struct tkphi_quant_pool {

@@ -34,13 +34,14 @@ def e4m3(y: np.ndarray) -> np.ndarray:
 
 def quantise(x: np.ndarray):
     """Rows [..., d] -> codes as the numbers they are, exponent bytes b: code * 2^(b - 127) stands for x.  The smallest power of two of which the row's largest
-    finite element is at most 448, b within 10 .. 247."""
+    finite element is at most 448, b within 10 .. 247; of the last one codes up to 240 (256 of it would be 2^128, no bf16 number)."""
     x = np.where(np.isfinite(x), x, np.nan)
     top = np.nan_to_num(np.abs(x), nan=0.0).max(-1)
     b = np.full(top.shape, 10)
     for _ in range(237):
         b = np.where(top > 448 * np.exp2(b - 127.0), b + 1, b)
-    return e4m3(x / np.exp2(b - 127.0)[..., None]), b
+    codes, most = e4m3(x / np.exp2(b - 127.0)[..., None]), np.where(b == 247, 240.0, 448.0)[..., None]
+    return np.clip(codes, -most, most), b
 
 
 def gather(pool: np.ndarray, table, length: int):

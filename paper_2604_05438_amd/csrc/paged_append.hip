@@ -75,6 +75,17 @@ __device__ __forceinline__ uint32_t codes_of(uint32_t a, uint32_t b, float scale
   r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2_t, b), scale, true);
   return __builtin_bit_cast(uint32_t, r);
 }
+// Code 256 (0x78) of the largest power of two would be 2^128, no bf16 number: elements that round to it, from 1.9375 x 2^127 on, take the code before, 240, which is
+// still within 2^-4 of them (by the size x: x - 240 2^120 < 2^-4 x up to 2^128)
+__device__ __forceinline__ uint32_t below_256(uint32_t codes) {
+  const uint32_t other = ((codes & 0x7f7f7f7fu) ^ 0x78787878u) + 0x7f7f7f7fu;        // highest bit of a byte: it is another code
+  return codes - ((~other & 0x80808080u) >> 7);
+}
+__device__ __forceinline__ void keep_finite(Coded& c) {
+  if (c.scale != kMostScale) return;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) { c.x[i] = below_256(c.x[i]); c.y[i] = below_256(c.y[i]); }
+}
 // of 32-bit numbers; their sizes compare as integers
 __device__ __forceinline__ Coded encode(const float* x, const float* y, int lanes) {
   const auto size = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
@@ -92,6 +103,7 @@ __device__ __forceinline__ Coded encode(const float* x, const float* y, int lane
   const float scale = __uint_as_float(c.scale << 23);
   c.x[0] = codes_of(x, scale); c.x[1] = codes_of(x + 4, scale);
   c.y[0] = codes_of(y, scale); c.y[1] = codes_of(y + 4, scale);
+  keep_finite(c);
   return c;
 }
 // of bf16 pairs as they are
@@ -114,6 +126,7 @@ __device__ __forceinline__ Coded encode(u32x4 x, u32x4 y, int lanes) {
   const float scale = __uint_as_float(c.scale << 23);
   c.x[0] = codes_of(x.x, x.y, scale); c.x[1] = codes_of(x.z, x.w, scale);
   c.y[0] = codes_of(y.x, y.y, scale); c.y[1] = codes_of(y.z, y.w, scale);
+  keep_finite(c);
   return c;
 }
 
