@@ -480,10 +480,11 @@ tkphi_status tkphi_block_attention(const tkphi_paged_config* cfg, const tkphi_st
  * Everything said above holds for them: steps, checks, status bits, workspaces (those of tkphi_paged_workspace_bytes), streams, capture.
  *
  * The cache in 8 bits.  A key or value row of a token and KV head is d_head codes in OCP e4m3 and a byte b, 1 <= b <= 254; it stands for
- * code x 2^(b - 127), which is a bf16 number.  tkphi_quant_append takes the smallest power of two for which the row's largest finite
+ * code x 2^(b - 127) as a bf16 number: exactly for b = 3 .. 246 and for what tkphi_quant_append stores, otherwise the nearest one (ties to even),
+ * infinity from 2^128 on.  tkphi_quant_append takes the smallest power of two for which the row's largest finite
  * element is at most 448 times it, within b = 10 .. 247 (a row of zeros: 10), so that an element x is stored within half a step of e4m3 (2^-4 |x|, or
- * 2^-10 of the power of two where that is more); elements of 1.9375 2^127 and more, for which half a step would be 2^128, take 240 2^120 (2^-4 |x| too);
- * elements that are not finite become NaN.
+ * 2^-10 of the power of two where that is more); those that would round to 2^128, from 1.9375 2^127 on, are stored
+ * as 1.875 2^127, also within 2^-4 |x|; elements that are not finite become NaN.
  * Rows, queries and outputs are bf16 (kv_dtype TKPHI_BF16; others: TKPHI_EUNSUPPORTED).  The config's strides count elements, here bytes, multiples of 16.
  * Mean keys are bf16, over the keys as stored. */
 typedef struct tkphi_quant_pool {
@@ -525,7 +526,7 @@ tkphi_status tkphi_quant_attention(const tkphi_paged_config* cfg, const tkphi_st
 tkphi_status tkphi_quant_block_attention(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool,
                                          const tkphi_attention_rows* io, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Tokens [cached, cached + new_tokens) of every sequence of the step, exactly, to the rows that the step gives them.  Tokens of absent pages read as zeros and
+/* Tokens [cached, cached + new_tokens) of every sequence of the step, the numbers that they stand for, to the rows that the step gives them.  Tokens of absent pages read as zeros and
  * are recorded (TKPHI_DEV_BAD_PAGE). */
 tkphi_status tkphi_quant_read(const tkphi_paged_config* cfg, const tkphi_step* step, const tkphi_quant_pool* pool, const tkphi_read_rows* io,
                               void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -104,8 +104,8 @@ void launch_block_select(const PagedGeom& g, hipStream_t s);
 void launch_block_attention(const PagedGeom& g, hipStream_t s);
 
 // A row of the cache in 8 bits: e4m3 codes, and a byte b: the row is codes x 2^(b - 127), the smallest power for which the largest one fits.  A finer scale
-// would gain nothing, the codes are floating point numbers themselves; codes times a power of two are bf16 numbers, which the
-// conversion instruction delivers, so everything behind it is what it is for a bf16 cache.
+// would gain nothing, the codes are floating point numbers themselves; codes times a power of two are bf16 numbers (b = 3 .. 246, and what is stored with
+// kMostScale: codes up to 240), which the conversion instruction delivers, so everything behind it is what it is for a bf16 cache.
 struct Code8 {};
 // the type that rows and outputs have, and bytes of a cached element
 template <typename T> struct Cached {
