@@ -23,7 +23,7 @@ tkphi_status hip_status(hipError_t e, const char* what) {
 }
 
 // Config and step: everything a call and the workspace's size have in common
-// (codes: strides of the pool are those of a cache in 8 bits.  One that is right there is right for the rows' type too.)
+// (codes: strides of the pool are those of a cache in 8 bits)
 tkphi_status check_config(const tkphi_paged_config* c, const tkphi_step* st, PagedGeom* g, bool codes = false) {
   if (!c || !st) { set_error("cfg or step is null"); return TKPHI_EINVAL; }
   if (c->kv_dtype != TKPHI_F32 && c->kv_dtype != TKPHI_BF16) { set_error("kv_dtype=%d is not a tkphi_dtype", c->kv_dtype); return TKPHI_EINVAL; }
@@ -337,7 +337,8 @@ extern "C" {
 
 size_t tkphi_paged_workspace_bytes(const tkphi_paged_config* cfg, const tkphi_step* step) {
   PagedGeom g;
-  if (check_config(cfg, step, &g) != TKPHI_OK) return 0;
+  // (strides of codes pass as strides of bf16 rows, but for tokens of 2^27 and more that are taken by blocks)
+  if (check_config(cfg, step, &g) != TKPHI_OK && (!cfg || cfg->kv_dtype != TKPHI_BF16 || check_config(cfg, step, &g, true) != TKPHI_OK)) return 0;
   return space_of(cfg, g).total;
 }
 
