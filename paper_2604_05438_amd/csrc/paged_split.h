@@ -421,7 +421,7 @@ __device__ __forceinline__ void join_waves(WaveAttend<T, D, RT, STREAM, UNIFORM,
 }
 
 // UNIFORM: 8 tokens always lie in one page
-// STREAM: non-temporal loads, where the cache is read once for sure: every sequence has one item per KV head.  (With several items of a sequence they read the same
+// STREAM: non-temporal loads, where a workgroup is the only one that reads a line: every sequence has one item per KV head, whose rows are whole lines.  (With several items of a sequence they read the same
 // rows.  128 single tokens over up to 8000, which have a plan for their number: 378 us, with plain loads 416.)  WIDE, PAIR: see WaveAttend
 template <typename T, int D, int RT, bool PLAN, bool UNIFORM, bool STREAM, bool WIDE = false, bool PAIR = false>
 __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_attend_kernel(PagedGeom g) {
@@ -535,7 +535,9 @@ __global__ __launch_bounds__(kPagedThreads, attend_per_cu(D, RT)) void paged_att
   if constexpr (PLAN) join.store(g, w);
 }
 
-// ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens
+// ---- over blocks: `splits` workgroups per query token and KV head, each with an equal share of the listed blocks' tokens.  Non-temporal loads: of one token each of 64
+// sequences, 128 blocks of codes of 64 channels, 118 us (plain loads 121), tokens outermost 141 (146), over bf16 139 (152).  Tokens of one sequence read the same blocks in
+// part: 512 of them, d = 128, 479 us over codes and 648 over bf16 (plain loads 441, 637).
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g) {
   using Wave = WaveAttend<T, D, 1, true, true>;
@@ -597,12 +599,13 @@ __global__ __launch_bounds__(kPagedThreads) void block_attend_kernel(PagedGeom g
                       [&](int row, int* t, int* hd) { *t = token; *hd = h * g.G + row; });
 }
 
+static inline bool groups_in_pages(const PagedGeom& g) { return g.by_page.d % 8 == 0 && g.st_tok < (1ll << 28); }       // (offsets of 32 bits within 8 tokens)
 template <typename T, int D, int RT, bool PLAN, bool STREAM>
 static void launch_split(const PagedGeom& g, hipStream_t s) {
-  const bool uniform = g.by_page.d % 8 == 0 && g.st_tok < (1ll << 28);           // (offsets of 32 bits within 8 tokens)
+  const bool uniform = groups_in_pages(g);
   const dim3 grid(g.splits), block(kPagedThreads);
   if constexpr (Cached<T>::codes && D == 64 && RT == 1) {
-    if constexpr (!PLAN)
+    if constexpr (!PLAN && STREAM)
       if (g.pairs) {
         hipLaunchKernelGGL((paged_attend_kernel<T, 128, RT, PLAN, true, STREAM, false, true>), grid, block, 0, s, g);
         return;
@@ -612,12 +615,24 @@ static void launch_split(const PagedGeom& g, hipStream_t s) {
       return;
     }
   }
-  if (uniform) hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, PLAN, true, STREAM>), grid, block, 0, s, g);
-  else hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, PLAN, false, STREAM>), grid, block, 0, s, g);
+  if constexpr (PLAN || STREAM)
+    if (!uniform) {
+      hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, PLAN, false, STREAM>), grid, block, 0, s, g);
+      return;
+    }
+  hipLaunchKernelGGL((paged_attend_kernel<T, D, RT, PLAN, true, STREAM>), grid, block, 0, s, g);
 }
 template <typename T, int D, int RT>
 static void launch_split(const PagedGeom& g, hipStream_t s) {
-  const bool half_lines = Cached<T>::codes && D == 64 && g.st_tok != 64;           // (the other half is another workgroup's: 253 us with STREAM, 225 without)
+  // Codes of 64 channels, tokens outermost: the other half of a line is another workgroup's.  128 single tokens over 4000 to 8000 253 us with STREAM, 219 without, on pages
+  // of 100 tokens 254 and 232; without a plan 3 tokens each of 32 sequences of 2000 to 65000 334 and 251, of 500 to 2000 27.1 and 26.6, one token of three heads
+  // 93 and 91; but on pages of 100 tokens, without a plan, 234 and 259.
+  const bool half_lines = Cached<T>::codes && D == 64 && g.st_tok != 64;
+  if constexpr (Cached<T>::codes && D == 64)
+    if (!g.plan_room && half_lines && !g.pairs && groups_in_pages(g)) {
+      launch_split<T, D, RT, false, false>(g, s);
+      return;
+    }
   if (!g.plan_room) launch_split<T, D, RT, false, true>(g, s);
   else if ((int64_t)g.max_new * g.G <= g.tile_rows && !half_lines) launch_split<T, D, RT, true, true>(g, s);
   else launch_split<T, D, RT, true, false>(g, s);
