@@ -496,7 +496,8 @@ typedef struct tkphi_quant_pool {
   int32_t reserved;      /* 0 */
 } tkphi_quant_pool;
 
-/* y = x / sqrt(mean of x^2 over the head's channels + eps) * (weight + weight_offset), in 32 bits; the rotation follows before the result is rounded. */
+/* y = x / sqrt(mean of x^2 over the head's channels + eps) * (weight + weight_offset), in 32 bits (heads whose squares
+ * sum to 2^128 and more come out as zeros); the rotation follows before the result is rounded. */
 typedef struct tkphi_head_norms {
   const void* q_weight;  /* [n_q_heads][d_head] kv_dtype, stride below; NULL: y = x / sqrt(..)      */
   const void* k_weight;  /* [n_kv_heads][d_head]                                                    */
