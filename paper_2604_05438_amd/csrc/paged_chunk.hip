@@ -477,7 +477,7 @@ __global__ __launch_bounds__(ChunkTile<D>::THREADS) __attribute__((amdgpu_waves_
 
 template <typename T>
 static void launch_chunk(const PagedGeom& g, hipStream_t s) {
-  const bool uniform = g.by_page.d % 16 == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 8 tokens)
+  const bool uniform = g.by_page.d % 16 == 0 && g.st_tok < (1ll << 27);       // (offsets of 32 bits within 16 tokens)
   if (g.d == 64) hipLaunchKernelGGL((uniform ? paged_chunk_kernel<T, 64, true> : paged_chunk_kernel<T, 64, false>), dim3(g.splits), dim3(ChunkTile<64>::THREADS), 0, s, g);
   else hipLaunchKernelGGL((uniform ? paged_chunk_kernel<T, 128, true> : paged_chunk_kernel<T, 128, false>), dim3(g.splits), dim3(ChunkTile<128>::THREADS), 0, s, g);
 }

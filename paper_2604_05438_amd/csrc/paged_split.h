@@ -9,8 +9,9 @@
 // paged_join_kernel does).
 //
 // Bound by the read stream where there is much of it: a step of 32 sequences of a 3B layer, 720000 cached tokens (2.96 GB), 450 us = 6.6 TB/s, as codes (1.49 GB)
-// 235 us = 6.3 TB/s; five tokens each of 8 sequences (283 MB) 61 us.  Short calls are a chain of round trips: a 1B layer over 4002 tokens 8.5 us, of which sequences 0.7, page ids and
-// rows 2.5, the join of the wavefronts 0.6, partials and their count 1.5, the join of 32 pieces 2.5.
+// 235 us = 6.3 TB/s; five tokens each of 8 sequences (283 MB) 61 us.  Short calls are a chain of round trips: a 1B layer over 4002 tokens 8.5 us (as codes 8.2), of which, by the
+// clock in the workgroup that ends last, sequences 1.3 (1.1), queries 0.2, page ids and rows 2.6 (2.0), the join of the wavefronts with the wait for them 0.6 (1.3),
+// partials and their count 0.7, the join of 32 pieces 2.4 (2.3).
 #pragma once
 
 #include "paged_attention.h"
